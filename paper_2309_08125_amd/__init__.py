@@ -13,3 +13,6 @@ from .binding import (  # noqa: F401
     INST_SYMBOLS, Instantiator, oob_inst_count, oob_inst_enumerate, oob_inst_workspace_size,
     OOB_INST_STATIC_BYTES, oob_inst_enumerate_static,
 )
+from .layer import (  # noqa: F401
+    ACTIVATIONS, LAYER_SYMBOLS, linear, linear_backward,
+)

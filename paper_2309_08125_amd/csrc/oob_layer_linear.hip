@@ -1,0 +1,519 @@
+/* Matrix products of a transformer layer: y = act(x W^T + b) + r, and its gradients. */
+#include "oob_layer_device.h"
+
+namespace layer {
+
+/* ---- the product -------------------------------------------------------------------------------------------------------
+ * C[m][n] = sum_k A(m, k) B(n, k), each operand stored with k contiguous (rows of k) or with m (n) contiguous (rows of m per k). */
+struct Product {
+  const void *A, *B;
+  int64_t lda, ldb; /* elements between rows */
+  int64_t M, N, K;
+  /* epilogue: v = act(sum + bias[n]) + residual[m][n]; z gets sum + bias[n] */
+  const void *bias, *residual;
+  int64_t ldr;
+  void *C, *Z;
+  int64_t ldc, ldz;
+  float *partial; /* [splits][M][N] sums in place of the epilogue, or null */
+  int act, splits, whole; /* whole: every row of C, Z and residual starts at 16 bytes and N % 8 == 0 */
+  int tiles_m, tiles_n;
+};
+
+constexpr int KSTEP = 64; /* depth of a step: 128-byte rows of k */
+
+__device__ inline float activate(float z, int act) {
+  switch (act) {
+    case OOB_ACT_RELU: return z > 0 ? z : (z != z ? z : 0.f);
+    case OOB_ACT_SILU: return z / (1 + __expf(-z));
+    case OOB_ACT_GELU: return 0.5f * z * (1 + erff(z * 0.70710678f));
+    case OOB_ACT_GELU_TANH: return z / (1 + __expf(-1.5957691216f * (z + 0.044715f * z * z * z)));
+    default: return z;
+  }
+}
+
+/* act'(z) */
+__device__ inline float slope(float z, int act) {
+  switch (act) {
+    case OOB_ACT_RELU: return z > 0 ? 1.f : 0.f;
+    case OOB_ACT_SILU: { float e = 1 / (1 + __expf(-z)); return e * (1 + z * (1 - e)); }
+    case OOB_ACT_GELU: return 0.5f * (1 + erff(z * 0.70710678f)) + z * 0.39894228f * __expf(-0.5f * z * z);
+    case OOB_ACT_GELU_TANH: {
+      /* 0.5 (1 + tanh(u)) = 1 / (1 + exp(-2 u)) = e;  its derivative is 2 e (1 - e) u' */
+      float e = 1 / (1 + __expf(-1.5957691216f * (z + 0.044715f * z * z * z)));
+      return e + z * 2 * e * (1 - e) * 0.7978845608f * (1 + 0.134145f * z * z);
+    }
+    default: return 1.f;
+  }
+}
+
+/* One operand's tile of ROWS (m or n) x KSTEP in LDS and the way from memory to there and to registers.
+ * k contiguous: ROWS rows of 128 bytes, eight 16-byte chunks, chunk c of row r at c ^ (r / 2) % 8: sixteen lanes that read one chunk
+ * of sixteen rows then meet all 64 banks.  m contiguous: KSTEP rows of 2 ROWS bytes, chunk c of row k at c ^ 4 (k % 4) (64-row tiles:
+ * c ^ 4 (k / 2 % 2)): the four rows of a transposed read lie in different quarters of the banks. */
+template <class E, int ROWS, int THREADS, bool KC> struct Tile {
+  static constexpr int BYTES = ROWS * KSTEP * 2;
+  static constexpr int LOADS = BYTES / (THREADS * 16);
+  uint32_t off[LOADS]; /* this lane's byte offsets from the start of the step */
+  int at[LOADS];       /* first k of the 16 bytes (k contiguous) or the row k */
+
+  __device__ void init(int64_t ld, int64_t left) { /* left: rows (m or n) there are from the tile's first on */
+    for (int i = 0; i < LOADS; i++) {
+      int p = (i * THREADS + threadIdx.x) * 16;
+      if (KC) {
+        int r = p / 128, c = (p / 16 % 8) ^ (r / 2 % 8);
+        at[i] = c * 8;
+        off[i] = r < left ? (uint32_t)(r * ld * 2 + c * 16) : OOB_LAYER_OUT;
+      } else {
+        constexpr int CH = ROWS / 8;
+        int k = p / (ROWS * 2), c = (p / 16 % CH) ^ (ROWS == 64 ? k / 2 % 2 * 4 : k % 4 * 4);
+        at[i] = k;
+        off[i] = c * 8 < left ? (uint32_t)(k * ld * 2 + c * 16) : OOB_LAYER_OUT;
+      }
+    }
+  }
+  /* Asks for the step that starts at `base`; kleft: values of k there are from here on. */
+  __device__ void load(const char *base, lds_char *to, int64_t kleft) {
+    __amdgpu_buffer_rsrc_t r = buffer(base);
+    int wave = uniform(threadIdx.x / 64);
+#pragma unroll
+    for (int i = 0; i < LOADS; i++)
+      load_lds(r, to + (i * THREADS + wave * 64) * 16, at[i] < kleft ? off[i] : OOB_LAYER_OUT);
+  }
+};
+
+/* Fragment reads: the lane's byte offsets in a tile for a wave whose rows start at w0 (a multiple of 32). */
+template <class E, int ROWS, int FR, bool KC> struct Fragment {
+  int o[KC ? 4 : FR];
+  __device__ void init(int w0) {
+    int l = lane(), h = l >> 5;
+    if (KC) {
+      int r = w0 + (l & 31);
+      for (int s = 0; s < 4; s++) o[s] = r * 128 + (((2 * s + h) ^ (r / 2 % 8)) * 16);
+    } else {
+      int j = (l & 15) >> 2, k = 8 * h + j;
+      int x = ROWS == 64 ? k / 2 % 2 * 4 : k % 4 * 4;
+      for (int i = 0; i < FR; i++) o[i] = k * ROWS * 2 + ((((w0 + 32 * i) / 8 + ((l >> 4) & 1) * 2 + ((l >> 1) & 1)) ^ x) * 16) + (l & 1) * 8;
+    }
+  }
+  __device__ typename Vec<E>::v8 read(lds_char *tile, int i, int s) const {
+    if (KC) return lds_read8<E>(tile + o[s] + i * 32 * 128);
+    lds_char *p = tile + o[i] + s * 16 * ROWS * 2;
+    return lds_read_tr<E>(p, p + 4 * ROWS * 2);
+  }
+};
+
+template <class E> __device__ inline typename Vec<E>::v8 load8(const E *p, bool whole, int64_t left) {
+  if (whole) return *(const typename Vec<E>::v8 *)p;
+  typename Vec<E>::v8 v;
+  for (int e = 0; e < 8; e++) v[e] = e < left ? p[e] : (E)0.f;
+  return v;
+}
+template <class E> __device__ inline void store8(E *p, typename Vec<E>::v8 v, bool whole, int64_t left) {
+  if (whole) *(typename Vec<E>::v8 *)p = v;
+  else
+    for (int e = 0; e < 8; e++)
+      if (e < left) p[e] = v[e];
+}
+
+/* Eight consecutive values of one row through the epilogue. */
+template <class E> __device__ inline void epilogue(const Product &g, int64_t m, int64_t n, float *v) {
+  int64_t left = g.N - n;
+  if (g.bias) {
+    const E *b = (const E *)g.bias + n;
+    for (int e = 0; e < 8; e++) v[e] += e < left ? (float)b[e] : 0.f;
+  }
+  typename Vec<E>::v8 out;
+  if (g.Z) {
+    for (int e = 0; e < 8; e++) out[e] = (E)v[e];
+    store8<E>((E *)g.Z + m * g.ldz + n, out, g.whole, left);
+  }
+  if (g.act != OOB_ACT_NONE)
+    for (int e = 0; e < 8; e++) v[e] = activate(v[e], g.act);
+  if (g.residual) {
+    typename Vec<E>::v8 r = load8<E>((const E *)g.residual + m * g.ldr + n, g.whole, left);
+    for (int e = 0; e < 8; e++) v[e] += (float)r[e];
+  }
+  for (int e = 0; e < 8; e++) out[e] = (E)v[e];
+  store8<E>((E *)g.C + m * g.ldc + n, out, g.whole, left);
+}
+
+template <class E, int TM, int TN, int WM, int WN, bool AK, bool BK>
+__global__ __launch_bounds__(WM *WN * 64, 2) void k_product(Product g) {
+  constexpr int THREADS = WM * WN * 64, FM = TM / WM / 32, FN = TN / WN / 32;
+  using TA = Tile<E, TM, THREADS, AK>;
+  using TB = Tile<E, TN, THREADS, BK>;
+  constexpr int STAGE = TA::BYTES + TB::BYTES, PITCH = FN * 32 + 4;
+  constexpr int EPI = WM * WN * 32 * PITCH * 4;
+  __shared__ __attribute__((aligned(1024))) char mem[2 * STAGE > EPI ? 2 * STAGE : EPI];
+  lds_char *lds = (lds_char *)mem;
+
+  /* tiles of C in bands of eight rows of tiles, so that consecutive workgroups of an XCD share rows of both operands in its L2 */
+  int64_t tiles = (int64_t)g.tiles_m * g.tiles_n;
+  int64_t id = xcd_order(blockIdx.x, tiles * g.splits);
+  int split = (int)(id / tiles);
+  id %= tiles;
+  constexpr int BAND = 8;
+  int64_t band = id / (BAND * (int64_t)g.tiles_n);
+  int high = (int)(g.tiles_m - band * BAND < BAND ? g.tiles_m - band * BAND : BAND);
+  int64_t in = id - band * BAND * g.tiles_n;
+  int64_t m0 = (band * BAND + in % high) * TM, n0 = in / high * TN;
+
+  int steps = (int)((g.K + KSTEP - 1) / KSTEP);
+  int first = (int)((int64_t)steps * split / g.splits), last = (int)((int64_t)steps * (split + 1) / g.splits);
+
+  TA ta;
+  TB tb;
+  ta.init(g.lda, g.M - m0);
+  tb.init(g.ldb, g.N - n0);
+  const char *pa = (const char *)g.A + (AK ? m0 * g.lda + (int64_t)first * KSTEP : (int64_t)first * KSTEP * g.lda + m0) * 2;
+  const char *pb = (const char *)g.B + (BK ? n0 * g.ldb + (int64_t)first * KSTEP : (int64_t)first * KSTEP * g.ldb + n0) * 2;
+  int64_t da = AK ? KSTEP * 2 : KSTEP * 2 * g.lda, db = BK ? KSTEP * 2 : KSTEP * 2 * g.ldb;
+  int64_t kleft = g.K - (int64_t)first * KSTEP;
+
+  int wave = uniform(threadIdx.x / 64), wm = wave / WN, wn = wave % WN;
+  Fragment<E, TM, FM, AK> fa;
+  Fragment<E, TN, FN, BK> fb;
+  fa.init(wm * FM * 32);
+  fb.init(wn * FN * 32);
+
+  f32x16 acc[FM][FN];
+  for (int i = 0; i < FM; i++)
+    for (int j = 0; j < FN; j++)
+      for (int r = 0; r < 16; r++) acc[i][j][r] = 0;
+
+  if (first < last) {
+    ta.load(pa, lds, kleft);
+    tb.load(pb, lds + TA::BYTES, kleft);
+  }
+  for (int t = first; t < last; t++) {
+    wait_barrier(); /* the step's loads have landed, and nobody reads the other buffer any more */
+    lds_char *now = lds + (t - first) % 2 * STAGE, *next = lds + (t - first + 1) % 2 * STAGE;
+    pa += da, pb += db, kleft -= KSTEP;
+    if (t + 1 < last) {
+      ta.load(pa, next, kleft);
+      tb.load(pb, next + TA::BYTES, kleft);
+    }
+#pragma unroll
+    for (int s = 0; s < 4; s++) {
+      typename Vec<E>::v8 a[FM], b[FN];
+#pragma unroll
+      for (int i = 0; i < FM; i++) a[i] = fa.read(now, i, s);
+#pragma unroll
+      for (int j = 0; j < FN; j++) b[j] = fb.read(now + TA::BYTES, j, s);
+#pragma unroll
+      for (int i = 0; i < FM; i++)
+#pragma unroll
+        for (int j = 0; j < FN; j++) acc[i][j] = mfma(b[j], a[i], acc[i][j]); /* lane: m, registers: n */
+    }
+  }
+  __syncthreads();
+
+  /* 32 rows of m at a time through the wave's own part of LDS, so that a row of C is written in one go */
+  __attribute__((address_space(3))) float *stage = (__attribute__((address_space(3))) float *)lds + wave * 32 * PITCH;
+  int l = lane();
+  constexpr int LPR = FN * 4, RPP = 64 / LPR; /* lanes per row, rows per pass */
+#pragma unroll
+  for (int i = 0; i < FM; i++) {
+#pragma unroll
+    for (int j = 0; j < FN; j++)
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        *(__attribute__((address_space(3))) f32x4 *)(stage + (l & 31) * PITCH + j * 32 + 8 * q + 4 * (l >> 5)) = v;
+      }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int p = 0; p < 32 / RPP; p++) {
+      int row = p * RPP + l / LPR;
+      int64_t m = m0 + (wm * FM + i) * 32 + row, n = n0 + wn * FN * 32 + l % LPR * 8;
+      float v[8];
+      for (int e = 0; e < 8; e += 4) *(f32x4 *)(v + e) = *(__attribute__((address_space(3))) f32x4 *)(stage + row * PITCH + l % LPR * 8 + e);
+      if (m < g.M && n < g.N) {
+        if (g.partial) {
+          float *to = g.partial + ((int64_t)split * g.M + m) * g.N + n;
+          for (int e = 0; e < 8; e++)
+            if (n + e < g.N) to[e] = v[e];
+        } else {
+          epilogue<E>(g, m, n, v);
+        }
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+/* Joins the parts of a product whose k was split. */
+template <class E> __global__ __launch_bounds__(256) void k_join(Product g) {
+  int64_t per = (g.N + 7) / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  int64_t m = id / per, n = id % per * 8;
+  if (m >= g.M) return;
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int s = 0; s < g.splits; s++) {
+    const float *p = g.partial + ((int64_t)s * g.M + m) * g.N + n;
+    for (int e = 0; e < 8; e++) v[e] += n + e < g.N ? p[e] : 0.f;
+  }
+  epilogue<E>(g, m, n, v);
+}
+
+/* ---- rows of another pitch: what the product's loads cannot take (rows that do not start at 16 bytes, a ragged contiguous axis)
+ * goes to the workspace first, in rows of a multiple of 8 with zeros behind. */
+struct Packed { const uint16_t *from; uint16_t *to; int64_t rows, cols, ld, ld_to; };
+
+__global__ __launch_bounds__(256) void k_pack(Packed p) {
+  int64_t per = p.ld_to / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  int64_t r = id / per, c = id % per * 8;
+  if (r >= p.rows) return;
+  i16x8 v;
+  for (int e = 0; e < 8; e++) v[e] = c + e < p.cols ? (short)p.from[r * p.ld + c + e] : (short)0;
+  *(i16x8 *)(p.to + r * p.ld_to + c) = v;
+}
+
+/* ---- dz = dy act'(z), and the sums of its columns ------------------------------------------------------------------------
+ * A workgroup takes 512 columns (64 lanes x 8) and a run of rows, four rows at a time, and leaves one row of sums. */
+struct ActGrad {
+  const void *dy, *z;
+  void *dz; /* rows of a multiple of 8; null: act is none, dz is dy */
+  int64_t ld_dy, ld_z, ld_dz, T, N;
+  float *sums; /* [runs][N] or null */
+  int64_t rows; /* of a run */
+  int act, whole;
+};
+
+template <class E> __global__ __launch_bounds__(256) void k_act_grad(ActGrad g) {
+  __shared__ float part[4][512 + 8];
+  int64_t n = (int64_t)blockIdx.x * 512 + lane() * 8, left = g.N - n;
+  int64_t t1 = ((int64_t)blockIdx.y + 1) * g.rows < g.T ? ((int64_t)blockIdx.y + 1) * g.rows : g.T;
+  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (left > 0)
+#pragma unroll 4
+    for (int64_t t = (int64_t)blockIdx.y * g.rows + threadIdx.x / 64; t < t1; t += 4) {
+      typename Vec<E>::v8 d = load8<E>((const E *)g.dy + t * g.ld_dy + n, g.whole, left), out;
+      if (g.dz) {
+        typename Vec<E>::v8 z = d;
+        if (g.act != OOB_ACT_NONE) z = load8<E>((const E *)g.z + t * g.ld_z + n, g.whole, left);
+        for (int e = 0; e < 8; e++) {
+          float v = (float)d[e] * slope((float)z[e], g.act);
+          out[e] = (E)v;
+          sum[e] += v; /* before the rounding: the bias's gradient does not see it */
+        }
+        store8<E>((E *)g.dz + t * g.ld_dz + n, out, true, left); /* past N: zeros */
+      } else {
+        for (int e = 0; e < 8; e++) sum[e] += (float)d[e];
+      }
+    }
+  if (!g.sums) return;
+  for (int e = 0; e < 8; e++) part[threadIdx.x / 64][lane() * 8 + e] = sum[e];
+  __syncthreads();
+  for (int c = threadIdx.x; c < 512; c += 256) {
+    int64_t at = (int64_t)blockIdx.x * 512 + c;
+    if (at < g.N) g.sums[blockIdx.y * g.N + at] = (part[0][c] + part[1][c]) + (part[2][c] + part[3][c]);
+  }
+}
+
+template <class E> __global__ __launch_bounds__(256) void k_sum_rows(const float *sums, int64_t runs, int64_t N, E *out) {
+  __shared__ float part[4][64];
+  int64_t n = (int64_t)blockIdx.x * 64 + lane();
+  float s = 0;
+  if (n < N)
+    for (int64_t r = threadIdx.x / 64; r < runs; r += 4) s += sums[r * N + n];
+  part[threadIdx.x / 64][lane()] = s;
+  __syncthreads();
+  if (threadIdx.x < 64 && n < N) out[n] = (E)((part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]));
+}
+
+/* ---- host ------------------------------------------------------------------------------------------------------------------ */
+struct Operand { const void *p; int64_t ld, rows, cols; }; /* stored rows x cols, ld elements apart */
+
+static inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+static inline size_t up_bytes(size_t x) { return (x + 255) / 256 * 256; }
+
+static inline bool aligned16(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+
+/* What the loads to LDS can take: 16-byte pieces of rows that end with the row, offsets within a tile below 2^31. */
+static bool loadable(const Operand &o) { return o.cols % 8 == 0 && aligned16(o.p, o.ld) && o.ld < (1 << 21); }
+
+/* Memory handed out in order; sizes alone when there is none. */
+struct Arena {
+  char *base;
+  size_t used;
+  void *take(size_t bytes) {
+    void *p = base ? base + used : nullptr;
+    used += up_bytes(bytes);
+    return p;
+  }
+};
+
+struct Shape { int tile, splits; };
+
+/* Which tile and how many parts of k.  A step of the large tile costs a compute unit as much as four of the middle one, but reads half
+ * as much per product; below 256 tiles units stand idle.  So: the largest tile that gives (nearly) every unit one; the smallest,
+ * with k split until there are two workgroups a unit and no part has under four steps, where none does. */
+static Shape choose(int64_t M, int64_t N, int64_t K) {
+  auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
+  int64_t steps = (K + KSTEP - 1) / KSTEP;
+  if (tiles(256) >= 192) return {256, 1};
+  if (tiles(128) >= 192) return {128, 1};
+  int64_t n = tiles(64), s = 1;
+  while (n * s < 512 && steps / (s * 2) >= 4 && s < 32) s *= 2;
+  return {64, (int)s};
+}
+
+static size_t product_workspace(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K) {
+  Arena w{nullptr, 0};
+  if (!loadable(a)) w.take((size_t)a.rows * up(a.cols, 8) * 2);
+  if (!loadable(b)) w.take((size_t)b.rows * up(b.cols, 8) * 2);
+  Shape s = choose(M, N, K);
+  if (s.splits > 1) w.take((size_t)s.splits * M * N * 4);
+  return w.used;
+}
+
+static Operand pack(const Operand &o, Arena &w, hipStream_t st) {
+  if (loadable(o)) return o;
+  int64_t ld = up(o.cols, 8);
+  void *to = w.take((size_t)o.rows * ld * 2);
+  int64_t n = o.rows * (ld / 8);
+  if (n) k_pack<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(Packed{(const uint16_t *)o.p, (uint16_t *)to, o.rows, o.cols, o.ld, ld});
+  return {to, ld, o.rows, ld};
+}
+
+template <class E, bool AK, bool BK> static void launch(const Product &g, int tile, hipStream_t st) {
+  unsigned n = (unsigned)((int64_t)g.tiles_m * g.tiles_n * g.splits);
+  if (tile == 256) k_product<E, 256, 256, 2, 4, AK, BK><<<n, 512, 0, st>>>(g);
+  else if (tile == 128) k_product<E, 128, 128, 2, 2, AK, BK><<<n, 256, 0, st>>>(g);
+  else k_product<E, 64, 64, 2, 2, AK, BK><<<n, 256, 0, st>>>(g);
+  if (g.splits > 1) k_join<E><<<(unsigned)((g.M * ((g.N + 7) / 8) + 255) / 256), 256, 0, st>>>(g);
+}
+
+/* The product with its operands as they are stored: ak (bk) says that k is contiguous. */
+template <class E> static void product(Operand a, bool ak, Operand b, bool bk, Product g, Arena &w, hipStream_t st) {
+  if (g.M == 0 || g.N == 0) return;
+  Shape s = choose(g.M, g.N, g.K);
+  a = pack(a, w, st);
+  b = pack(b, w, st);
+  g.A = a.p, g.lda = a.ld, g.B = b.p, g.ldb = b.ld;
+  g.splits = s.splits;
+  g.partial = s.splits > 1 ? (float *)w.take((size_t)s.splits * g.M * g.N * 4) : nullptr;
+  g.tiles_m = (int)((g.M + s.tile - 1) / s.tile), g.tiles_n = (int)((g.N + s.tile - 1) / s.tile);
+  g.whole = g.N % 8 == 0 && aligned16(g.C, g.ldc) && (!g.Z || aligned16(g.Z, g.ldz)) && (!g.residual || aligned16(g.residual, g.ldr));
+  if (ak && bk) launch<E, true, true>(g, s.tile, st);
+  else if (ak) launch<E, true, false>(g, s.tile, st);
+  else launch<E, false, false>(g, s.tile, st);
+}
+
+static bool sizes_ok(int dtype, int act, int64_t T, int64_t N, int64_t K) {
+  const int64_t most = (int64_t)1 << 31;
+  return (dtype == OOB_BF16 || dtype == OOB_FP16) && act >= 0 && act < OOB_ACTS && T >= 0 && N >= 1 && K >= 1 && T < most && N < most && K < most;
+}
+static bool fits(int64_t a, int64_t b) { /* workgroups of the smallest tile and its parts */
+  return ((a + 63) / 64) * ((b + 63) / 64) < ((int64_t)1 << 31) / 64;
+}
+
+static int64_t runs_of(int64_t T, int64_t N) { /* runs of rows of k_act_grad: about 1024 workgroups, 16 rows at least */
+  int64_t r = 1024 / ((N + 511) / 512);
+  if (r > (T + 15) / 16) r = (T + 15) / 16;
+  return r < 1 ? 1 : r;
+}
+
+static size_t linear_bytes(const oob_linear *p) {
+  return product_workspace({p->x, p->x_stride, p->T, p->K}, {p->w, p->w_stride, p->N, p->K}, p->T, p->N, p->K);
+}
+
+template <class E> static void linear(const oob_linear *p, Arena w, hipStream_t st) {
+  Product g{};
+  g.M = p->T, g.N = p->N, g.K = p->K;
+  g.bias = p->bias, g.residual = p->residual, g.ldr = p->residual_stride;
+  g.C = p->y, g.ldc = p->y_stride, g.Z = p->z, g.ldz = p->z_stride, g.act = p->act;
+  product<E>({p->x, p->x_stride, p->T, p->K}, true, {p->w, p->w_stride, p->N, p->K}, true, g, w, st);
+}
+
+/* dz in the workspace (rows of a multiple of 8, zeros behind) where there is an activation or the products cannot load dy as it is;
+ * then the sums of the bias's gradient and what the larger product takes */
+static bool makes_dz(const oob_linear_grad *p) { return p->act != OOB_ACT_NONE || !loadable({p->dy, p->dy_stride, p->T, p->N}); }
+static Operand dz_of(const oob_linear_grad *p, Arena &w) {
+  if (!makes_dz(p)) return {p->dy, p->dy_stride, p->T, p->N};
+  int64_t ld = up(p->N, 8);
+  return {w.take((size_t)p->T * ld * 2), ld, p->T, ld};
+}
+
+static size_t grad_bytes(const oob_linear_grad *p) {
+  Arena w{nullptr, 0};
+  Operand dz = dz_of(p, w);
+  if (p->db) w.take((size_t)runs_of(p->T, p->N) * p->N * 4);
+  size_t dx = p->dx ? product_workspace(dz, {p->w, p->w_stride, p->N, p->K}, p->T, p->K, p->N) : 0;
+  size_t dw = p->dw ? product_workspace(dz, {p->x, p->x_stride, p->T, p->K}, p->N, p->K, p->T) : 0;
+  return w.used + (dx > dw ? dx : dw);
+}
+
+template <class E> static void linear_grad(const oob_linear_grad *p, Arena w, hipStream_t st) {
+  Operand dz = dz_of(p, w);
+  float *sums = p->db ? (float *)w.take((size_t)runs_of(p->T, p->N) * p->N * 4) : nullptr;
+  bool makes = makes_dz(p);
+  if (makes || sums) {
+    ActGrad a{};
+    a.dy = p->dy, a.ld_dy = p->dy_stride, a.z = p->z, a.ld_z = p->z_stride;
+    a.dz = makes ? const_cast<void *>(dz.p) : nullptr, a.ld_dz = dz.ld;
+    a.T = p->T, a.N = p->N, a.sums = sums, a.act = p->act;
+    int64_t runs = runs_of(p->T, p->N);
+    a.rows = (p->T + runs - 1) / runs;
+    a.whole = p->N % 8 == 0 && aligned16(p->dy, p->dy_stride) && (p->act == OOB_ACT_NONE || aligned16(p->z, p->z_stride));
+    k_act_grad<E><<<dim3((unsigned)((p->N + 511) / 512), (unsigned)runs), 256, 0, st>>>(a);
+    if (sums) k_sum_rows<E><<<(unsigned)((p->N + 63) / 64), 256, 0, st>>>(sums, runs, p->N, (E *)p->db);
+  }
+  if (p->dx) {
+    Product g{};
+    g.M = p->T, g.N = p->K, g.K = p->N, g.C = p->dx, g.ldc = p->dx_stride;
+    product<E>(dz, true, {p->w, p->w_stride, p->N, p->K}, false, g, w, st);
+  }
+  if (p->dw) {
+    Product g{};
+    g.M = p->N, g.N = p->K, g.K = p->T, g.C = p->dw, g.ldc = p->dw_stride;
+    product<E>(dz, false, {p->x, p->x_stride, p->T, p->K}, false, g, w, st);
+  }
+}
+
+static bool even(const void *p) { return ((uintptr_t)p & 1) == 0; }
+
+}  // namespace layer
+
+using namespace layer;
+
+extern "C" size_t oob_layer_linear_workspace_size(const oob_linear *p) {
+  return p && sizes_ok(p->dtype, p->act, p->T, p->N, p->K) ? linear_bytes(p) : 0;
+}
+
+extern "C" int oob_layer_linear(const oob_linear *p, void *workspace, size_t bytes, void *stream) {
+  if (!p || !sizes_ok(p->dtype, p->act, p->T, p->N, p->K) || !fits(p->T, p->N)) return OOB_EINVAL;
+  if (p->T == 0) return OOB_OK;
+  if (!p->x || !p->w || !p->y || p->x_stride < p->K || p->w_stride < p->K || p->y_stride < p->N) return OOB_EINVAL;
+  if ((p->residual && p->residual_stride < p->N) || (p->z && p->z_stride < p->N)) return OOB_EINVAL;
+  if (!even(p->x) || !even(p->w) || !even(p->y) || !even(p->bias) || !even(p->residual) || !even(p->z)) return OOB_EINVAL;
+  if ((uintptr_t)workspace & 255) return OOB_EINVAL;
+  size_t need = linear_bytes(p);
+  if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
+  Arena w{(char *)workspace, 0};
+  if (p->dtype == OOB_BF16) linear<bf16>(p, w, (hipStream_t)stream);
+  else linear<fp16>(p, w, (hipStream_t)stream);
+  return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
+}
+
+extern "C" size_t oob_layer_linear_backward_workspace_size(const oob_linear_grad *p) {
+  return p && sizes_ok(p->dtype, p->act, p->T, p->N, p->K) ? grad_bytes(p) : 0;
+}
+
+extern "C" int oob_layer_linear_backward(const oob_linear_grad *p, void *workspace, size_t bytes, void *stream) {
+  if (!p || !sizes_ok(p->dtype, p->act, p->T, p->N, p->K) || !fits(p->T, p->N) || !fits(p->T, p->K) || !fits(p->N, p->K)) return OOB_EINVAL;
+  if (p->T && (!p->dy || p->dy_stride < p->N)) return OOB_EINVAL;
+  if (p->T && p->act != OOB_ACT_NONE && (!p->z || p->z_stride < p->N)) return OOB_EINVAL;
+  if (p->T && p->dx && (!p->w || p->w_stride < p->K || p->dx_stride < p->K)) return OOB_EINVAL;
+  if (p->dw && ((p->T && (!p->x || p->x_stride < p->K)) || p->dw_stride < p->K)) return OOB_EINVAL;
+  if (!even(p->dy) || !even(p->x) || !even(p->w) || !even(p->z) || !even(p->dx) || !even(p->dw) || !even(p->db)) return OOB_EINVAL;
+  if ((uintptr_t)workspace & 255) return OOB_EINVAL;
+  size_t need = grad_bytes(p);
+  if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
+  Arena w{(char *)workspace, 0};
+  if (p->dtype == OOB_BF16) linear_grad<bf16>(p, w, (hipStream_t)stream);
+  else linear_grad<fp16>(p, w, (hipStream_t)stream);
+  return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
+}
