@@ -14,5 +14,5 @@ from .binding import (  # noqa: F401
     OOB_INST_STATIC_BYTES, oob_inst_enumerate_static,
 )
 from .layer import (  # noqa: F401
-    ACTIVATIONS, LAYER_SYMBOLS, linear, linear_backward,
+    ACTIVATIONS, LAYER_SYMBOLS, dropout, linear, linear_backward, residual_norm, residual_norm_backward,
 )

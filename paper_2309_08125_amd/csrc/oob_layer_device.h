@@ -71,7 +71,71 @@ __device__ inline int64_t xcd_order(int64_t id, int64_t n) {
   return x * per + (x < more ? x : more) + id / 8;
 }
 
-template <class E> __device__ inline float to_float(E x) { return (float)x; }
+/* Eight consecutive values of a row, `left` of them in it.  Rows start anywhere: memory takes 16-byte accesses at any address. */
+template <class E> struct Loose { typedef typename Vec<E>::v8 v8 __attribute__((aligned(sizeof(E)))); };
+template <class E> __device__ inline typename Vec<E>::v8 load8(const E *p, int64_t left) {
+  if (left >= 8) return *(const typename Loose<E>::v8 *)p;
+  typename Vec<E>::v8 v;
+  for (int e = 0; e < 8; e++) v[e] = e < left ? p[e] : (E)0.f;
+  return v;
+}
+template <class E> __device__ inline void store8(E *p, typename Vec<E>::v8 v, int64_t left) {
+  if (left >= 8) *(typename Loose<E>::v8 *)p = v;
+  else
+    for (int e = 0; e < 8; e++)
+      if (e < left) p[e] = v[e];
+}
+
+/* ---- random bits from a counter: word n of the SplitMix64 sequence (Steele, Lea, Flood 2014) whose state starts at `key` ---- */
+__host__ __device__ inline uint64_t mix64(uint64_t z) {
+  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+  return z ^ (z >> 31);
+}
+struct Dropout {
+  uint64_t key, offset;
+  uint32_t threshold; /* an element is kept where its 16 bits are not below this; 0: no dropout */
+  float scale;        /* 65536 / (65536 - threshold): the mean stays exactly, p being rounded to a multiple of 2^-16 */
+};
+static inline Dropout dropout_of(float p, uint64_t seed, uint64_t offset) {
+  uint32_t t = (uint32_t)((double)p * 65536 + 0.5);
+  return {mix64(seed), offset, t, (float)(65536.0 / (65536 - t))};
+}
+/* The 16 bits of elements i .. i + 7: element n has bits 16 (n % 4) .. + 15 of word n / 4. */
+__device__ inline void random8(const Dropout &d, uint64_t i, uint64_t &lo, uint64_t &hi) {
+  uint64_t n = d.offset + i;
+  uint64_t at = d.key + ((n >> 2) + 1) * 0x9E3779B97F4A7C15ull;
+  int shift = (int)(n & 3) * 16;
+  lo = mix64(at);
+  hi = mix64(at + 0x9E3779B97F4A7C15ull);
+  if (shift) {
+    uint64_t more = mix64(at + 2 * 0x9E3779B97F4A7C15ull);
+    lo = lo >> shift | hi << (64 - shift);
+    hi = hi >> shift | more << (64 - shift);
+  }
+}
+/* keep / (1 - p) of element e of random8's */
+__device__ inline float keep(const Dropout &d, uint64_t lo, uint64_t hi, int e) {
+  uint32_t bits = (uint32_t)((e < 4 ? lo : hi) >> (e % 4 * 16)) & 0xffff;
+  return bits >= d.threshold ? d.scale : 0.f;
+}
+
+/* ---- host ---- */
+static inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+/* Memory handed out in order, 256 bytes apart; sizes alone when there is none.  ok() before anything that was taken is used. */
+struct Arena {
+  char *base;
+  size_t size, used;
+  void *take(size_t bytes) {
+    void *p = base ? base + used : nullptr;
+    used += (bytes + 255) / 256 * 256;
+    return p;
+  }
+  bool ok() const { return used <= size; }
+};
+
+static inline bool multiple(const void *p, size_t of) { return (uintptr_t)p % of == 0; }
 
 }  // namespace layer
 #endif

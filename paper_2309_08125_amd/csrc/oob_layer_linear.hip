@@ -15,7 +15,7 @@ struct Product {
   void *C, *Z;
   int64_t ldc, ldz;
   float *partial; /* [splits][M][N] sums in place of the epilogue, or null */
-  int act, splits, whole; /* whole: every row of C, Z and residual starts at 16 bytes and N % 8 == 0 */
+  int act, splits;
   int tiles_m, tiles_n;
 };
 
@@ -102,19 +102,6 @@ template <class E, int ROWS, int FR, bool KC> struct Fragment {
   }
 };
 
-template <class E> __device__ inline typename Vec<E>::v8 load8(const E *p, bool whole, int64_t left) {
-  if (whole) return *(const typename Vec<E>::v8 *)p;
-  typename Vec<E>::v8 v;
-  for (int e = 0; e < 8; e++) v[e] = e < left ? p[e] : (E)0.f;
-  return v;
-}
-template <class E> __device__ inline void store8(E *p, typename Vec<E>::v8 v, bool whole, int64_t left) {
-  if (whole) *(typename Vec<E>::v8 *)p = v;
-  else
-    for (int e = 0; e < 8; e++)
-      if (e < left) p[e] = v[e];
-}
-
 /* Eight consecutive values of one row through the epilogue. */
 template <class E> __device__ inline void epilogue(const Product &g, int64_t m, int64_t n, float *v) {
   int64_t left = g.N - n;
@@ -125,16 +112,16 @@ template <class E> __device__ inline void epilogue(const Product &g, int64_t m, 
   typename Vec<E>::v8 out;
   if (g.Z) {
     for (int e = 0; e < 8; e++) out[e] = (E)v[e];
-    store8<E>((E *)g.Z + m * g.ldz + n, out, g.whole, left);
+    store8<E>((E *)g.Z + m * g.ldz + n, out, left);
   }
   if (g.act != OOB_ACT_NONE)
     for (int e = 0; e < 8; e++) v[e] = activate(v[e], g.act);
   if (g.residual) {
-    typename Vec<E>::v8 r = load8<E>((const E *)g.residual + m * g.ldr + n, g.whole, left);
+    typename Vec<E>::v8 r = load8<E>((const E *)g.residual + m * g.ldr + n, left);
     for (int e = 0; e < 8; e++) v[e] += (float)r[e];
   }
   for (int e = 0; e < 8; e++) out[e] = (E)v[e];
-  store8<E>((E *)g.C + m * g.ldc + n, out, g.whole, left);
+  store8<E>((E *)g.C + m * g.ldc + n, out, left);
 }
 
 template <class E, int TM, int TN, int WM, int WN, bool AK, bool BK>
@@ -278,7 +265,7 @@ struct ActGrad {
   int64_t ld_dy, ld_z, ld_dz, T, N;
   float *sums; /* [runs][N] or null */
   int64_t rows; /* of a run */
-  int act, whole;
+  int act;
 };
 
 template <class E> __global__ __launch_bounds__(256) void k_act_grad(ActGrad g) {
@@ -289,16 +276,16 @@ template <class E> __global__ __launch_bounds__(256) void k_act_grad(ActGrad g) 
   if (left > 0)
 #pragma unroll 4
     for (int64_t t = (int64_t)blockIdx.y * g.rows + threadIdx.x / 64; t < t1; t += 4) {
-      typename Vec<E>::v8 d = load8<E>((const E *)g.dy + t * g.ld_dy + n, g.whole, left), out;
+      typename Vec<E>::v8 d = load8<E>((const E *)g.dy + t * g.ld_dy + n, left), out;
       if (g.dz) {
         typename Vec<E>::v8 z = d;
-        if (g.act != OOB_ACT_NONE) z = load8<E>((const E *)g.z + t * g.ld_z + n, g.whole, left);
+        if (g.act != OOB_ACT_NONE) z = load8<E>((const E *)g.z + t * g.ld_z + n, left);
         for (int e = 0; e < 8; e++) {
           float v = (float)d[e] * slope((float)z[e], g.act);
           out[e] = (E)v;
           sum[e] += v; /* before the rounding: the bias's gradient does not see it */
         }
-        store8<E>((E *)g.dz + t * g.ld_dz + n, out, true, left); /* past N: zeros */
+        store8<E>((E *)g.dz + t * g.ld_dz + n, out, 8); /* past N: zeros */
       } else {
         for (int e = 0; e < 8; e++) sum[e] += (float)d[e];
       }
@@ -326,24 +313,8 @@ template <class E> __global__ __launch_bounds__(256) void k_sum_rows(const float
 /* ---- host ------------------------------------------------------------------------------------------------------------------ */
 struct Operand { const void *p; int64_t ld, rows, cols; }; /* stored rows x cols, ld elements apart */
 
-static inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
-static inline size_t up_bytes(size_t x) { return (x + 255) / 256 * 256; }
-
-static inline bool aligned16(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
-
 /* What the loads to LDS can take: 16-byte pieces of rows that end with the row, offsets within a tile below 2^31. */
-static bool loadable(const Operand &o) { return o.cols % 8 == 0 && aligned16(o.p, o.ld) && o.ld < (1 << 21); }
-
-/* Memory handed out in order; sizes alone when there is none. */
-struct Arena {
-  char *base;
-  size_t used;
-  void *take(size_t bytes) {
-    void *p = base ? base + used : nullptr;
-    used += up_bytes(bytes);
-    return p;
-  }
-};
+static bool loadable(const Operand &o) { return o.cols % 8 == 0 && multiple(o.p, 16) && o.ld % 8 == 0 && o.ld < (1 << 21); }
 
 struct Shape { int tile, splits; };
 
@@ -361,7 +332,7 @@ static Shape choose(int64_t M, int64_t N, int64_t K) {
 }
 
 static size_t product_workspace(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K) {
-  Arena w{nullptr, 0};
+  Arena w{nullptr, 0, 0};
   if (!loadable(a)) w.take((size_t)a.rows * up(a.cols, 8) * 2);
   if (!loadable(b)) w.take((size_t)b.rows * up(b.cols, 8) * 2);
   Shape s = choose(M, N, K);
@@ -374,7 +345,7 @@ static Operand pack(const Operand &o, Arena &w, hipStream_t st) {
   int64_t ld = up(o.cols, 8);
   void *to = w.take((size_t)o.rows * ld * 2);
   int64_t n = o.rows * (ld / 8);
-  if (n) k_pack<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(Packed{(const uint16_t *)o.p, (uint16_t *)to, o.rows, o.cols, o.ld, ld});
+  if (n && w.ok()) k_pack<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(Packed{(const uint16_t *)o.p, (uint16_t *)to, o.rows, o.cols, o.ld, ld});
   return {to, ld, o.rows, ld};
 }
 
@@ -386,20 +357,22 @@ template <class E, bool AK, bool BK> static void launch(const Product &g, int ti
   if (g.splits > 1) k_join<E><<<(unsigned)((g.M * ((g.N + 7) / 8) + 255) / 256), 256, 0, st>>>(g);
 }
 
-/* The product with its operands as they are stored: ak (bk) says that k is contiguous. */
-template <class E> static void product(Operand a, bool ak, Operand b, bool bk, Product g, Arena &w, hipStream_t st) {
-  if (g.M == 0 || g.N == 0) return;
+/* The product with its operands as they are stored: ak (bk) says that k is contiguous.  The arena comes by value: what one product
+ * takes is free again for the next on the stream, as the workspace's size has it. */
+template <class E> static int product(Operand a, bool ak, Operand b, bool bk, Product g, Arena w, hipStream_t st) {
+  if (g.M == 0 || g.N == 0) return OOB_OK;
   Shape s = choose(g.M, g.N, g.K);
   a = pack(a, w, st);
   b = pack(b, w, st);
   g.A = a.p, g.lda = a.ld, g.B = b.p, g.ldb = b.ld;
   g.splits = s.splits;
   g.partial = s.splits > 1 ? (float *)w.take((size_t)s.splits * g.M * g.N * 4) : nullptr;
+  if (!w.ok()) return OOB_ECAPACITY;
   g.tiles_m = (int)((g.M + s.tile - 1) / s.tile), g.tiles_n = (int)((g.N + s.tile - 1) / s.tile);
-  g.whole = g.N % 8 == 0 && aligned16(g.C, g.ldc) && (!g.Z || aligned16(g.Z, g.ldz)) && (!g.residual || aligned16(g.residual, g.ldr));
   if (ak && bk) launch<E, true, true>(g, s.tile, st);
   else if (ak) launch<E, true, false>(g, s.tile, st);
   else launch<E, false, false>(g, s.tile, st);
+  return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
 }
 
 static bool sizes_ok(int dtype, int act, int64_t T, int64_t N, int64_t K) {
@@ -420,12 +393,12 @@ static size_t linear_bytes(const oob_linear *p) {
   return product_workspace({p->x, p->x_stride, p->T, p->K}, {p->w, p->w_stride, p->N, p->K}, p->T, p->N, p->K);
 }
 
-template <class E> static void linear(const oob_linear *p, Arena w, hipStream_t st) {
+template <class E> static int linear(const oob_linear *p, Arena w, hipStream_t st) {
   Product g{};
   g.M = p->T, g.N = p->N, g.K = p->K;
   g.bias = p->bias, g.residual = p->residual, g.ldr = p->residual_stride;
   g.C = p->y, g.ldc = p->y_stride, g.Z = p->z, g.ldz = p->z_stride, g.act = p->act;
-  product<E>({p->x, p->x_stride, p->T, p->K}, true, {p->w, p->w_stride, p->N, p->K}, true, g, w, st);
+  return product<E>({p->x, p->x_stride, p->T, p->K}, true, {p->w, p->w_stride, p->N, p->K}, true, g, w, st);
 }
 
 /* dz in the workspace (rows of a multiple of 8, zeros behind) where there is an activation or the products cannot load dy as it is;
@@ -438,7 +411,7 @@ static Operand dz_of(const oob_linear_grad *p, Arena &w) {
 }
 
 static size_t grad_bytes(const oob_linear_grad *p) {
-  Arena w{nullptr, 0};
+  Arena w{nullptr, 0, 0};
   Operand dz = dz_of(p, w);
   if (p->db) w.take((size_t)runs_of(p->T, p->N) * p->N * 4);
   size_t dx = p->dx ? product_workspace(dz, {p->w, p->w_stride, p->N, p->K}, p->T, p->K, p->N) : 0;
@@ -446,9 +419,10 @@ static size_t grad_bytes(const oob_linear_grad *p) {
   return w.used + (dx > dw ? dx : dw);
 }
 
-template <class E> static void linear_grad(const oob_linear_grad *p, Arena w, hipStream_t st) {
+template <class E> static int linear_grad(const oob_linear_grad *p, Arena w, hipStream_t st) {
   Operand dz = dz_of(p, w);
   float *sums = p->db ? (float *)w.take((size_t)runs_of(p->T, p->N) * p->N * 4) : nullptr;
+  if (!w.ok()) return OOB_ECAPACITY;
   bool makes = makes_dz(p);
   if (makes || sums) {
     ActGrad a{};
@@ -457,23 +431,24 @@ template <class E> static void linear_grad(const oob_linear_grad *p, Arena w, hi
     a.T = p->T, a.N = p->N, a.sums = sums, a.act = p->act;
     int64_t runs = runs_of(p->T, p->N);
     a.rows = (p->T + runs - 1) / runs;
-    a.whole = p->N % 8 == 0 && aligned16(p->dy, p->dy_stride) && (p->act == OOB_ACT_NONE || aligned16(p->z, p->z_stride));
     k_act_grad<E><<<dim3((unsigned)((p->N + 511) / 512), (unsigned)runs), 256, 0, st>>>(a);
     if (sums) k_sum_rows<E><<<(unsigned)((p->N + 63) / 64), 256, 0, st>>>(sums, runs, p->N, (E *)p->db);
   }
-  if (p->dx) {
+  int rc = hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
+  if (rc == OOB_OK && p->dx) {
     Product g{};
     g.M = p->T, g.N = p->K, g.K = p->N, g.C = p->dx, g.ldc = p->dx_stride;
-    product<E>(dz, true, {p->w, p->w_stride, p->N, p->K}, false, g, w, st);
+    rc = product<E>(dz, true, {p->w, p->w_stride, p->N, p->K}, false, g, w, st);
   }
-  if (p->dw) {
+  if (rc == OOB_OK && p->dw) {
     Product g{};
     g.M = p->N, g.N = p->K, g.K = p->T, g.C = p->dw, g.ldc = p->dw_stride;
-    product<E>(dz, false, {p->x, p->x_stride, p->T, p->K}, false, g, w, st);
+    rc = product<E>(dz, false, {p->x, p->x_stride, p->T, p->K}, false, g, w, st);
   }
+  return rc;
 }
 
-static bool even(const void *p) { return ((uintptr_t)p & 1) == 0; }
+static bool even(const void *p) { return multiple(p, 2); }
 
 }  // namespace layer
 
@@ -489,13 +464,11 @@ extern "C" int oob_layer_linear(const oob_linear *p, void *workspace, size_t byt
   if (!p->x || !p->w || !p->y || p->x_stride < p->K || p->w_stride < p->K || p->y_stride < p->N) return OOB_EINVAL;
   if ((p->residual && p->residual_stride < p->N) || (p->z && p->z_stride < p->N)) return OOB_EINVAL;
   if (!even(p->x) || !even(p->w) || !even(p->y) || !even(p->bias) || !even(p->residual) || !even(p->z)) return OOB_EINVAL;
-  if ((uintptr_t)workspace & 255) return OOB_EINVAL;
+  if (!multiple(workspace, 256)) return OOB_EINVAL;
   size_t need = linear_bytes(p);
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
-  Arena w{(char *)workspace, 0};
-  if (p->dtype == OOB_BF16) linear<bf16>(p, w, (hipStream_t)stream);
-  else linear<fp16>(p, w, (hipStream_t)stream);
-  return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
+  Arena w{(char *)workspace, bytes, 0};
+  return p->dtype == OOB_BF16 ? linear<bf16>(p, w, (hipStream_t)stream) : linear<fp16>(p, w, (hipStream_t)stream);
 }
 
 extern "C" size_t oob_layer_linear_backward_workspace_size(const oob_linear_grad *p) {
@@ -509,11 +482,9 @@ extern "C" int oob_layer_linear_backward(const oob_linear_grad *p, void *workspa
   if (p->T && p->dx && (!p->w || p->w_stride < p->K || p->dx_stride < p->K)) return OOB_EINVAL;
   if (p->dw && ((p->T && (!p->x || p->x_stride < p->K)) || p->dw_stride < p->K)) return OOB_EINVAL;
   if (!even(p->dy) || !even(p->x) || !even(p->w) || !even(p->z) || !even(p->dx) || !even(p->dw) || !even(p->db)) return OOB_EINVAL;
-  if ((uintptr_t)workspace & 255) return OOB_EINVAL;
+  if (!multiple(workspace, 256)) return OOB_EINVAL;
   size_t need = grad_bytes(p);
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
-  Arena w{(char *)workspace, 0};
-  if (p->dtype == OOB_BF16) linear_grad<bf16>(p, w, (hipStream_t)stream);
-  else linear_grad<fp16>(p, w, (hipStream_t)stream);
-  return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
+  Arena w{(char *)workspace, bytes, 0};
+  return p->dtype == OOB_BF16 ? linear_grad<bf16>(p, w, (hipStream_t)stream) : linear_grad<fp16>(p, w, (hipStream_t)stream);
 }

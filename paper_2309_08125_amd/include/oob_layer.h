@@ -60,6 +60,55 @@ typedef struct oob_linear_grad {
 size_t oob_layer_linear_backward_workspace_size(const oob_linear_grad *p);
 int oob_layer_linear_backward(const oob_linear_grad *p, void *workspace, size_t bytes, void *stream);
 
+/* ---- norms before and after a block, its gate, residual scale and dropout ---------------------
+ * A residual stream x [T][C] and a block's output z [T][C]:
+ *   u = keep / (1 - p) * post(z) * post_weight + post_bias;  xp = alpha x + gate u;
+ *   h = pre(xp) * weight + bias
+ * with post NONE (u = keep / (1 - p) z), LAYER or RMS and pre LAYER or RMS: LAYER(v) = (v - mean) /
+ * sqrt(variance + eps), RMS(v) = v / sqrt(mean of squares + eps).  weight, bias, post_weight, post_bias
+ * [C]: each may be NULL (1, 0).  (keep multiplies post_bias too.)  gate [gates][C], T a
+ * multiple of gates, above 0: gate g is that of rows g T / gates .. (g + 1) T / gates - 1; gates = 0: none.  keep: as in
+ * oob_layer_dropout, element t C + c.  z NULL: xp is x itself and not written (post NONE, no gate, p 0,
+ * alpha 1).  h is formed from xp before its rounding.
+ * Types: OOB_BF16, OOB_FP16, OOB_FP32.  xp may be x (with stride C). */
+enum { OOB_NORM_NONE = 0, OOB_NORM_LAYER = 1, OOB_NORM_RMS = 2 };
+#define OOB_NORM_MAX_C 16384
+
+typedef struct oob_norm {
+  int dtype, pre, post;
+  float eps, alpha, p;      /* eps >= 0; 0 <= p, rounded to a multiple of 2^-16 below 1 */
+  int64_t T, C, gates;      /* T >= 0, 1 <= C <= OOB_NORM_MAX_C */
+  uint64_t seed, offset;    /* of the dropout */
+  const void *x, *z, *weight, *bias, *post_weight, *post_bias, *gate;
+  int64_t x_stride, z_stride;
+  void *xp, *h;             /* [T][C] out */
+  float *saved;             /* [4][T] out: mean and 1 / deviation of pre, of post; or NULL */
+} oob_norm;
+
+int oob_layer_norm(const oob_norm *p, void *stream);
+
+/* From the gradients of xp (dxp, NULL: zero) and h: those of x, z, and of the weights that are not
+ * NULL.  Of p: x is xp (the forward call's result, x_stride its stride), saved and everything else as
+ * in the forward call, xp and h are not used. */
+typedef struct oob_norm_grad {
+  const void *dxp, *dh;
+  int64_t dxp_stride, dh_stride;
+  void *dx, *dz;                                        /* [T][C] out; dz where there is a z */
+  void *dweight, *dbias, *dpost_weight, *dpost_bias;    /* [C] out, each may be NULL */
+  void *dgate;                                          /* [gates][C] out where there are gates */
+} oob_norm_grad;
+
+size_t oob_layer_norm_backward_workspace_size(const oob_norm *p);
+int oob_layer_norm_backward(const oob_norm *p, const oob_norm_grad *g, void *workspace, size_t bytes, void *stream);
+
+/* ---- dropout -----------------------------------------------------------------------------------
+ * y[i] = keep_i x[i] / (1 - p), n elements; y may be x.  keep_i: bits 16 (m % 4) .. + 15 of word m / 4,
+ * m = offset + i, are not below round(65536 p), and 1 - p is that of the rounded p.  Word k is output
+ * k of a SplitMix64 generator whose state starts at output function(seed).  The mask is never stored:
+ * the backward pass is the same call on dy. */
+int oob_layer_dropout(int dtype, const void *x, void *y, int64_t n, float p, uint64_t seed, uint64_t offset,
+                      void *stream);
+
 #ifdef __cplusplus
 }
 #endif

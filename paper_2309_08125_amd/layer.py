@@ -5,6 +5,7 @@ enqueued on torch's current stream of the tensors' device; nothing waits.  There
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 
 from . import binding
@@ -12,7 +13,10 @@ from . import binding
 OOB_BF16, OOB_FP16, OOB_FP32 = 0, 1, 2
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 LAYER_SYMBOLS = ["oob_layer_linear", "oob_layer_linear_workspace_size", "oob_layer_linear_backward",
-                 "oob_layer_linear_backward_workspace_size"]
+                 "oob_layer_linear_backward_workspace_size", "oob_layer_norm", "oob_layer_norm_backward",
+                 "oob_layer_norm_backward_workspace_size", "oob_layer_dropout"]
+MASK64 = (1 << 64) - 1
+NORMS = {"none": 0, "layer": 1, "rms": 2}
 
 
 class oob_linear(C.Structure):
@@ -27,6 +31,18 @@ class oob_linear_grad(C.Structure):
                [(n + "_stride", C.c_int64) for n in ("dy", "x", "w", "z", "dx", "dw")]
 
 
+class oob_norm(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("dtype", "pre", "post")] + [(n, C.c_float) for n in ("eps", "alpha", "p")] + \
+               [(n, C.c_int64) for n in ("T", "C", "gates")] + [(n, C.c_uint64) for n in ("seed", "offset")] + \
+               [(n, C.c_void_p) for n in ("x", "z", "weight", "bias", "post_weight", "post_bias", "gate")] + \
+               [(n, C.c_int64) for n in ("x_stride", "z_stride")] + [(n, C.c_void_p) for n in ("xp", "h", "saved")]
+
+
+class oob_norm_grad(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("dxp", "dh")] + [(n, C.c_int64) for n in ("dxp_stride", "dh_stride")] + \
+               [(n, C.c_void_p) for n in ("dx", "dz", "dweight", "dbias", "dpost_weight", "dpost_bias", "dgate")]
+
+
 _lib = None
 
 
@@ -38,6 +54,13 @@ def _load():
             size, call = getattr(L, f"oob_layer_{name}_workspace_size"), getattr(L, f"oob_layer_{name}")
             size.argtypes, size.restype = [C.POINTER(struct)], C.c_size_t
             call.argtypes, call.restype = [C.POINTER(struct), C.c_void_p, C.c_size_t, C.c_void_p], C.c_int
+        L.oob_layer_norm.argtypes, L.oob_layer_norm.restype = [C.POINTER(oob_norm), C.c_void_p], C.c_int
+        L.oob_layer_norm_backward_workspace_size.argtypes = [C.POINTER(oob_norm)]
+        L.oob_layer_norm_backward_workspace_size.restype = C.c_size_t
+        L.oob_layer_norm_backward.argtypes = [C.POINTER(oob_norm), C.POINTER(oob_norm_grad), C.c_void_p, C.c_size_t, C.c_void_p]
+        L.oob_layer_norm_backward.restype = C.c_int
+        L.oob_layer_dropout.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C.c_int64, C.c_float, C.c_uint64, C.c_uint64, C.c_void_p]
+        L.oob_layer_dropout.restype = C.c_int
         _lib = L
     return _lib
 
@@ -86,18 +109,34 @@ def _vector(t, n, like, name):
     return t.data_ptr()
 
 
-def _run(name, args, device):
-    """Asks for the workspace of a call and enqueues it on the current stream of `device`."""
+def _on(device):
+    """Makes `device` the current one where it is not (a context manager), and nothing where it is."""
     import torch
 
-    lib = _load()
-    if device.index is not None and device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return _run(name, args, torch.device("cuda"))
-    ref = C.byref(args)
-    nbytes = getattr(lib, f"oob_layer_{name}_workspace_size")(ref)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device).data_ptr() if nbytes else None
-    binding.check(getattr(lib, f"oob_layer_{name}")(ref, ws, nbytes, torch.cuda.current_stream().cuda_stream), f"oob_layer_{name}")
+    if device.index is None or device.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
+def _stream():
+    import torch
+
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _workspace(nbytes, device):
+    import torch
+
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _run(name, args, device):
+    """Asks for the workspace of a call and enqueues it on the current stream of `device`."""
+    lib, ref = _load(), C.byref(args)
+    with _on(device):
+        nbytes = getattr(lib, f"oob_layer_{name}_workspace_size")(ref)
+        ws = _workspace(nbytes, device)  # held until the call is enqueued; torch gives it to later work of this stream only
+        binding.check(getattr(lib, f"oob_layer_{name}")(ref, ws.data_ptr(), nbytes, _stream()), f"oob_layer_{name}")
 
 
 def _act(act):
@@ -158,3 +197,95 @@ def linear_backward(dy, x, w, z=None, act="none", need=("x", "w", "b")):
                            _stride(dy2), _stride(x2), _stride(w2), 0 if z2 is None else _stride(z2), K, K)
     _run("linear_backward", args, x.device)
     return dx, dw, db
+
+
+def _norm_args(x, z, xp, h, saved, weight, bias, pre, post, post_weight, post_bias, gate, alpha, eps, p, seed, offset):
+    _need(x.is_cuda and x.dim() >= 1, "x has to be on the GPU")
+    width = x.shape[-1]
+    dtype = _dtype(x, wide=True)
+    _need(pre in ("layer", "rms") and post in NORMS, "pre: layer or rms, post: none, layer or rms")
+    _need(0 <= p < 1 and p * 65536 + 0.5 < 65536, "p: at least 0 and below 1")
+    x2 = _rows(x, width, x, "x")
+    T = x2.shape[0]
+    z2 = None
+    if z is not None:
+        _need(z.shape == x.shape, "z and x: different shapes")
+        z2 = _rows(z, width, x, "z")
+    else:
+        _need(post == "none" and gate is None and p == 0 and alpha == 1, "without z there is nothing to norm, gate, drop or scale")
+    _need(post != "none" or (post_weight is None and post_bias is None), "post_weight and post_bias belong to a norm behind the block")
+    gates, g = 0, None
+    if gate is not None:
+        _need(gate.shape[-1] == width and gate.numel() > 0, "gate: the last axis is not x's")
+        gates = gate.numel() // width
+        _need(T > 0 and T % gates == 0, f"gate: {T} rows do not divide among {gates}")
+        _need(gate.dtype == x.dtype and gate.device == x.device and gate.is_contiguous(), "gate: contiguous, of x's type and device")
+        g = gate.data_ptr()
+    vec = lambda t, name: None if t is None else _vector(t, width, x, name)  # noqa: E731
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    return oob_norm(dtype, NORMS[pre], NORMS[post], eps, alpha, p, T, width, gates, seed & MASK64, offset & MASK64, x2.data_ptr(), ptr(z2),
+                    vec(weight, "weight"), vec(bias, "bias"), vec(post_weight, "post_weight"), vec(post_bias, "post_bias"), g,
+                    _stride(x2), 0 if z2 is None else _stride(z2), ptr(xp), ptr(h), ptr(saved))
+
+
+def residual_norm(x, z=None, weight=None, bias=None, pre="layer", post="none", post_weight=None, post_bias=None, gate=None,
+                  alpha=1.0, eps=1e-5, p=0.0, seed=0, offset=0):
+    """The norms around a block: xp = alpha x + gate * dropout(post(z)), h = pre(xp); (xp, h, saved).
+
+    x: the residual stream [..., C]; z: the block's output, or None (xp is x: the first norm of a model); pre: "layer" or "rms" with
+    weight and bias [C]; post: "none" or a norm with post_weight and post_bias; gate [C] or [G, C]: one for each G-th of the rows;
+    dropout: dropout(post(z), p, seed, offset), element by element of the rows.  bfloat16, float16 or float32.  saved: statistics
+    that the backward pass wants."""
+    import torch
+
+    new = lambda: torch.empty(x.shape, dtype=x.dtype, device=x.device)  # noqa: E731
+    h, xp = new(), x if z is None else new()
+    width = x.shape[-1] if x.dim() else 0
+    saved = torch.empty((2 if post == "none" else 4, x.numel() // max(width, 1)), dtype=torch.float32, device=x.device)
+    args = _norm_args(x, z, None if z is None else xp, h, saved, weight, bias, pre, post, post_weight, post_bias, gate, alpha, eps, p, seed, offset)
+    with _on(x.device):
+        binding.check(_load().oob_layer_norm(C.byref(args), _stream()), "oob_layer_norm")
+    return xp, h, saved
+
+
+def residual_norm_backward(dxp, dh, xp, z, saved, weight=None, bias=None, pre="layer", post="none", post_weight=None, post_bias=None,
+                           gate=None, alpha=1.0, eps=1e-5, p=0.0, seed=0, offset=0):
+    """Gradients of residual_norm from those of its results (dxp None: zero), as a dict: "x", "z" and the name of every weight that is
+    given (None for the others).  Everything behind `saved` as in the forward call."""
+    import torch
+
+    args = _norm_args(xp, z, None, None, saved, weight, bias, pre, post, post_weight, post_bias, gate, alpha, eps, p, seed, offset)
+    T, width = args.T, args.C
+    _need(saved.dtype == torch.float32 and saved.device == xp.device and saved.is_contiguous() and
+          tuple(saved.shape) == (2 if post == "none" else 4, T), "saved: not that of such a call")
+    _need(dh.shape == xp.shape and (dxp is None or dxp.shape == xp.shape), "dxp, dh and xp: different shapes")
+    dh2 = _rows(dh, width, xp, "dh")
+    dxp2 = None if dxp is None else _rows(dxp, width, xp, "dxp")
+    new = lambda t: None if t is None else torch.empty(t.shape, dtype=xp.dtype, device=xp.device)  # noqa: E731
+    out = {"x": new(xp), "z": new(z), "weight": new(weight), "bias": new(bias), "post_weight": new(post_weight),
+           "post_bias": new(post_bias), "gate": new(gate)}
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    grad = oob_norm_grad(ptr(dxp2), dh2.data_ptr(), 0 if dxp2 is None else _stride(dxp2), _stride(dh2), *(ptr(t) for t in out.values()))
+    lib, ref = _load(), C.byref(args)
+    with _on(xp.device):
+        nbytes = lib.oob_layer_norm_backward_workspace_size(ref)
+        ws = _workspace(nbytes, xp.device)
+        binding.check(lib.oob_layer_norm_backward(ref, C.byref(grad), ws.data_ptr(), nbytes, _stream()), "oob_layer_norm_backward")
+    return out
+
+
+def dropout(x, p, seed, offset=0, out=None):
+    """keep / (1 - p) * x for a contiguous tensor of any shape (bfloat16, float16, float32); out may be x.  The mask comes from
+    (seed, offset + element) alone and is never stored: the backward pass is the same call on the gradient."""
+    import torch
+
+    _need(x.is_cuda and x.is_contiguous(), "x has to be contiguous and on the GPU")
+    dtype = _dtype(x, wide=True)
+    _need(0 <= p < 1 and p * 65536 + 0.5 < 65536, "p: at least 0 and below 1")
+    if out is None:
+        out = torch.empty_like(x)
+    _need(out.shape == x.shape and out.dtype == x.dtype and out.device == x.device and out.is_contiguous(), "out: not like x")
+    with _on(x.device):
+        binding.check(_load().oob_layer_dropout(dtype, x.data_ptr(), out.data_ptr(), x.numel(), p, seed & MASK64, offset & MASK64, _stream()),
+                      "oob_layer_dropout")
+    return out
