@@ -14,5 +14,6 @@ from .binding import (  # noqa: F401
     OOB_INST_STATIC_BYTES, oob_inst_enumerate_static,
 )
 from .layer import (  # noqa: F401
-    ACTIVATIONS, LAYER_SYMBOLS, dropout, linear, linear_backward, residual_norm, residual_norm_backward,
+    ACTIVATIONS, LAYER_SYMBOLS, attention, attention_backward, document_ranges, dropout, linear, linear_backward, prefix_ranges,
+    residual_norm, residual_norm_backward,
 )

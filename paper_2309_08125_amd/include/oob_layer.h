@@ -101,6 +101,46 @@ typedef struct oob_norm_grad {
 size_t oob_layer_norm_backward_workspace_size(const oob_norm *p);
 int oob_layer_norm_backward(const oob_norm *p, const oob_norm_grad *g, void *workspace, size_t bytes, void *stream);
 
+/* ---- attention ---------------------------------------------------------------------------------
+ * B sequences of Sq queries and Sk keys, H heads of D values for queries and G for keys and values (head h
+ * uses h / (H / G)).  Query i sees the keys j with begin_i <= j < end_i, key_begin (or 0) and key_end (or
+ * Sk) [B][Sq]; causal: only those with j <= i + Sk - Sq as well.  Document, prefix and window masks are
+ * such ranges.
+ *   s_ij = scale q_i . k_j;  cap > 0: s_ij = cap tanh(s_ij / cap);  slopes [H] (or NULL): s_ij -= slope_h
+ *   |i + Sk - Sq - j|;  o_i = sum_j softmax_j(s_ij) v_j;  lse_i = log sum_j e^s_ij
+ * A query that sees no key has o = 0, lse = -inf and no part in any gradient, whatever it holds.  Keys that no
+ * query of a tile of 128 sees are not read; others have to be finite, also for queries that do not see them.
+ * q, o [B][Sq][H][D], k, v [B][Sk][G][D]: strides of a sequence, a row and a head, the last axis
+ * contiguous. */
+#define OOB_ATTENTION_MAX_D 128
+
+typedef struct oob_attention {
+  int dtype;                    /* OOB_BF16 or OOB_FP16 */
+  int B, Sq, Sk, H, G, D;       /* B, Sq, Sk >= 0 (below 2^29); H a multiple of G >= 1; 1 <= D <= 128 */
+  int causal;
+  float scale, cap;             /* scale > 0; cap 0: none */
+  const void *q, *k, *v;
+  const int32_t *key_begin, *key_end;
+  const float *slopes;
+  void *o;
+  float *lse;                   /* [B][H][Sq] out, or NULL; read by the backward pass */
+  int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];
+} oob_attention;
+
+size_t oob_layer_attention_workspace_size(const oob_attention *p);
+int oob_layer_attention(const oob_attention *p, void *workspace, size_t bytes, void *stream);
+
+/* dq, dk, dv from dout, the gradient of o.  Of p: everything as in the forward call, o and lse its results. */
+typedef struct oob_attention_grad {
+  const void *dout;
+  void *dq, *dk, *dv;
+  int64_t dout_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];
+} oob_attention_grad;
+
+size_t oob_layer_attention_backward_workspace_size(const oob_attention *p, const oob_attention_grad *g);
+int oob_layer_attention_backward(const oob_attention *p, const oob_attention_grad *g, void *workspace, size_t bytes,
+                                 void *stream);
+
 /* ---- dropout -----------------------------------------------------------------------------------
  * y[i] = keep_i x[i] / (1 - p), n elements; y may be x.  keep_i: bits 16 (m % 4) .. + 15 of word m / 4,
  * m = offset + i, are not below round(65536 p), and 1 - p is that of the rounded p.  Word k is output

@@ -14,7 +14,8 @@ OOB_BF16, OOB_FP16, OOB_FP32 = 0, 1, 2
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 LAYER_SYMBOLS = ["oob_layer_linear", "oob_layer_linear_workspace_size", "oob_layer_linear_backward",
                  "oob_layer_linear_backward_workspace_size", "oob_layer_norm", "oob_layer_norm_backward",
-                 "oob_layer_norm_backward_workspace_size", "oob_layer_dropout"]
+                 "oob_layer_norm_backward_workspace_size", "oob_layer_dropout", "oob_layer_attention",
+                 "oob_layer_attention_workspace_size", "oob_layer_attention_backward", "oob_layer_attention_backward_workspace_size"]
 MASK64 = (1 << 64) - 1
 NORMS = {"none": 0, "layer": 1, "rms": 2}
 
@@ -43,6 +44,16 @@ class oob_norm_grad(C.Structure):
                [(n, C.c_void_p) for n in ("dx", "dz", "dweight", "dbias", "dpost_weight", "dpost_bias", "dgate")]
 
 
+class oob_attention(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("dtype", "B", "Sq", "Sk", "H", "G", "D", "causal")] + [(n, C.c_float) for n in ("scale", "cap")] + \
+               [(n, C.c_void_p) for n in ("q", "k", "v", "key_begin", "key_end", "slopes", "o", "lse")] + \
+               [(n + "_stride", C.c_int64 * 3) for n in "qkvo"]
+
+
+class oob_attention_grad(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("dout", "dq", "dk", "dv")] + [(n + "_stride", C.c_int64 * 3) for n in ("dout", "dq", "dk", "dv")]
+
+
 _lib = None
 
 
@@ -54,6 +65,11 @@ def _load():
             size, call = getattr(L, f"oob_layer_{name}_workspace_size"), getattr(L, f"oob_layer_{name}")
             size.argtypes, size.restype = [C.POINTER(struct)], C.c_size_t
             call.argtypes, call.restype = [C.POINTER(struct), C.c_void_p, C.c_size_t, C.c_void_p], C.c_int
+        one, two = [C.POINTER(oob_attention)], [C.POINTER(oob_attention), C.POINTER(oob_attention_grad)]
+        for call, args in ((L.oob_layer_attention, one), (L.oob_layer_attention_backward, two)):
+            call.argtypes, call.restype = args + [C.c_void_p, C.c_size_t, C.c_void_p], C.c_int
+        for call, args in ((L.oob_layer_attention_workspace_size, one), (L.oob_layer_attention_backward_workspace_size, two)):
+            call.argtypes, call.restype = args, C.c_size_t
         L.oob_layer_norm.argtypes, L.oob_layer_norm.restype = [C.POINTER(oob_norm), C.c_void_p], C.c_int
         L.oob_layer_norm_backward_workspace_size.argtypes = [C.POINTER(oob_norm)]
         L.oob_layer_norm_backward_workspace_size.restype = C.c_size_t
@@ -289,3 +305,101 @@ def dropout(x, p, seed, offset=0, out=None):
         binding.check(_load().oob_layer_dropout(dtype, x.data_ptr(), out.data_ptr(), x.numel(), p, seed & MASK64, offset & MASK64, _stream()),
                       "oob_layer_dropout")
     return out
+
+
+def _heads(t, name, like, B, S, N, D):
+    _need(t.dim() == 4 and tuple(t.shape) == (B, S, N, D), f"{name}: [{B}, {S}, {N}, {D}] is wanted, not {list(t.shape)}")
+    _need(t.dtype == like.dtype and t.device == like.device, f"{name}: type and device have to be {like.dtype}, {like.device}")
+    _need(D == 1 or t.stride(3) == 1, f"{name}: the last axis has to be contiguous")
+    return t.data_ptr(), (C.c_int64 * 3)(*t.stride()[:3])
+
+
+def _attention_args(q, k, v, o, lse, scale, causal, key_begin, key_end, slopes, cap):
+    import torch
+
+    _need(q.is_cuda and q.dim() == 4 and k.dim() == 4, "q and k have to be on the GPU: [batch, length, heads, width]")
+    B, Sq, H, D = q.shape
+    Sk, G = k.shape[1], k.shape[2]
+    _need(1 <= D <= 128, "heads of 1 to 128 values are supported")
+    _need(G >= 1 and H >= 1 and H % G == 0, f"{H} heads do not divide among {G}")
+    dtype = _dtype(q)
+    scale = D ** -0.5 if scale is None else scale
+    _need(0 < scale < float("inf") and 0 <= cap < float("inf"), "scale has to be above 0, cap 0 (none) or above")
+    (pq, sq), (pk, sk), (pv, sv) = _heads(q, "q", q, B, Sq, H, D), _heads(k, "k", q, B, Sk, G, D), _heads(v, "v", q, B, Sk, G, D)
+    po, so = _heads(o, "o", q, B, Sq, H, D)
+    ranges = []
+    for t, name in ((key_begin, "key_begin"), (key_end, "key_end")):
+        _need(t is None or (t.dtype == torch.int32 and t.device == q.device and tuple(t.shape) == (B, Sq) and t.is_contiguous()),
+              f"{name}: a contiguous int32 [{B}, {Sq}] on {q.device} is wanted")
+        ranges.append(None if t is None else t.data_ptr())
+    _need(slopes is None or (slopes.dtype == torch.float32 and slopes.device == q.device and tuple(slopes.shape) == (H,) and slopes.is_contiguous()),
+          f"slopes: {H} contiguous float32 values on {q.device} are wanted")
+    return oob_attention(dtype, B, Sq, Sk, H, G, D, bool(causal), scale, cap, pq, pk, pv, *ranges,
+                         None if slopes is None else slopes.data_ptr(), po, lse.data_ptr(), sq, sk, sv, so)
+
+
+def attention(q, k, v, scale=None, causal=False, key_begin=None, key_end=None, slopes=None, cap=0.0):
+    """(o, lse) with o_i = sum_j softmax_j(s_ij) v_j, s_ij = cap tanh(scale q_i.k_j / cap) - slope |i + Sk - Sq - j| over the keys
+    key_begin_i <= j < key_end_i (causal: and j <= i + Sk - Sq).
+
+    q [B, Sq, H, D], k, v [B, Sk, G, D] of any strides with a contiguous last axis, H a multiple of G; bfloat16 or float16, D up to
+    128.  scale: D ** -0.5 where None.  key_begin, key_end: int32 [B, Sq] or None; document, prefix and window masks are such ranges
+    (document_ranges, prefix_ranges).  slopes: float32 [H] or None; cap 0: none.  A query that sees no key gets 0 and lse -inf.
+    lse [B, H, Sq] in float32 goes to attention_backward."""
+    import torch
+
+    _need(q.dim() == 4, "q: [batch, length, heads, width]")
+    B, Sq, H, D = q.shape
+    o = torch.empty((B, Sq, H, D), dtype=q.dtype, device=q.device)
+    lse = torch.empty((B, H, Sq), dtype=torch.float32, device=q.device)
+    _run("attention", _attention_args(q, k, v, o, lse, scale, causal, key_begin, key_end, slopes, cap), q.device)
+    return o, lse
+
+
+def attention_backward(do, q, k, v, o, lse, scale=None, causal=False, key_begin=None, key_end=None, slopes=None, cap=0.0, out=None):
+    """(dq, dk, dv) of attention from `do`, the gradient of o.  out: three tensors to write them to, of any strides with a contiguous
+    last axis (the parts of one tensor, say)."""
+    import torch
+
+    args = _attention_args(q, k, v, o, lse, scale, causal, key_begin, key_end, slopes, cap)
+    B, Sq, H, D = q.shape
+    Sk, G = k.shape[1], k.shape[2]
+    _need(tuple(lse.shape) == (B, H, Sq) and lse.dtype == torch.float32 and lse.device == q.device and lse.is_contiguous(),
+          "lse: not that of such a call")
+    if out is None:
+        out = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    parts = [_heads(do, "do", q, B, Sq, H, D), _heads(out[0], "dq", q, B, Sq, H, D), _heads(out[1], "dk", q, B, Sk, G, D),
+             _heads(out[2], "dv", q, B, Sk, G, D)]
+    grad = oob_attention_grad(*(p for p, _ in parts), *(s for _, s in parts))
+    lib, ref, gref = _load(), C.byref(args), C.byref(grad)
+    with _on(q.device):
+        nbytes = lib.oob_layer_attention_backward_workspace_size(ref, gref)
+        ws = _workspace(nbytes, q.device)
+        binding.check(lib.oob_layer_attention_backward(ref, gref, ws.data_ptr(), nbytes, _stream()), "oob_layer_attention_backward")
+    return tuple(out)
+
+
+def document_ranges(lengths, S, device="cuda"):
+    """(key_begin, key_end) of documents packed one behind the other into sequences of S tokens, causal within each: `lengths` has a
+    list of lengths per sequence.  Tokens behind the last document see nothing and are seen by none."""
+    import torch
+
+    begin, end = torch.zeros((len(lengths), S), dtype=torch.int32), torch.zeros((len(lengths), S), dtype=torch.int32)
+    for b, docs in enumerate(lengths):
+        _need(all(n >= 0 for n in docs) and sum(docs) <= S, f"sequence {b}: documents of {sum(docs)} tokens in {S}")
+        at = 0
+        for n in docs:
+            begin[b, at: at + n] = at
+            end[b, at: at + n] = torch.arange(at + 1, at + n + 1, dtype=torch.int32)
+            at += n
+    return begin.to(device), end.to(device)
+
+
+def prefix_ranges(lengths, S, device="cuda"):
+    """(key_begin, key_end) of sequences whose first lengths[b] tokens are seen by all and whose others are causal."""
+    import torch
+
+    prefix = torch.tensor([int(n) for n in lengths], dtype=torch.int32)[:, None]
+    _need(bool(((prefix >= 0) & (prefix <= S)).all()), "a prefix is longer than the sequence")
+    end = torch.maximum(torch.arange(1, S + 1, dtype=torch.int32)[None], prefix)
+    return torch.zeros_like(end).to(device), end.to(device)
