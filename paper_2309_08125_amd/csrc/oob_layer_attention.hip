@@ -17,7 +17,7 @@ struct Attention {
   float scale, cap;
   /* backward */
   Heads dout, dq, dk, dv;
-  const float *delta;  /* [B][H][Sq]: do . o */
+  const float *lse2, *delta; /* [B][H][Sq]: lse log2 e (0 where there is none), do . o */
   const int4 *ranges;  /* [B][tiles of 64 queries]: smallest begin, largest end, largest begin, smallest end */
 };
 
@@ -45,43 +45,64 @@ __device__ inline void key_range(const Attention &a, int b, int i, int &begin, i
   if (lo < hi) begin = lo, end = hi;
 }
 
-/* 64 rows of a head on their way to LDS. */
+/* 64 rows of a head on their way to LDS, 16 (DP 128) or 32 rows a load: rows that far apart have the same swizzle, so that a lane has one
+ * offset and the loads differ by a scalar. */
 template <int DP> struct Rows {
-  static constexpr int BYTES = KT * DP * 2, LOADS = BYTES / (WAVES * 64 * 16);
-  uint32_t off[LOADS];
-  int row[LOADS];
+  static constexpr int BYTES = KT * DP * 2, LOADS = BYTES / (WAVES * 64 * 16), STEP = KT / LOADS;
+  uint32_t off;
+  int row;
   __device__ void init(int64_t stride, int D) {
-    for (int i = 0; i < LOADS; i++) {
-      int p = (i * WAVES * 64 + threadIdx.x) * 16, r = p / (DP * 2), c = (p / 16 % (DP / 8)) ^ swizzle<DP>(r);
-      row[i] = r;
-      off[i] = c * 8 < D ? (uint32_t)(r * stride + c * 16) : OOB_LAYER_OUT;
-    }
+    int p = threadIdx.x * 16, c = (p / 16 % (DP / 8)) ^ swizzle<DP>(p / (DP * 2));
+    row = p / (DP * 2);
+    off = c * 8 < D ? (uint32_t)(row * stride + c * 16) : OOB_LAYER_OUT;
   }
   /* rows lo <= first + r < hi; zeros for the others */
   __device__ void load(const char *base, int64_t stride, lds_char *to, int first, int lo, int hi) {
+    load(base, stride, to, first, [&](int at) { return at >= lo && at < hi; });
+  }
+  template <class F> __device__ void load(const char *base, int64_t stride, lds_char *to, int first, F in) {
     __amdgpu_buffer_rsrc_t r = buffer(base + first * stride);
     int wave = uniform(threadIdx.x / 64);
 #pragma unroll
-    for (int i = 0; i < LOADS; i++) {
-      int at = first + row[i];
-      load_lds(r, to + (i * WAVES * 64 + wave * 64) * 16, at >= lo && at < hi ? off[i] : OOB_LAYER_OUT);
-    }
+    for (int i = 0; i < LOADS; i++)
+      load_lds(r, to + (i * WAVES * 64 + wave * 64) * 16, in(first + row + i * STEP) ? off : OOB_LAYER_OUT, (uint32_t)(i * STEP * stride));
   }
 };
 
-/* Fragments of a tile's 32 rows from r0 on.  Straight: row l % 32, columns 16 t + 8 (l / 32) .. + 7. */
-template <class E, int DP> __device__ inline typename Vec<E>::v8 straight(lds_char *tile, int r0, int t) {
-  int l = lane(), r = r0 + (l & 31);
-  return lds_read8<E>(tile + r * DP * 2 + ((2 * t + (l >> 5)) ^ swizzle<DP>(r)) * 16);
-}
-/* Transposed: column d0 + l % 32, rows r0 + 4 (l / 32) .. + 3 and r0 + 8 + 4 (l / 32) .. + 3: the rows whose values of a product a lane
- * holds in eight registers in a row, so that they are the other operand as they are. */
-template <class E, int DP> __device__ inline typename Vec<E>::v8 transposed(lds_char *tile, int r0, int d0) {
-  int l = lane(), r = r0 + 4 * (l >> 5) + ((l & 15) >> 2), c = d0 / 8 + ((l >> 4) & 1) * 2 + ((l >> 1) & 1);
-  lds_char *p = tile + r * DP * 2 + (c ^ swizzle<DP>(r)) * 16 + (l & 1) * 8;
-  lds_char *q = tile + (r + 8) * DP * 2 + (c ^ swizzle<DP>(r + 8)) * 16 + (l & 1) * 8;
-  return lds_read_tr<E>(p, q);
-}
+/* A lane's places in a tile: everything else about an address is a constant, so that reads need no arithmetic.
+ * Straight fragments: row r0 + l % 32, columns 16 t + 8 (l / 32) .. + 7.  Transposed: column d0 + l % 32, rows r0 + 4 (l / 32) .. + 3 and
+ * r0 + 8 + 4 (l / 32) .. + 3: the rows whose values of a product a lane holds in eight registers in a row, so that those are the other
+ * operand as they are.  (r0: a multiple of 32 and of 16; the swizzle of row r + 8 is that of row r with one bit flipped.) */
+template <class E, int DP> struct Places {
+  int s[DP / 16], t[DP / 32];
+  __device__ void init() {
+    int l = lane(), r = l & 31;
+    for (int i = 0; i < DP / 16; i++) s[i] = r * DP * 2 + ((2 * i + (l >> 5)) ^ swizzle<DP>(r)) * 16;
+    r = 4 * (l >> 5) + ((l & 15) >> 2);
+    for (int i = 0; i < DP / 32; i++) t[i] = r * DP * 2 + ((4 * i + ((l >> 4) & 1) * 2 + ((l >> 1) & 1)) ^ swizzle<DP>(r)) * 16 + (l & 1) * 8;
+  }
+  __device__ typename Vec<E>::v8 straight(lds_char *lds, int tile, int r0, int i) const { return lds_read8<E>(lds + s[i] + (tile + r0 * DP * 2)); }
+  __device__ typename Vec<E>::v8 transposed(lds_char *lds, int tile, int r0, int i) const {
+    static_assert(DP == 64 || DP == 128, "rows 8 apart differ in bit 1 of the swizzle");
+    return lds_read_tr<E>(lds + t[i] + (tile + r0 * DP * 2), lds + (t[i] ^ 32) + (tile + (r0 + 8) * DP * 2));
+  }
+};
+
+/* The same in two registers: a chunk's number enters its place by exclusive or, so that every place is one such step from the first.
+ * fresh() keeps the compiler from holding them all. */
+template <class E, int DP> struct FewPlaces {
+  int s, t;
+  __device__ void init() {
+    Places<E, DP> p;
+    p.init();
+    s = p.s[0], t = p.t[0];
+  }
+  __device__ void fresh() { asm volatile("" : "+v"(s), "+v"(t)); }
+  __device__ typename Vec<E>::v8 straight(lds_char *lds, int tile, int r0, int i) const { return lds_read8<E>(lds + (s ^ 32 * i) + (tile + r0 * DP * 2)); }
+  __device__ typename Vec<E>::v8 transposed(lds_char *lds, int tile, int r0, int i) const {
+    return lds_read_tr<E>(lds + (t ^ 64 * i) + (tile + r0 * DP * 2), lds + (t ^ 64 * i ^ 32) + (tile + (r0 + 8) * DP * 2));
+  }
+};
 
 /* Row `i` of a head as the second operand of products over d: d = 16 t + 8 (l / 32) .. + 7. */
 template <class E, int DP> __device__ inline void row_fragments(const Heads &h, int64_t at, int i, bool in, int D, typename Vec<E>::v8 (&f)[DP / 16]) {
@@ -118,14 +139,25 @@ template <class E, int DP> __device__ inline void store_column(const f32x16 (&ac
       store4<E>(row, 32 * t + 8 * (r >> 2) + 4 * (lane() >> 5), D, acc[t][r] * by, acc[t][r + 1] * by, acc[t][r + 2] * by, acc[t][r + 3] * by);
 }
 
+template <int N> struct Int { static constexpr int value = N; };
+__device__ inline float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline float tanh_(float x) { return 1 - 2 * __builtin_amdgcn_rcpf(1 + exp2_(x * (2 * LOG2E))); }
 
-/* Raw products to scores times log2 e, where there is a cap or a bias (with neither, the caller folds the scale into the exponent). */
-__device__ inline float score(const Attention &a, float slope2, float raw, int distance) {
-  float s = raw * a.scale;
-  if (a.cap > 0) s = a.cap * tanh_(s / a.cap);
-  return s * LOG2E - slope2 * abs(distance);
+/* Kinds of scores: the scale alone (folded into the exponent), capped, with a bias, both. */
+constexpr int CAP = 1, BIAS = 2;
+
+/* Of a raw product: the score times log2 e, and dscore / draw over the scale, where wanted. */
+template <int KIND> __device__ inline float score(const Attention &a, float slope2, float raw, int distance, float &by) {
+  by = 1;
+  float s = raw * (a.scale * LOG2E);
+  if (KIND & CAP) {
+    float t = tanh_(raw * (a.scale / a.cap));
+    s = a.cap * LOG2E * t;
+    by = 1 - t * t;
+  }
+  if (KIND & BIAS) s -= slope2 * (float)abs(distance);
+  return s;
 }
 
 /* The smallest begin and largest end over the workgroup's rows (each wave's in its lanes). */
@@ -145,25 +177,27 @@ __device__ inline int wave_max(int v) {
   return uniform(v);
 }
 
-/* Which (tile, head, sequence) a workgroup takes.  Heads vary slowest within an XCD's share, so that what it reads of keys and values
- * stays in its L2; the last tiles, which see most keys where a mask is causal, go first. */
-__device__ inline void place(int tiles, int heads, int &tile, int &head, int &b) {
-  int64_t id = xcd_order(blockIdx.x, gridDim.x);
-  tile = tiles - 1 - (int)(id % tiles);
-  head = (int)(id / tiles % heads);
-  b = (int)(id / tiles / heads);
+/* Which (tile, head, sequence) a workgroup takes: tile by tile, all heads of one tile in a row.  Workgroups are dealt to the 8 XCDs in
+ * turn, so that with a multiple of 8 heads an XCD sees only its own keys and values; the tiles that see most keys where a mask is causal
+ * go first (the last of queries, the first of keys), so that short ones fill up what long ones leave. */
+__device__ inline void place(int heads, int B, int &tile, int &head, int &b) {
+  int n = heads * B;
+  tile = blockIdx.x / n;
+  head = blockIdx.x % n % heads;
+  b = blockIdx.x % n / heads;
 }
 
 /* ---- forward ------------------------------------------------------------------------------------------------------------------
  * A wave has 32 queries, one a lane pair: scores are formed transposed (keys in the registers, the query in the lane), so that a
  * query's running maximum and sum are its lane's own and the exponentials are, as they lie, the second operand of o^T += v^T p^T. */
-template <class E, int DP> __global__ __launch_bounds__(WAVES * 64, 2) void k_attention(Attention a) {
+template <class E, int DP, int KIND> __global__ __launch_bounds__(WAVES * 64, 2) void k_attention(Attention a) {
   using R = Rows<DP>;
   __shared__ __attribute__((aligned(1024))) char mem[4 * R::BYTES];
   __shared__ int part[WAVES][2];
   lds_char *lds = (lds_char *)mem;
   int tile, h, b;
-  place((a.Sq + ROWS - 1) / ROWS, a.H, tile, h, b);
+  place(a.H, a.B, tile, h, b);
+  tile = (a.Sq + ROWS - 1) / ROWS - 1 - tile;
   int g = h / (a.H / a.G);
   int wave = uniform(threadIdx.x / 64), l = lane(), half = l >> 5;
   int i = tile * ROWS + wave * 32 + (l & 31), offset = a.Sk - a.Sq;
@@ -179,9 +213,11 @@ template <class E, int DP> __global__ __launch_bounds__(WAVES * 64, 2) void k_at
   for (int t = 0; t < DP / 32; t++)
     for (int r = 0; r < 16; r++) acc[t][r] = 0;
   float top = -INFINITY, sum = 0;
-  bool plain = !(a.cap > 0) && !a.slopes;
-  float slope2 = a.slopes ? a.slopes[h] * LOG2E : 0.f, c = plain ? a.scale * LOG2E : 1.f;
+  float slope2 = KIND & BIAS ? a.slopes[h] * LOG2E : 0.f;
+  const float c = KIND ? 1.f : a.scale * LOG2E;
 
+  Places<E, DP> at;
+  at.init();
   R rk, rv;
   rk.init(a.k.row, a.D);
   rv.init(a.v.row, a.D);
@@ -191,59 +227,79 @@ template <class E, int DP> __global__ __launch_bounds__(WAVES * 64, 2) void k_at
     rk.load(pk, a.k.row, lds, first * KT, lo, hi);
     rv.load(pv, a.v.row, lds + R::BYTES, first * KT, lo, hi);
   }
-  for (int t = first; t < last; t++) {
+  auto step = [&](int t, auto which) {
+    constexpr int K = decltype(which)::value * 2 * R::BYTES, V = K + R::BYTES, NEXT = 2 * R::BYTES - K;
     wait_barrier();
-    lds_char *K = lds + (t - first) % 2 * 2 * R::BYTES, *V = K + R::BYTES;
     if (t + 1 < last) {
-      lds_char *next = lds + (t + 1 - first) % 2 * 2 * R::BYTES;
-      rk.load(pk, a.k.row, next, (t + 1) * KT, lo, hi);
-      rv.load(pv, a.v.row, next + R::BYTES, (t + 1) * KT, lo, hi);
+      rk.load(pk, a.k.row, lds + NEXT, (t + 1) * KT, lo, hi);
+      rv.load(pv, a.v.row, lds + NEXT + R::BYTES, (t + 1) * KT, lo, hi);
     }
     int j0 = t * KT;
-    if (j0 >= whi || j0 + KT <= wlo) continue;
+    if (j0 >= whi || j0 + KT <= wlo) return;
     f32x16 s[2];
 #pragma unroll
     for (int x = 0; x < 2; x++) {
+#pragma unroll
       for (int r = 0; r < 16; r++) s[x][r] = 0;
 #pragma unroll
-      for (int d = 0; d < DP / 16; d++) s[x] = mfma(straight<E, DP>(K, 32 * x, d), q[d], s[x]);
+      for (int d = 0; d < DP / 16; d++) s[x] = mfma(at.straight(lds, K, 32 * x, d), q[d], s[x]);
     }
-    if (!plain)
+    int j1 = j0 + 4 * half;
+    if (KIND) {
+#pragma unroll
       for (int x = 0; x < 2; x++)
-        for (int r = 0; r < 16; r++) s[x][r] = score(a, slope2, s[x][r], i + offset - (j0 + 32 * x + 8 * (r >> 2) + 4 * half + (r & 3)));
-    if (j0 < full_lo || j0 + KT > full_hi)
-      for (int x = 0; x < 2; x++)
+#pragma unroll
         for (int r = 0; r < 16; r++) {
-          int j = j0 + 32 * x + 8 * (r >> 2) + 4 * half + (r & 3);
+          float by;
+          s[x][r] = score<KIND>(a, slope2, s[x][r], i + offset - (j1 + 32 * x + 8 * (r >> 2) + (r & 3)), by);
+        }
+    }
+    if (j0 < full_lo || j0 + KT > full_hi) {
+#pragma unroll
+      for (int x = 0; x < 2; x++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+          int j = j1 + 32 * x + 8 * (r >> 2) + (r & 3);
           s[x][r] = j >= begin && j < end ? s[x][r] : -INFINITY;
         }
-    float m = fmaxf(s[0][0], s[1][0]);
-    for (int r = 1; r < 16; r++) m = fmaxf(m, fmaxf(s[0][r], s[1][r]));
-    m = fmaxf(m, __shfl_xor(m, 32)) * c;
+    }
+    float m = max3(s[0][0], s[0][1], s[1][0]);
+#pragma unroll
+    for (int r = 2; r < 16; r += 2) m = max3(m, s[0][r], s[0][r + 1]);
+#pragma unroll
+    for (int r = 1; r < 15; r += 2) m = max3(m, s[1][r], s[1][r + 1]);
+    m = max3(m, s[1][15], s[1][15]);
+    m = max3(m, __shfl_xor(m, 32), m) * c;
     /* The exponents' origin follows the maximum only when it has risen by 8: what was summed before is then scaled, and no
      * exponential passes 2^8. */
     if (__any(m > top + 8)) {
-      float to = fmaxf(m, top), by = to == -INFINITY ? 1.f : exp2_(top - to);
+      float to = m > top ? m : top, by = to == -INFINITY ? 1.f : exp2_(top - to);
       sum *= by;
+#pragma unroll
       for (int d = 0; d < DP / 32; d++)
+#pragma unroll
         for (int r = 0; r < 16; r++) acc[d][r] *= by;
       top = to;
     }
     float from = top == -INFINITY ? 0.f : top;
-    float p[2][16];
-    for (int x = 0; x < 2; x++)
-      for (int r = 0; r < 16; r++) {
-        p[x][r] = exp2_(s[x][r] * c - from);
-        sum += p[x][r];
-      }
 #pragma unroll
     for (int x = 0; x < 2; x++)
 #pragma unroll
       for (int k = 0; k < 2; k++) {
-        typename Vec<E>::v8 w = round8<E>(p[x] + 8 * k);
+        float p[8];
 #pragma unroll
-        for (int d = 0; d < DP / 32; d++) acc[d] = mfma(transposed<E, DP>(V, 32 * x + 16 * k, 32 * d), w, acc[d]);
+        for (int r = 0; r < 8; r++) {
+          p[r] = exp2_(s[x][8 * k + r] * c - from);
+          sum += p[r];
+        }
+        typename Vec<E>::v8 w = round8<E>(p);
+#pragma unroll
+        for (int d = 0; d < DP / 32; d++) acc[d] = mfma(at.transposed(lds, V, 32 * x + 16 * k, d), w, acc[d]);
       }
+  };
+  for (int t = first; t < last; t += 2) {
+    step(t, Int<0>());
+    if (t + 1 < last) step(t + 1, Int<1>());
   }
   sum += __shfl_xor(sum, 32);
   if (i < a.Sq) {
@@ -253,8 +309,8 @@ template <class E, int DP> __global__ __launch_bounds__(WAVES * 64, 2) void k_at
 }
 
 /* ---- backward --------------------------------------------------------------------------------------------------------------- */
-/* delta = do . o: 16 lanes a row, eight values each. */
-template <class E> __global__ __launch_bounds__(256) void k_delta(Attention a, float *delta) {
+/* delta = do . o and lse in powers of 2: 16 lanes a row, eight values each. */
+template <class E> __global__ __launch_bounds__(256) void k_delta(Attention a, float *lse2, float *delta) {
   int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16, rows = (int64_t)a.B * a.H * a.Sq;
   if (row >= rows) return;
   int i = (int)(row % a.Sq), h = (int)(row / a.Sq % a.H), b = (int)(row / a.Sq / a.H), d = threadIdx.x % 16 * 8;
@@ -263,7 +319,10 @@ template <class E> __global__ __launch_bounds__(256) void k_delta(Attention a, f
   typename Vec<E>::v8 y = load8<E>((const E *)(a.o.p + b * a.o.batch + h * a.o.head + i * a.o.row) + d, a.D - d);
   for (int e = 0; e < 8; e++) s += (float)x[e] * (float)y[e];
   for (int k = 8; k > 0; k >>= 1) s += __shfl_xor(s, k);
-  if (d == 0) delta[row] = s;
+  if (d == 0) {
+    float x = a.lse[row];
+    delta[row] = s, lse2[row] = x == -INFINITY ? 0.f : x * LOG2E;
+  }
 }
 
 __global__ __launch_bounds__(64) void k_ranges(Attention a, int4 *ranges) {
@@ -274,33 +333,24 @@ __global__ __launch_bounds__(64) void k_ranges(Attention a, int4 *ranges) {
   if (threadIdx.x == 0) ranges[blockIdx.x] = make_int4(lo, hi, flo, fhi);
 }
 
-/* What a pair (query, key) gives: p = e^(s - lse) and ds = p (dp - delta) ds/draw, both 0 where the key is not seen. */
-__device__ inline void pair(const Attention &a, bool plain, float c, float slope2, bool seen, int distance, float lse2, float delta, float raw, float dp,
-                            float &p, float &ds) {
-  float by = a.scale, e = raw * c;
-  if (!plain) {
-    float s = raw * a.scale;
-    if (a.cap > 0) {
-      float t = tanh_(s / a.cap);
-      s = a.cap * t;
-      by *= 1 - t * t;
-    }
-    e = s * LOG2E - slope2 * abs(distance);
-  }
-  p = exp2_(e - lse2);
-  ds = p * (dp - delta) * by;
-  p = seen ? p : 0.f;
-  ds = seen ? ds : 0.f;
+/* What a pair (query, key) gives: p = e^(s - lse) and ds = p (dp - delta) ds/draw but for the scale, which the sums
+ * get at the end. */
+template <int KIND> __device__ inline void pair(const Attention &a, float slope2, int distance, float lse2, float delta, float raw, float dp, float &p, float &ds) {
+  float by;
+  p = exp2_(score<KIND>(a, slope2, raw, distance, by) - lse2);
+  ds = p * (dp - delta);
+  if (KIND & CAP) ds *= by;
 }
 
 /* dq: as in the forward pass a wave has 32 queries, one a lane pair; dp^T = v do^T beside s^T = k q^T, then dq^T += k^T ds^T. */
-template <class E, int DP> __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(Attention a) {
+template <class E, int DP, int KIND> __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(Attention a) {
   using R = Rows<DP>;
   __shared__ __attribute__((aligned(1024))) char mem[4 * R::BYTES];
   __shared__ int part[WAVES][2];
   lds_char *lds = (lds_char *)mem;
   int tile, h, b;
-  place((a.Sq + ROWS - 1) / ROWS, a.H, tile, h, b);
+  place(a.H, a.B, tile, h, b);
+  tile = (a.Sq + ROWS - 1) / ROWS - 1 - tile;
   int g = h / (a.H / a.G);
   int wave = uniform(threadIdx.x / 64), l = lane(), half = l >> 5;
   int i = tile * ROWS + wave * 32 + (l & 31), offset = a.Sk - a.Sq;
@@ -315,15 +365,16 @@ template <class E, int DP> __global__ __launch_bounds__(WAVES * 64, 2) void k_at
   row_fragments<E, DP>(a.dout, b * a.dout.batch + h * a.dout.head, i, begin < end, a.D, dout);
   float lse2 = 0, delta = 0;
   if (begin < end) {
-    int64_t at = ((int64_t)b * a.H + h) * a.Sq + i;
-    lse2 = a.lse[at] * LOG2E, delta = a.delta[at];
+    int64_t row = ((int64_t)b * a.H + h) * a.Sq + i;
+    lse2 = a.lse2[row], delta = a.delta[row];
   }
   f32x16 acc[DP / 32];
   for (int t = 0; t < DP / 32; t++)
     for (int r = 0; r < 16; r++) acc[t][r] = 0;
-  bool plain = !(a.cap > 0) && !a.slopes;
-  float slope2 = a.slopes ? a.slopes[h] * LOG2E : 0.f, c = a.scale * LOG2E;
+  float slope2 = KIND & BIAS ? a.slopes[h] * LOG2E : 0.f;
 
+  Places<E, DP> at;
+  at.init();
   R rk, rv;
   rk.init(a.k.row, a.D);
   rv.init(a.v.row, a.D);
@@ -333,53 +384,63 @@ template <class E, int DP> __global__ __launch_bounds__(WAVES * 64, 2) void k_at
     rk.load(pk, a.k.row, lds, first * KT, lo, hi);
     rv.load(pv, a.v.row, lds + R::BYTES, first * KT, lo, hi);
   }
-  for (int t = first; t < last; t++) {
+  auto step = [&](int t, auto which) {
+    constexpr int K = decltype(which)::value * 2 * R::BYTES, V = K + R::BYTES, NEXT = 2 * R::BYTES - K;
     wait_barrier();
-    lds_char *K = lds + (t - first) % 2 * 2 * R::BYTES, *V = K + R::BYTES;
     if (t + 1 < last) {
-      lds_char *next = lds + (t + 1 - first) % 2 * 2 * R::BYTES;
-      rk.load(pk, a.k.row, next, (t + 1) * KT, lo, hi);
-      rv.load(pv, a.v.row, next + R::BYTES, (t + 1) * KT, lo, hi);
+      rk.load(pk, a.k.row, lds + NEXT, (t + 1) * KT, lo, hi);
+      rv.load(pv, a.v.row, lds + NEXT + R::BYTES, (t + 1) * KT, lo, hi);
     }
-    int j0 = t * KT;
-    if (j0 >= whi || j0 + KT <= wlo) continue;
+    int j0 = t * KT, j1 = j0 + 4 * half;
+    if (j0 >= whi || j0 + KT <= wlo) return;
     bool all = j0 >= full_lo && j0 + KT <= full_hi;
 #pragma unroll
     for (int x = 0; x < 2; x++) {
       f32x16 s, dp;
+#pragma unroll
       for (int r = 0; r < 16; r++) s[r] = dp[r] = 0;
 #pragma unroll
       for (int d = 0; d < DP / 16; d++) {
-        s = mfma(straight<E, DP>(K, 32 * x, d), q[d], s);
-        dp = mfma(straight<E, DP>(V, 32 * x, d), dout[d], dp);
+        s = mfma(at.straight(lds, K, 32 * x, d), q[d], s);
+        dp = mfma(at.straight(lds, V, 32 * x, d), dout[d], dp);
       }
       float ds[16];
+#pragma unroll
       for (int r = 0; r < 16; r++) {
-        int j = j0 + 32 * x + 8 * (r >> 2) + 4 * half + (r & 3);
         float p;
-        pair(a, plain, c, slope2, all || (j >= begin && j < end), i + offset - j, lse2, delta, s[r], dp[r], p, ds[r]);
+        pair<KIND>(a, slope2, i + offset - (j1 + 32 * x + 8 * (r >> 2) + (r & 3)), lse2, delta, s[r], dp[r], p, ds[r]);
+      }
+      if (!all) {
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+          int j = j1 + 32 * x + 8 * (r >> 2) + (r & 3);
+          ds[r] = j >= begin && j < end ? ds[r] : 0.f;
+        }
       }
 #pragma unroll
       for (int k = 0; k < 2; k++) {
         typename Vec<E>::v8 w = round8<E>(ds + 8 * k);
 #pragma unroll
-        for (int d = 0; d < DP / 32; d++) acc[d] = mfma(transposed<E, DP>(K, 32 * x + 16 * k, 32 * d), w, acc[d]);
+        for (int d = 0; d < DP / 32; d++) acc[d] = mfma(at.transposed(lds, K, 32 * x + 16 * k, d), w, acc[d]);
       }
     }
+  };
+  for (int t = first; t < last; t += 2) {
+    step(t, Int<0>());
+    if (t + 1 < last) step(t + 1, Int<1>());
   }
-  if (i < a.Sq) store_column<E, DP>(acc, 1.f, (char *)a.dq.p + b * a.dq.batch + h * a.dq.head + i * a.dq.row, a.D);
+  if (i < a.Sq) store_column<E, DP>(acc, a.scale, (char *)a.dq.p + b * a.dq.batch + h * a.dq.head + i * a.dq.row, a.D);
 }
 
 /* dk, dv: a wave has 32 keys, one a lane pair, and meets all queries that see them, of every head that shares them, 64 at a time:
  * s = q k^T and dp = do v^T (queries in the registers), then dv^T += do^T p and dk^T += q^T ds. */
-template <class E, int DP> __global__ __launch_bounds__(WAVES * 64, DP == 128 ? 1 : 2) void k_attention_dkv(Attention a) {
+template <class E, int DP, int KIND> __global__ __launch_bounds__(WAVES * 64, DP == 128 ? 1 : 2) void k_attention_dkv(Attention a) {
   using R = Rows<DP>;
-  __shared__ __attribute__((aligned(1024))) char mem[4 * R::BYTES];
-  __shared__ __attribute__((aligned(16))) float row_lse[2][KT], row_delta[2][KT];
-  __shared__ __attribute__((aligned(16))) int row_begin[2][KT], row_end[2][KT];
+  __shared__ __attribute__((aligned(1024))) char mem[4 * R::BYTES + 2 * 4 * KT * 4];
+  constexpr int NUMBERS = 4 * R::BYTES; /* per buffer: lse, delta, begin, end of 64 queries */
   lds_char *lds = (lds_char *)mem;
   int tiles = (a.Sq + KT - 1) / KT, tile, g, b;
-  place((a.Sk + ROWS - 1) / ROWS, a.G, tile, g, b);
+  place(a.G, a.B, tile, g, b);
   int wave = uniform(threadIdx.x / 64), l = lane(), half = l >> 5;
   int k0 = tile * ROWS, w0 = k0 + wave * 32, j = w0 + (l & 31), offset = a.Sk - a.Sq, shared = a.H / a.G;
 
@@ -389,107 +450,112 @@ template <class E, int DP> __global__ __launch_bounds__(WAVES * 64, DP == 128 ? 
   f32x16 dk[DP / 32], dv[DP / 32];
   for (int t = 0; t < DP / 32; t++)
     for (int r = 0; r < 16; r++) dk[t][r] = dv[t][r] = 0;
-  bool plain = !(a.cap > 0) && !a.slopes;
-  float c = a.scale * LOG2E;
+  FewPlaces<E, DP> at;
+  at.init();
   R rq, rd;
   rq.init(a.q.row, a.D);
   rd.init(a.dout.row, a.D);
 
   /* (head of the group, tile of queries) pairs in order, those that see none of the workgroup's keys left out */
   const int4 *ranges = a.ranges + (int64_t)b * tiles;
-  auto next = [&](int at) {
-    for (at++; at < shared * tiles; at++) {
-      int4 r = ranges[at % tiles];
-      if (r.x < k0 + ROWS && r.y > k0) break;
-    }
-    return at;
+  int head = 0, qt = -1; /* the pair that is loaded next */
+  auto next = [&] {
+    for (qt++; head < shared; head++, qt = 0)
+      for (; qt < tiles; qt++) {
+        int4 r = ranges[qt];
+        if (r.x < k0 + ROWS && r.y > k0) return;
+      }
   };
-  float in_lse = 0, in_delta = 0;
-  int in_begin = FAR, in_end = 0;
-  auto ask = [&](int at, int which) { /* rows that see nothing are zeros, whatever they hold */
-    int h = g * shared + at / tiles, i0 = at % tiles * KT;
+  auto ask = [&](int which) { /* rows that see nothing are zeros, whatever they hold */
+    int h = g * shared + head, i0 = qt * KT;
     lds_char *to = lds + which * 2 * R::BYTES;
     const char *pq = a.q.p + b * a.q.batch + h * a.q.head, *pd = a.dout.p + b * a.dout.batch + h * a.dout.head;
-    if (ranges[at % tiles].z == FAR) { /* some row of the tile sees nothing, or there is none */
-      __amdgpu_buffer_rsrc_t bq = buffer(pq + (int64_t)i0 * a.q.row), bd = buffer(pd + (int64_t)i0 * a.dout.row);
-      for (int n = 0; n < R::LOADS; n++) {
+    if (ranges[qt].z == FAR) { /* some row of the tile sees nothing, or there is none */
+      auto in = [&](int i) {
         int lo, hi;
-        key_range(a, b, i0 + rq.row[n], lo, hi);
-        lds_char *place = to + (n * WAVES * 64 + wave * 64) * 16;
-        load_lds(bq, place, lo < hi ? rq.off[n] : OOB_LAYER_OUT);
-        load_lds(bd, place + R::BYTES, lo < hi ? rd.off[n] : OOB_LAYER_OUT);
-      }
+        key_range(a, b, i, lo, hi);
+        return lo < hi;
+      };
+      rq.load(pq, a.q.row, to, i0, in);
+      rd.load(pd, a.dout.row, to + R::BYTES, i0, in);
     } else {
       rq.load(pq, a.q.row, to, i0, 0, a.Sq);
       rd.load(pd, a.dout.row, to + R::BYTES, i0, 0, a.Sq);
     }
-    if (threadIdx.x < KT) {
-      int i = i0 + threadIdx.x;
-      key_range(a, b, i, in_begin, in_end);
-      in_lse = in_delta = 0;
-      if (in_begin < in_end) {
-        int64_t row = ((int64_t)b * a.H + h) * a.Sq + i;
-        in_lse = a.lse[row] * LOG2E, in_delta = a.delta[row];
-      }
-    }
+    /* a wave each for the rows' numbers; past the last row: zeros */
+    int64_t row = ((int64_t)b * a.H + h) * a.Sq + i0, at = (int64_t)b * a.Sq + i0;
+    const void *from = wave == 0 ? (const void *)(a.lse2 + row) : wave == 1 ? (const void *)(a.delta + row) : wave == 2 ? (const void *)(a.begin + at) : (const void *)(a.end + at);
+    if (wave < 2 || (wave == 2 ? a.begin : a.end)) load_lds4(buffer(from), lds + NUMBERS + (which * 4 + wave) * KT * 4, i0 + l < a.Sq ? l * 4 : OOB_LAYER_OUT);
   };
-  auto put = [&](int which) {
-    if (threadIdx.x < KT) {
-      row_lse[which][threadIdx.x] = in_lse, row_delta[which][threadIdx.x] = in_delta;
-      row_begin[which][threadIdx.x] = in_begin, row_end[which][threadIdx.x] = in_end;
-    }
-  };
-
-  int at = next(-1), buf = 0;
-  if (at < shared * tiles) ask(at, 0);
-  while (at < shared * tiles) {
-    put(buf);
-    __builtin_amdgcn_s_waitcnt(0xc07f); /* lgkmcnt(0): the row's numbers are in LDS */
+  next();
+  if (head < shared) ask(0);
+  auto step = [&](auto which) {
+    constexpr int B = decltype(which)::value, Q = B * 2 * R::BYTES, D = Q + R::BYTES, N = NUMBERS + B * 4 * KT * 4;
+    int i0 = qt * KT;
+    int4 range = ranges[qt];
+    float slope2 = KIND & BIAS ? a.slopes[g * shared + head] * LOG2E : 0.f;
     wait_barrier();
-    int then = next(at);
-    if (then < shared * tiles) ask(then, buf ^ 1);
-    lds_char *Q = lds + buf * 2 * R::BYTES, *D = Q + R::BYTES;
-    int4 range = ranges[at % tiles];
-    int i0 = at % tiles * KT;
-    float slope2 = a.slopes ? a.slopes[g * shared + at / tiles] * LOG2E : 0.f;
-    if (w0 < range.y && w0 + 32 > range.x) {
-      bool all = w0 >= range.z && w0 + 32 <= range.w;
+    next();
+    if (head < shared) ask(B ^ 1);
+    if (w0 >= range.y || w0 + 32 <= range.x) return;
+    bool all = w0 >= range.z && w0 + 32 <= range.w;
 #pragma unroll
-      for (int x = 0; x < 2; x++) {
-        f32x16 s, dp;
-        for (int r = 0; r < 16; r++) s[r] = dp[r] = 0;
+    for (int x = 0; x < 2; x++) {
+      at.fresh();
+      f32x16 s, dp;
 #pragma unroll
-        for (int d = 0; d < DP / 16; d++) {
-          s = mfma(straight<E, DP>(Q, 32 * x, d), k[d], s);
-          dp = mfma(straight<E, DP>(D, 32 * x, d), v[d], dp);
+      for (int r = 0; r < 16; r++) s[r] = dp[r] = 0;
+#pragma unroll
+      for (int d = 0; d < DP / 16; d++) {
+        s = mfma(at.straight(lds, Q, 32 * x, d), k[d], s);
+        dp = mfma(at.straight(lds, D, 32 * x, d), v[d], dp);
+      }
+#pragma unroll
+      for (int n = 0; n < 4; n++) {
+        int row = 32 * x + 8 * n;
+        f32x4 lse = lds_numbers<f32x4>(lds + 16 * half + (N + row * 4)), delta = lds_numbers<f32x4>(lds + 16 * half + (N + KT * 4 + row * 4));
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          float p, ds;
+          pair<KIND>(a, slope2, i0 + row + 4 * half + e + offset - j, lse[e], delta[e], s[4 * n + e], dp[4 * n + e], p, ds);
+          s[4 * n + e] = p, dp[4 * n + e] = ds;
         }
-        float p[16], ds[16];
+      }
+      if (!all) {
 #pragma unroll
         for (int n = 0; n < 4; n++) {
-          int row = 32 * x + 8 * n + 4 * half;
-          float4 lse = *(const float4 *)(row_lse[buf] + row), delta = *(const float4 *)(row_delta[buf] + row);
-          int4 lo = *(const int4 *)(row_begin[buf] + row), hi = *(const int4 *)(row_end[buf] + row);
-          const float *pl = &lse.x, *pd = &delta.x;
-          const int *pb = &lo.x, *pe = &hi.x;
+          int row = 32 * x + 8 * n;
+          i32x4 lo = {0, 0, 0, 0}, hi = {a.Sk, a.Sk, a.Sk, a.Sk};
+          if (a.begin) lo = lds_numbers<i32x4>(lds + 16 * half + (N + 2 * KT * 4 + row * 4));
+          if (a.end) hi = lds_numbers<i32x4>(lds + 16 * half + (N + 3 * KT * 4 + row * 4));
 #pragma unroll
-          for (int e = 0; e < 4; e++)
-            pair(a, plain, c, slope2, all || (j >= pb[e] && j < pe[e]), i0 + row + e + offset - j, pl[e], pd[e], s[4 * n + e], dp[4 * n + e], p[4 * n + e], ds[4 * n + e]);
-        }
-#pragma unroll
-        for (int m = 0; m < 2; m++) {
-          typename Vec<E>::v8 wp = round8<E>(p + 8 * m), ws = round8<E>(ds + 8 * m);
-#pragma unroll
-          for (int d = 0; d < DP / 32; d++) {
-            dv[d] = mfma(transposed<E, DP>(D, 32 * x + 16 * m, 32 * d), wp, dv[d]);
-            dk[d] = mfma(transposed<E, DP>(Q, 32 * x + 16 * m, 32 * d), ws, dk[d]);
+          for (int e = 0; e < 4; e++) {
+            int i = i0 + row + 4 * half + e;
+            bool seen = j >= lo[e] && j < hi[e] && i < a.Sq && (!a.causal || j - offset <= i);
+            s[4 * n + e] = seen ? s[4 * n + e] : 0.f;
+            dp[4 * n + e] = seen ? dp[4 * n + e] : 0.f;
           }
         }
       }
+#pragma unroll
+      for (int m = 0; m < 2; m++) {
+        typename Vec<E>::v8 wp, ws;
+#pragma unroll
+        for (int e = 0; e < 8; e++) wp[e] = (E)s[8 * m + e], ws[e] = (E)dp[8 * m + e];
+#pragma unroll
+        for (int d = 0; d < DP / 32; d++) {
+          dv[d] = mfma(at.transposed(lds, D, 32 * x + 16 * m, d), wp, dv[d]);
+          dk[d] = mfma(at.transposed(lds, Q, 32 * x + 16 * m, d), ws, dk[d]);
+        }
+      }
     }
-    at = then, buf ^= 1;
+  };
+  while (head < shared) {
+    step(Int<0>());
+    if (head < shared) step(Int<1>());
   }
   if (j < a.Sk) {
-    store_column<E, DP>(dk, 1.f, (char *)a.dk.p + b * a.dk.batch + g * a.dk.head + j * a.dk.row, a.D);
+    store_column<E, DP>(dk, a.scale, (char *)a.dk.p + b * a.dk.batch + g * a.dk.head + j * a.dk.row, a.D);
     store_column<E, DP>(dv, 1.f, (char *)a.dv.p + b * a.dv.batch + g * a.dv.head + j * a.dv.row, a.D);
   }
 }
@@ -547,6 +613,13 @@ static Attention attention_of(const oob_attention *p) {
   return a;
 }
 
+template <class F> static void by_kind(const Attention &a, F f) {
+  if (a.cap > 0 && a.slopes) f(Int<CAP | BIAS>());
+  else if (a.cap > 0) f(Int<CAP>());
+  else if (a.slopes) f(Int<BIAS>());
+  else f(Int<0>());
+}
+
 static size_t forward_bytes(const oob_attention *p) {
   Attention a = attention_of(p);
   Arena w{nullptr, 0, 0};
@@ -562,8 +635,11 @@ template <class E> static int forward(const oob_attention *p, Arena w, hipStream
   if (!w.ok()) return OOB_ECAPACITY;
   unsigned n = (unsigned)((int64_t)a.B * a.H * ((a.Sq + ROWS - 1) / ROWS));
   if (n) {
-    if (a.D <= 64) k_attention<E, 64><<<n, WAVES * 64, 0, st>>>(a);
-    else k_attention<E, 128><<<n, WAVES * 64, 0, st>>>(a);
+    by_kind(a, [&](auto kind) {
+      constexpr int KIND = decltype(kind)::value;
+      if (a.D <= 64) k_attention<E, 64, KIND><<<n, WAVES * 64, 0, st>>>(a);
+      else k_attention<E, 128, KIND><<<n, WAVES * 64, 0, st>>>(a);
+    });
   }
   return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
 }
@@ -571,7 +647,7 @@ template <class E> static int forward(const oob_attention *p, Arena w, hipStream
 static size_t backward_bytes(const oob_attention *p, const oob_attention_grad *q) {
   Attention a = attention_of(p);
   Arena w{nullptr, 0, 0};
-  w.take((size_t)a.B * a.H * a.Sq * 4);
+  w.take((size_t)a.B * a.H * a.Sq * 8);
   w.take((size_t)a.B * ((a.Sq + KT - 1) / KT) * sizeof(int4));
   for (const Heads &h : {a.k, a.v})
     if (!loadable(h, a.D)) w.take(packed_bytes(a.B, a.Sk, a.G, a.D));
@@ -584,13 +660,13 @@ template <class E> static int backward(const oob_attention *p, const oob_attenti
   Attention a = attention_of(p);
   a.dout = heads_of(q->dout, q->dout_stride);
   a.dq = heads_of(q->dq, q->dq_stride), a.dk = heads_of(q->dk, q->dk_stride), a.dv = heads_of(q->dv, q->dv_stride);
-  float *delta = (float *)w.take((size_t)a.B * a.H * a.Sq * 4);
-  int4 *ranges = (int4 *)w.take((size_t)a.B * ((a.Sq + KT - 1) / KT) * sizeof(int4));
-  a.delta = delta, a.ranges = ranges;
-  if (!w.ok()) return OOB_ECAPACITY;
   int64_t rows = (int64_t)a.B * a.H * a.Sq;
+  float *lse2 = (float *)w.take((size_t)rows * 8), *delta = lse2 + rows;
+  int4 *ranges = (int4 *)w.take((size_t)a.B * ((a.Sq + KT - 1) / KT) * sizeof(int4));
+  a.lse2 = lse2, a.delta = delta, a.ranges = ranges;
+  if (!w.ok()) return OOB_ECAPACITY;
   if (rows) {
-    k_delta<E><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>(a, delta);
+    k_delta<E><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>(a, lse2, delta);
     k_ranges<<<(unsigned)(a.B * ((a.Sq + KT - 1) / KT)), 64, 0, st>>>(a, ranges);
   }
   pack(a.k, a.B, a.Sk, a.G, a.D, w, st);
@@ -599,14 +675,13 @@ template <class E> static int backward(const oob_attention *p, const oob_attenti
   pack(a.dout, a.B, a.Sq, a.H, a.D, w, st);
   if (!w.ok()) return OOB_ECAPACITY;
   unsigned nq = (unsigned)((int64_t)a.B * a.H * ((a.Sq + ROWS - 1) / ROWS)), nk = (unsigned)((int64_t)a.B * a.G * ((a.Sk + ROWS - 1) / ROWS));
-  if (nk) {
-    if (a.D <= 64) k_attention_dkv<E, 64><<<nk, WAVES * 64, 0, st>>>(a);
-    else k_attention_dkv<E, 128><<<nk, WAVES * 64, 0, st>>>(a);
-  }
-  if (nq) {
-    if (a.D <= 64) k_attention_dq<E, 64><<<nq, WAVES * 64, 0, st>>>(a);
-    else k_attention_dq<E, 128><<<nq, WAVES * 64, 0, st>>>(a);
-  }
+  by_kind(a, [&](auto kind) {
+    constexpr int KIND = decltype(kind)::value;
+    if (nk && a.D <= 64) k_attention_dkv<E, 64, KIND><<<nk, WAVES * 64, 0, st>>>(a);
+    else if (nk) k_attention_dkv<E, 128, KIND><<<nk, WAVES * 64, 0, st>>>(a);
+    if (nq && a.D <= 64) k_attention_dq<E, 64, KIND><<<nq, WAVES * 64, 0, st>>>(a);
+    else if (nq) k_attention_dq<E, 128, KIND><<<nq, WAVES * 64, 0, st>>>(a);
+  });
   return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
 }
 

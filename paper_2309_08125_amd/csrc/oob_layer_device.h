@@ -15,6 +15,7 @@ typedef __bf16 bf16;
 typedef _Float16 fp16;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -49,10 +50,14 @@ __device__ inline __amdgpu_buffer_rsrc_t buffer(const void *base) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, 0x7fffffff, 0x00020000);
 }
 
-/* 64 lanes x 16 bytes from `r` at each lane's offset to 1024 consecutive bytes of LDS. */
-__device__ inline void load_lds(__amdgpu_buffer_rsrc_t r, lds_char *to, uint32_t offset) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)to, 16, offset, 0, 0, 0);
+/* 64 lanes x 16 (4) bytes from `r` at each lane's offset, and `more` (which the bounds do not see), to 1024 (256) consecutive bytes of LDS. */
+__device__ inline void load_lds(__amdgpu_buffer_rsrc_t r, lds_char *to, uint32_t offset, uint32_t more = 0) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)to, 16, offset, more, 0, 0);
 }
+__device__ inline void load_lds4(__amdgpu_buffer_rsrc_t r, lds_char *to, uint32_t offset) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)to, 4, offset, 0, 0, 0);
+}
+template <class V> __device__ inline V lds_numbers(lds_char *p) { return *(__attribute__((address_space(3))) V *)p; }
 
 /* Waits for the loads in flight, then for the workgroup. */
 __device__ inline void wait_barrier() {
