@@ -18,11 +18,16 @@ struct Attention {
   /* backward */
   Heads dout, dq, dk, dv;
   const float *lse2, *delta; /* [B][H][Sq]: lse log2 e (0 where there is none), do . o */
-  const int4 *ranges;  /* [B][tiles of 64 queries]: smallest begin, largest end, largest begin, smallest end */
+  const int4 *ranges;  /* [B][tiles of 32 queries]: smallest begin, largest end, largest begin, smallest end */
 };
 
-constexpr int KT = 64;      /* rows of a tile in LDS (keys; queries in dk, dv) */
-constexpr int WAVES = 4, ROWS = WAVES * 32; /* queries (keys) of a workgroup: 32 a wave */
+/* A workgroup is two teams of four waves on the same 128 rows (queries; keys in dk, dv): 32 rows a wave, the other side's tiles dealt to
+ * the teams in turn, and what the teams have summed joined at the end.  The teams take turns at the matrix cores as well: a step is a phase
+ * of matrix products and a phase of exponentials, a barrier behind each, and one team is a phase behind the other, so that each SIMD has
+ * one wave in either phase.  (Waves w and w + 4 share a SIMD.) */
+constexpr int TEAM = 256, THREADS = 2 * TEAM, ROWS = 128;
+constexpr int KT = 64; /* keys of a tile in the forward pass */
+constexpr int GT = 32; /* rows of a tile in the backward pass */
 constexpr float LOG2E = 1.44269504f, LN2 = 0.69314718f;
 constexpr int FAR = 0x3fffffff; /* the begin of a row that sees nothing */
 
@@ -45,14 +50,14 @@ __device__ inline void key_range(const Attention &a, int b, int i, int &begin, i
   if (lo < hi) begin = lo, end = hi;
 }
 
-/* 64 rows of a head on their way to LDS, 16 (DP 128) or 32 rows a load: rows that far apart have the same swizzle, so that a lane has one
- * offset and the loads differ by a scalar. */
-template <int DP> struct Rows {
-  static constexpr int BYTES = KT * DP * 2, LOADS = BYTES / (WAVES * 64 * 16), STEP = KT / LOADS;
+/* N rows of a head on their way to a team's LDS, 16 (DP 128) or 32 rows a load: rows that far apart have the same swizzle, so that a lane
+ * has one offset and the loads differ by a scalar.  Every load is issued, whether or not there are such rows: the waits count loads. */
+template <int DP, int N> struct Rows {
+  static constexpr int BYTES = N * DP * 2, LOADS = BYTES / (TEAM * 16), STEP = N / LOADS;
   uint32_t off;
   int row;
   __device__ void init(int64_t stride, int D) {
-    int p = threadIdx.x * 16, c = (p / 16 % (DP / 8)) ^ swizzle<DP>(p / (DP * 2));
+    int p = threadIdx.x % TEAM * 16, c = (p / 16 % (DP / 8)) ^ swizzle<DP>(p / (DP * 2));
     row = p / (DP * 2);
     off = c * 8 < D ? (uint32_t)(row * stride + c * 16) : OOB_LAYER_OUT;
   }
@@ -62,10 +67,10 @@ template <int DP> struct Rows {
   }
   template <class F> __device__ void load(const char *base, int64_t stride, lds_char *to, int first, F in) {
     __amdgpu_buffer_rsrc_t r = buffer(base + first * stride);
-    int wave = uniform(threadIdx.x / 64);
+    int wave = uniform(threadIdx.x % TEAM / 64);
 #pragma unroll
     for (int i = 0; i < LOADS; i++)
-      load_lds(r, to + (i * WAVES * 64 + wave * 64) * 16, in(first + row + i * STEP) ? off : OOB_LAYER_OUT, (uint32_t)(i * STEP * stride));
+      load_lds(r, to + (i * TEAM + wave * 64) * 16, in(first + row + i * STEP) ? off : OOB_LAYER_OUT, (uint32_t)(i * STEP * stride));
   }
 };
 
@@ -141,6 +146,11 @@ template <class E, int DP> __device__ inline void store_column(const f32x16 (&ac
 
 template <int N> struct Int { static constexpr int value = N; };
 __device__ inline float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
+/* The larger of lanes l and l ^ 32. */
+__device__ inline float max_halves(float x) {
+  float y = __shfl_xor(x, 32);
+  return max3(x, y, y);
+}
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline float tanh_(float x) { return 1 - 2 * __builtin_amdgcn_rcpf(1 + exp2_(x * (2 * LOG2E))); }
 
@@ -160,12 +170,24 @@ template <int KIND> __device__ inline float score(const Attention &a, float slop
   return s;
 }
 
-/* The smallest begin and largest end over the workgroup's rows (each wave's in its lanes). */
+/* Barriers between phases: what a wave has read from LDS before, nobody writes until all are behind.  Not a fence, which would wait for
+ * the loads in flight too; nothing is moved from one phase to another, arithmetic neither. */
+__device__ inline void phase() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+/* All but the last N loads of the wave have landed (N < 16). */
+template <int N> __device__ inline void landed() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+/* The smallest begin and largest end over the rows (each team has them all). */
 __device__ inline void join_ranges(int &lo, int &hi, int (*part)[2]) {
   int wave = threadIdx.x / 64;
   if (lane() == 0) part[wave][0] = lo, part[wave][1] = hi;
   __syncthreads();
-  for (int w = 0; w < WAVES; w++) lo = min(lo, part[w][0]), hi = max(hi, part[w][1]);
+  for (int w = 0; w < 4; w++) lo = min(lo, part[w][0]), hi = max(hi, part[w][1]);
   lo = uniform(lo), hi = uniform(hi);
 }
 __device__ inline int wave_min(int v) {
@@ -180,32 +202,34 @@ __device__ inline int wave_max(int v) {
 /* Which (tile, head, sequence) a workgroup takes: tile by tile, all heads of one tile in a row.  Workgroups are dealt to the 8 XCDs in
  * turn, so that with a multiple of 8 heads an XCD sees only its own keys and values; the tiles that see most keys where a mask is causal
  * go first (the last of queries, the first of keys), so that short ones fill up what long ones leave. */
-__device__ inline void place(int heads, int B, int &tile, int &head, int &b) {
+__device__ inline void place(int heads, int B, int id, int &tile, int &head, int &b) {
   int n = heads * B;
-  tile = blockIdx.x / n;
-  head = blockIdx.x % n % heads;
-  b = blockIdx.x % n / heads;
+  tile = id / n;
+  head = id % n % heads;
+  b = id % n / heads;
 }
 
 /* ---- forward ------------------------------------------------------------------------------------------------------------------
  * A wave has 32 queries, one a lane pair: scores are formed transposed (keys in the registers, the query in the lane), so that a
- * query's running maximum and sum are its lane's own and the exponentials are, as they lie, the second operand of o^T += v^T p^T. */
-template <class E, int DP, int KIND> __global__ __launch_bounds__(WAVES * 64, 2) void k_attention(Attention a) {
-  using R = Rows<DP>;
-  __shared__ __attribute__((aligned(1024))) char mem[4 * R::BYTES];
-  __shared__ int part[WAVES][2];
-  lds_char *lds = (lds_char *)mem;
+ * query's running maximum and sum are its lane's own and the exponentials are, as they lie, the second operand of o^T += v^T p^T.
+ * A step's products are the scores of its tile and o^T of the tile before. */
+template <class E, int DP, int KIND> __global__ __launch_bounds__(THREADS, DP == 64 ? 4 : 2) void k_attention(Attention a) {
+  using R = Rows<DP, KT>;
+  __shared__ __attribute__((aligned(1024))) char mem[8 * R::BYTES];
+  __shared__ int part[8][2];
+  int wave = uniform(threadIdx.x / 64), team = wave / 4, l = lane(), half = l >> 5;
+  lds_char *lds = (lds_char *)mem + team * 4 * R::BYTES; /* keys of even steps, of odd ones, values of even steps, of odd ones */
   int tile, h, b;
-  place(a.H, a.B, tile, h, b);
+  place(a.H, a.B, blockIdx.x, tile, h, b);
   tile = (a.Sq + ROWS - 1) / ROWS - 1 - tile;
   int g = h / (a.H / a.G);
-  int wave = uniform(threadIdx.x / 64), l = lane(), half = l >> 5;
-  int i = tile * ROWS + wave * 32 + (l & 31), offset = a.Sk - a.Sq;
+  int i = tile * ROWS + wave % 4 * 32 + (l & 31), offset = a.Sk - a.Sq;
   int begin, end;
   key_range(a, b, i, begin, end);
   int wlo = wave_min(begin), whi = wave_max(end), full_lo = wave_max(begin), full_hi = wave_min(end);
   int lo = wlo, hi = whi;
   join_ranges(lo, hi, part);
+  int first = lo / KT, tiles = lo < hi ? (hi + KT - 1) / KT - first : 0, steps = (tiles + 1) / 2;
 
   typename Vec<E>::v8 q[DP / 16];
   row_fragments<E, DP>(a.q, b * a.q.batch + h * a.q.head, i, begin < end, a.D, q);
@@ -222,21 +246,13 @@ template <class E, int DP, int KIND> __global__ __launch_bounds__(WAVES * 64, 2)
   rk.init(a.k.row, a.D);
   rv.init(a.v.row, a.D);
   const char *pk = a.k.p + b * a.k.batch + g * a.k.head, *pv = a.v.p + b * a.v.batch + g * a.v.head;
-  int first = lo / KT, last = lo < hi ? (hi + KT - 1) / KT : first;
-  if (first < last) {
-    rk.load(pk, a.k.row, lds, first * KT, lo, hi);
-    rv.load(pv, a.v.row, lds + R::BYTES, first * KT, lo, hi);
-  }
-  auto step = [&](int t, auto which) {
-    constexpr int K = decltype(which)::value * 2 * R::BYTES, V = K + R::BYTES, NEXT = 2 * R::BYTES - K;
-    wait_barrier();
-    if (t + 1 < last) {
-      rk.load(pk, a.k.row, lds + NEXT, (t + 1) * KT, lo, hi);
-      rv.load(pv, a.v.row, lds + NEXT + R::BYTES, (t + 1) * KT, lo, hi);
-    }
-    int j0 = t * KT;
-    if (j0 >= whi || j0 + KT <= wlo) return;
-    f32x16 s[2];
+  auto key0 = [&](int n) __attribute__((always_inline)) { return (first + 2 * n + team) * KT; };
+  auto load_k = [&](int n, int which) __attribute__((always_inline)) { rk.load(pk, a.k.row, lds + which * R::BYTES, key0(n), lo, hi); };
+  auto load_v = [&](int n, int which) __attribute__((always_inline)) { rv.load(pv, a.v.row, lds + (2 + which) * R::BYTES, key0(n), lo, hi); };
+
+  f32x16 s[2];
+  typename Vec<E>::v8 p[4]; /* exponentials of the step before, rounded: the second operand of its product with v */
+  auto scores = [&](int K) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < 2; x++) {
 #pragma unroll
@@ -244,7 +260,15 @@ template <class E, int DP, int KIND> __global__ __launch_bounds__(WAVES * 64, 2)
 #pragma unroll
       for (int d = 0; d < DP / 16; d++) s[x] = mfma(at.straight(lds, K, 32 * x, d), q[d], s[x]);
     }
-    int j1 = j0 + 4 * half;
+  };
+  auto outputs = [&](int V) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 4; x++)
+#pragma unroll
+      for (int d = 0; d < DP / 32; d++) acc[d] = mfma(at.transposed(lds, V, 16 * x, d), p[x], acc[d]);
+  };
+  auto exponentials = [&](int n) __attribute__((always_inline)) {
+    int j0 = key0(n), j1 = j0 + 4 * half;
     if (KIND) {
 #pragma unroll
       for (int x = 0; x < 2; x++)
@@ -269,7 +293,7 @@ template <class E, int DP, int KIND> __global__ __launch_bounds__(WAVES * 64, 2)
 #pragma unroll
     for (int r = 1; r < 15; r += 2) m = max3(m, s[1][r], s[1][r + 1]);
     m = max3(m, s[1][15], s[1][15]);
-    m = max3(m, __shfl_xor(m, 32), m) * c;
+    m = max_halves(m) * c;
     /* The exponents' origin follows the maximum only when it has risen by 8: what was summed before is then scaled, and no
      * exponential passes 2^8. */
     if (__any(m > top + 8)) {
@@ -283,28 +307,71 @@ template <class E, int DP, int KIND> __global__ __launch_bounds__(WAVES * 64, 2)
     }
     float from = top == -INFINITY ? 0.f : top;
 #pragma unroll
-    for (int x = 0; x < 2; x++)
+    for (int x = 0; x < 4; x++)
 #pragma unroll
-      for (int k = 0; k < 2; k++) {
-        float p[8];
-#pragma unroll
-        for (int r = 0; r < 8; r++) {
-          p[r] = exp2_(s[x][8 * k + r] * c - from);
-          sum += p[r];
-        }
-        typename Vec<E>::v8 w = round8<E>(p);
-#pragma unroll
-        for (int d = 0; d < DP / 32; d++) acc[d] = mfma(at.transposed(lds, V, 32 * x + 16 * k, d), w, acc[d]);
+      for (int r = 0; r < 8; r++) {
+        float e = exp2_(s[x / 2][8 * (x % 2) + r] * c - from);
+        sum += e;
+        p[x][r] = (E)e;
       }
   };
-  for (int t = first; t < last; t += 2) {
-    step(t, Int<0>());
-    if (t + 1 < last) step(t + 1, Int<1>());
+  load_k(0, 0);
+  load_k(1, 1);
+  load_v(0, 0);
+  landed<2 * R::LOADS>();
+  phase();
+  if (team) phase();
+  auto step = [&](int n, auto which, auto begun) __attribute__((always_inline)) {
+    constexpr int W = decltype(which)::value;
+    __builtin_amdgcn_s_setprio(1);
+    scores(W * R::BYTES);
+    if (begun.value) outputs((3 - W) * R::BYTES);
+    __builtin_amdgcn_s_setprio(0);
+    phase();
+    load_k(n + 2, W);
+    load_v(n + 1, W ^ 1);
+    exponentials(n);
+    landed<2 * R::LOADS>();
+    phase();
+  };
+  if (steps) {
+    step(0, Int<0>(), Int<0>());
+    int n = 1;
+    for (; n + 1 < steps; n += 2) {
+      step(n, Int<1>(), Int<1>());
+      step(n + 1, Int<0>(), Int<1>());
+    }
+    if (n < steps) step(n, Int<1>(), Int<1>());
+    outputs((steps % 2 ? 2 : 3) * R::BYTES);
   }
+  if (!team) phase();
+
+  /* what the second team has, through LDS, to the first */
   sum += __shfl_xor(sum, 32);
+  landed<0>();
+  phase();
+  __attribute__((address_space(3))) float *other = (__attribute__((address_space(3))) float *)(lds_char *)mem + wave % 4 * (DP / 2 + 2) * 64 + l;
+  if (team) {
+#pragma unroll
+    for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) other[(d * 16 + r) * 64] = acc[d][r];
+    other[DP / 2 * 64] = top, other[(DP / 2 + 1) * 64] = sum;
+  }
+  phase();
+  if (team) return;
+  float top1 = other[DP / 2 * 64], sum1 = other[(DP / 2 + 1) * 64];
+  float to = top > top1 ? top : top1, by = to == -INFINITY ? 1.f : exp2_(top - to), by1 = to == -INFINITY ? 1.f : exp2_(top1 - to);
+  sum = sum * by + sum1 * by1;
+  float over = sum > 0 ? 1 / sum : (sum == 0 ? 0.f : sum);
+  by *= over, by1 *= over;
+#pragma unroll
+  for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) acc[d][r] = acc[d][r] * by + other[(d * 16 + r) * 64] * by1;
   if (i < a.Sq) {
-    store_column<E, DP>(acc, sum > 0 ? 1 / sum : (sum == 0 ? 0.f : sum), (char *)a.o.p + b * a.o.batch + h * a.o.head + i * a.o.row, a.D);
-    if (a.lse && half == 0) a.lse[((int64_t)b * a.H + h) * a.Sq + i] = sum == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+    store_column<E, DP>(acc, 1.f, (char *)a.o.p + b * a.o.batch + h * a.o.head + i * a.o.row, a.D);
+    if (a.lse && half == 0) a.lse[((int64_t)b * a.H + h) * a.Sq + i] = sum == 0 ? -INFINITY : (to + __builtin_amdgcn_logf(sum)) * LN2;
   }
 }
 
@@ -325,12 +392,16 @@ template <class E> __global__ __launch_bounds__(256) void k_delta(Attention a, f
   }
 }
 
-__global__ __launch_bounds__(64) void k_ranges(Attention a, int4 *ranges) {
-  int tiles = (a.Sq + KT - 1) / KT, b = blockIdx.x / tiles, t = blockIdx.x % tiles;
+__global__ __launch_bounds__(64) void k_ranges(Attention a, int4 *ranges) { /* two tiles a wave, one a half */
+  int tiles = (a.Sq + GT - 1) / GT, pairs = (tiles + 1) / 2, b = blockIdx.x / pairs, t = blockIdx.x % pairs * 2 + lane() / 32;
   int begin, end;
-  key_range(a, b, t * KT + (int)threadIdx.x, begin, end);
-  int lo = wave_min(begin), hi = wave_max(end), flo = wave_max(begin), fhi = wave_min(end);
-  if (threadIdx.x == 0) ranges[blockIdx.x] = make_int4(lo, hi, flo, fhi);
+  key_range(a, b, t * GT + lane() % 32, begin, end);
+  int4 r = make_int4(begin, end, begin, end);
+  for (int k = 16; k > 0; k >>= 1) {
+    r.x = min(r.x, __shfl_xor(r.x, k)), r.y = max(r.y, __shfl_xor(r.y, k));
+    r.z = max(r.z, __shfl_xor(r.z, k)), r.w = min(r.w, __shfl_xor(r.w, k));
+  }
+  if (lane() % 32 == 0 && t < tiles) ranges[(int64_t)b * tiles + t] = r;
 }
 
 /* What a pair (query, key) gives: p = e^(s - lse) and ds = p (dp - delta) ds/draw but for the scale, which the sums
@@ -342,23 +413,47 @@ template <int KIND> __device__ inline void pair(const Attention &a, float slope2
   if (KIND & CAP) ds *= by;
 }
 
-/* dq: as in the forward pass a wave has 32 queries, one a lane pair; dp^T = v do^T beside s^T = k q^T, then dq^T += k^T ds^T. */
-template <class E, int DP, int KIND> __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(Attention a) {
-  using R = Rows<DP>;
-  __shared__ __attribute__((aligned(1024))) char mem[4 * R::BYTES];
-  __shared__ int part[WAVES][2];
-  lds_char *lds = (lds_char *)mem;
+/* The second team's sums to the first's, 16 registers x N at a time through LDS. */
+template <int N> __device__ __forceinline__ void join_sums(f32x16 (&acc)[N], lds_char *mem, int wave) {
+  __attribute__((address_space(3))) float *other = (__attribute__((address_space(3))) float *)mem + wave % 4 * N * 16 * 64 + lane();
+  phase();
+  if (wave >= 4)
+#pragma unroll
+    for (int d = 0; d < N; d++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) other[(d * 16 + r) * 64] = acc[d][r];
+  phase();
+  if (wave < 4)
+#pragma unroll
+    for (int d = 0; d < N; d++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) acc[d][r] += other[(d * 16 + r) * 64];
+}
+
+/* LDS of the backward pass: per team three tiles each of two streams (a tile is read in two steps), the numbers of a tile's 32 queries
+ * (lse, delta, begin, end); the join needs the first two streams' worth. */
+template <int DP> struct GradLds {
+  static constexpr int TILE = GT * DP * 2, NUMBERS = 4 * GT * 4, TEAM_BYTES = 6 * TILE + 3 * NUMBERS, BYTES = 2 * TEAM_BYTES;
+  static_assert(BYTES >= 4 * DP / 2 * 64 * 4, "the join");
+};
+
+/* dq: as in the forward pass a wave has 32 queries, one a lane pair; dp^T = v do^T beside s^T = k q^T, and dq^T += k^T ds^T of the tile before. */
+template <class E, int DP, int KIND> __device__ __forceinline__ void attention_dq(const Attention &a, lds_char *mem, int (*part)[2], int id) {
+  using R = Rows<DP, GT>;
+  constexpr int TILE = R::BYTES;
+  int wave = uniform(threadIdx.x / 64), team = wave / 4, l = lane(), half = l >> 5;
+  lds_char *lds = mem + team * GradLds<DP>::TEAM_BYTES; /* three tiles of keys, three of values */
   int tile, h, b;
-  place(a.H, a.B, tile, h, b);
+  place(a.H, a.B, id, tile, h, b);
   tile = (a.Sq + ROWS - 1) / ROWS - 1 - tile;
   int g = h / (a.H / a.G);
-  int wave = uniform(threadIdx.x / 64), l = lane(), half = l >> 5;
-  int i = tile * ROWS + wave * 32 + (l & 31), offset = a.Sk - a.Sq;
+  int i = tile * ROWS + wave % 4 * 32 + (l & 31), offset = a.Sk - a.Sq;
   int begin, end;
   key_range(a, b, i, begin, end);
   int wlo = wave_min(begin), whi = wave_max(end), full_lo = wave_max(begin), full_hi = wave_min(end);
   int lo = wlo, hi = whi;
   join_ranges(lo, hi, part);
+  int first = lo / GT, tiles = lo < hi ? (hi + GT - 1) / GT - first : 0, steps = (tiles + 1) / 2;
 
   typename Vec<E>::v8 q[DP / 16], dout[DP / 16];
   row_fragments<E, DP>(a.q, b * a.q.batch + h * a.q.head, i, begin < end, a.D, q);
@@ -379,70 +474,102 @@ template <class E, int DP, int KIND> __global__ __launch_bounds__(WAVES * 64, 2)
   rk.init(a.k.row, a.D);
   rv.init(a.v.row, a.D);
   const char *pk = a.k.p + b * a.k.batch + g * a.k.head, *pv = a.v.p + b * a.v.batch + g * a.v.head;
-  int first = lo / KT, last = lo < hi ? (hi + KT - 1) / KT : first;
-  if (first < last) {
-    rk.load(pk, a.k.row, lds, first * KT, lo, hi);
-    rv.load(pv, a.v.row, lds + R::BYTES, first * KT, lo, hi);
-  }
-  auto step = [&](int t, auto which) {
-    constexpr int K = decltype(which)::value * 2 * R::BYTES, V = K + R::BYTES, NEXT = 2 * R::BYTES - K;
-    wait_barrier();
-    if (t + 1 < last) {
-      rk.load(pk, a.k.row, lds + NEXT, (t + 1) * KT, lo, hi);
-      rv.load(pv, a.v.row, lds + NEXT + R::BYTES, (t + 1) * KT, lo, hi);
-    }
-    int j0 = t * KT, j1 = j0 + 4 * half;
-    if (j0 >= whi || j0 + KT <= wlo) return;
-    bool all = j0 >= full_lo && j0 + KT <= full_hi;
+  auto key0 = [&](int n) __attribute__((always_inline)) { return (first + 2 * n + team) * GT; };
+  auto load = [&](int n, int which) __attribute__((always_inline)) {
+    rk.load(pk, a.k.row, lds + which * TILE, key0(n), lo, hi);
+    rv.load(pv, a.v.row, lds + (3 + which) * TILE, key0(n), lo, hi);
+  };
+  f32x16 s, dp;
+  typename Vec<E>::v8 ds[2]; /* of the step before */
+  auto scores = [&](int K, int V) __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < 2; x++) {
-      f32x16 s, dp;
+    for (int r = 0; r < 16; r++) s[r] = dp[r] = 0;
 #pragma unroll
-      for (int r = 0; r < 16; r++) s[r] = dp[r] = 0;
-#pragma unroll
-      for (int d = 0; d < DP / 16; d++) {
-        s = mfma(at.straight(lds, K, 32 * x, d), q[d], s);
-        dp = mfma(at.straight(lds, V, 32 * x, d), dout[d], dp);
-      }
-      float ds[16];
-#pragma unroll
-      for (int r = 0; r < 16; r++) {
-        float p;
-        pair<KIND>(a, slope2, i + offset - (j1 + 32 * x + 8 * (r >> 2) + (r & 3)), lse2, delta, s[r], dp[r], p, ds[r]);
-      }
-      if (!all) {
-#pragma unroll
-        for (int r = 0; r < 16; r++) {
-          int j = j1 + 32 * x + 8 * (r >> 2) + (r & 3);
-          ds[r] = j >= begin && j < end ? ds[r] : 0.f;
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 2; k++) {
-        typename Vec<E>::v8 w = round8<E>(ds + 8 * k);
-#pragma unroll
-        for (int d = 0; d < DP / 32; d++) acc[d] = mfma(at.transposed(lds, K, 32 * x + 16 * k, d), w, acc[d]);
-      }
+    for (int d = 0; d < DP / 16; d++) {
+      s = mfma(at.straight(lds, K, 0, d), q[d], s);
+      dp = mfma(at.straight(lds, V, 0, d), dout[d], dp);
     }
   };
-  for (int t = first; t < last; t += 2) {
-    step(t, Int<0>());
-    if (t + 1 < last) step(t + 1, Int<1>());
+  auto sums = [&](int K) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int d = 0; d < DP / 32; d++) acc[d] = mfma(at.transposed(lds, K, 16 * x, d), ds[x], acc[d]);
+  };
+  auto exponentials = [&](int n) __attribute__((always_inline)) {
+    int j0 = key0(n), j1 = j0 + 4 * half;
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+      float p, d;
+      pair<KIND>(a, slope2, i + offset - (j1 + 8 * (r >> 2) + (r & 3)), lse2, delta, s[r], dp[r], p, d);
+      dp[r] = d;
+    }
+    if (j0 < full_lo || j0 + GT > full_hi) {
+#pragma unroll
+      for (int r = 0; r < 16; r++) {
+        int j = j1 + 8 * (r >> 2) + (r & 3);
+        dp[r] = j >= begin && j < end ? dp[r] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; r++) ds[r / 8][r % 8] = (E)dp[r];
+  };
+  load(0, 0);
+  load(1, 1);
+  landed<2 * R::LOADS>();
+  phase();
+  if (team) phase();
+  auto step = [&](int n, auto which, auto begun) __attribute__((always_inline)) {
+    constexpr int W = decltype(which)::value;
+    __builtin_amdgcn_s_setprio(1);
+    if (begun.value) sums((W + 2) % 3 * TILE);
+    scores(W * TILE, (3 + W) * TILE);
+    __builtin_amdgcn_s_setprio(0);
+    phase();
+    load(n + 2, (W + 2) % 3);
+    exponentials(n);
+    landed<2 * R::LOADS>();
+    phase();
+  };
+  int n = 0;
+  if (steps) {
+    step(0, Int<0>(), Int<0>());
+    for (n = 1; n + 2 < steps; n += 3) {
+      step(n, Int<1>(), Int<1>());
+      step(n + 1, Int<2>(), Int<1>());
+      step(n + 2, Int<0>(), Int<1>());
+    }
+    if (n < steps) step(n++, Int<1>(), Int<1>());
+    if (n < steps) step(n++, Int<2>(), Int<1>());
+    sums((steps - 1) % 3 * TILE);
   }
-  if (i < a.Sq) store_column<E, DP>(acc, a.scale, (char *)a.dq.p + b * a.dq.batch + h * a.dq.head + i * a.dq.row, a.D);
+  if (!team) phase();
+  landed<0>();
+  join_sums(acc, mem, wave);
+  if (!team && i < a.Sq) store_column<E, DP>(acc, a.scale, (char *)a.dq.p + b * a.dq.batch + h * a.dq.head + i * a.dq.row, a.D);
 }
 
-/* dk, dv: a wave has 32 keys, one a lane pair, and meets all queries that see them, of every head that shares them, 64 at a time:
- * s = q k^T and dp = do v^T (queries in the registers), then dv^T += do^T p and dk^T += q^T ds. */
-template <class E, int DP, int KIND> __global__ __launch_bounds__(WAVES * 64, DP == 128 ? 1 : 2) void k_attention_dkv(Attention a) {
-  using R = Rows<DP>;
-  __shared__ __attribute__((aligned(1024))) char mem[4 * R::BYTES + 2 * 4 * KT * 4];
-  constexpr int NUMBERS = 4 * R::BYTES; /* per buffer: lse, delta, begin, end of 64 queries */
-  lds_char *lds = (lds_char *)mem;
-  int tiles = (a.Sq + KT - 1) / KT, tile, g, b;
-  place(a.G, a.B, tile, g, b);
-  int wave = uniform(threadIdx.x / 64), l = lane(), half = l >> 5;
-  int k0 = tile * ROWS, w0 = k0 + wave * 32, j = w0 + (l & 31), offset = a.Sk - a.Sq, shared = a.H / a.G;
+/* dk, dv: a wave has 32 keys, one a lane pair, and meets the queries of every head that shares them, 32 at a time: s = q k^T and
+ * dp = do v^T (queries in the registers), and dv^T += do^T p, dk^T += q^T ds of the tile before.  The tiles are those between the first and
+ * the last that see any of the workgroup's keys. */
+template <class E, int DP, int KIND> __device__ __forceinline__ void attention_dkv(const Attention &a, lds_char *mem, int (*part)[2], int id) {
+  using R = Rows<DP, GT>;
+  constexpr int TILE = R::BYTES, NUMBERS = GradLds<DP>::NUMBERS;
+  int wave = uniform(threadIdx.x / 64), team = wave / 4, l = lane(), half = l >> 5;
+  lds_char *lds = mem + team * GradLds<DP>::TEAM_BYTES; /* three tiles of q, three of do, three times the numbers */
+  int tiles = (a.Sq + GT - 1) / GT, tile, g, b;
+  place(a.G, a.B, id, tile, g, b);
+  int k0 = tile * ROWS, w0 = k0 + wave % 4 * 32, j = w0 + (l & 31), offset = a.Sk - a.Sq, shared = a.H / a.G;
+
+  const int4 *ranges = a.ranges + (int64_t)b * tiles;
+  int lo = FAR, hi = 0;
+  for (int t = threadIdx.x % TEAM; t < tiles; t += TEAM) {
+    int4 r = ranges[t];
+    if (r.x < k0 + ROWS && r.y > k0) lo = min(lo, t), hi = t + 1;
+  }
+  lo = wave_min(lo), hi = wave_max(hi);
+  join_ranges(lo, hi, part);
+  int per = lo < hi ? hi - lo : 0, total = per * shared, steps = (total + 1) / 2;
 
   typename Vec<E>::v8 k[DP / 16], v[DP / 16];
   row_fragments<E, DP>(a.k, b * a.k.batch + g * a.k.head, j, j < a.Sk, a.D, k);
@@ -456,108 +583,146 @@ template <class E, int DP, int KIND> __global__ __launch_bounds__(WAVES * 64, DP
   rq.init(a.q.row, a.D);
   rd.init(a.dout.row, a.D);
 
-  /* (head of the group, tile of queries) pairs in order, those that see none of the workgroup's keys left out */
-  const int4 *ranges = a.ranges + (int64_t)b * tiles;
-  int head = 0, qt = -1; /* the pair that is loaded next */
-  auto next = [&] {
-    for (qt++; head < shared; head++, qt = 0)
-      for (; qt < tiles; qt++) {
-        int4 r = ranges[qt];
-        if (r.x < k0 + ROWS && r.y > k0) return;
-      }
+  /* a team's tiles: every other one of those of the first head, then of the next */
+  struct Tile { int head, t; };
+  auto advance = [&](Tile &x) __attribute__((always_inline)) {
+    for (x.t += 2; per && x.t >= hi; x.head++) x.t -= per;
   };
-  auto ask = [&](int which) { /* rows that see nothing are zeros, whatever they hold */
-    int h = g * shared + head, i0 = qt * KT;
-    lds_char *to = lds + which * 2 * R::BYTES;
+  Tile ahead = {0, lo + team}; /* the one that is loaded next */
+  if (per && ahead.t >= hi) ahead.t -= per, ahead.head++;
+  Tile now = ahead;
+  auto load = [&](int which) __attribute__((always_inline)) { /* rows that see nothing are zeros, whatever they hold; past the last head too */
+    bool there = ahead.head < shared && per;
+    int h = g * shared + (there ? ahead.head : 0), i0 = there ? ahead.t * GT : 0, most = there ? a.Sq : 0;
     const char *pq = a.q.p + b * a.q.batch + h * a.q.head, *pd = a.dout.p + b * a.dout.batch + h * a.dout.head;
-    if (ranges[qt].z == FAR) { /* some row of the tile sees nothing, or there is none */
+    lds_char *tq = lds + which * TILE, *td = lds + (3 + which) * TILE;
+    if (there && ranges[ahead.t].z == FAR) { /* some row of the tile sees nothing, or there is none */
       auto in = [&](int i) {
-        int lo, hi;
-        key_range(a, b, i, lo, hi);
-        return lo < hi;
+        int from, to;
+        key_range(a, b, i, from, to);
+        return from < to;
       };
-      rq.load(pq, a.q.row, to, i0, in);
-      rd.load(pd, a.dout.row, to + R::BYTES, i0, in);
+      rq.load(pq, a.q.row, tq, i0, in);
+      rd.load(pd, a.dout.row, td, i0, in);
     } else {
-      rq.load(pq, a.q.row, to, i0, 0, a.Sq);
-      rd.load(pd, a.dout.row, to + R::BYTES, i0, 0, a.Sq);
+      rq.load(pq, a.q.row, tq, i0, 0, most);
+      rd.load(pd, a.dout.row, td, i0, 0, most);
     }
-    /* a wave each for the rows' numbers; past the last row: zeros */
+    /* a wave each for the rows' numbers */
     int64_t row = ((int64_t)b * a.H + h) * a.Sq + i0, at = (int64_t)b * a.Sq + i0;
-    const void *from = wave == 0 ? (const void *)(a.lse2 + row) : wave == 1 ? (const void *)(a.delta + row) : wave == 2 ? (const void *)(a.begin + at) : (const void *)(a.end + at);
-    if (wave < 2 || (wave == 2 ? a.begin : a.end)) load_lds4(buffer(from), lds + NUMBERS + (which * 4 + wave) * KT * 4, i0 + l < a.Sq ? l * 4 : OOB_LAYER_OUT);
+    int w = wave % 4;
+    const void *from = w == 0 ? (const void *)(a.lse2 + row) : w == 1 ? (const void *)(a.delta + row) : w == 2 ? (const void *)(a.begin + at) : (const void *)(a.end + at);
+    bool in = (w < 2 || (w == 2 ? a.begin : a.end)) && l < GT && i0 + l < most;
+    if (l < GT) load_lds4(buffer(from), lds + 6 * TILE + which * NUMBERS + w * GT * 4, in ? l * 4 : OOB_LAYER_OUT);
+    advance(ahead);
   };
-  next();
-  if (head < shared) ask(0);
-  auto step = [&](auto which) {
-    constexpr int B = decltype(which)::value, Q = B * 2 * R::BYTES, D = Q + R::BYTES, N = NUMBERS + B * 4 * KT * 4;
-    int i0 = qt * KT;
-    int4 range = ranges[qt];
-    float slope2 = KIND & BIAS ? a.slopes[g * shared + head] * LOG2E : 0.f;
-    wait_barrier();
-    next();
-    if (head < shared) ask(B ^ 1);
-    if (w0 >= range.y || w0 + 32 <= range.x) return;
-    bool all = w0 >= range.z && w0 + 32 <= range.w;
+  constexpr int LOADS = 2 * R::LOADS + 1;
+
+  f32x16 s, dp;
+  typename Vec<E>::v8 wp[2], ws[2]; /* of the step before */
+  auto scores = [&](int Q, int D) __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < 2; x++) {
-      at.fresh();
-      f32x16 s, dp;
+    for (int r = 0; r < 16; r++) s[r] = dp[r] = 0;
 #pragma unroll
-      for (int r = 0; r < 16; r++) s[r] = dp[r] = 0;
+    for (int d = 0; d < DP / 16; d++) {
+      s = mfma(at.straight(lds, Q, 0, d), k[d], s);
+      dp = mfma(at.straight(lds, D, 0, d), v[d], dp);
+    }
+  };
+  auto sums = [&](int Q) __attribute__((always_inline)) {
 #pragma unroll
-      for (int d = 0; d < DP / 16; d++) {
-        s = mfma(at.straight(lds, Q, 32 * x, d), k[d], s);
-        dp = mfma(at.straight(lds, D, 32 * x, d), v[d], dp);
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int d = 0; d < DP / 32; d++) {
+        dv[d] = mfma(at.transposed(lds, Q + 3 * TILE, 16 * x, d), wp[x], dv[d]);
+        dk[d] = mfma(at.transposed(lds, Q, 16 * x, d), ws[x], dk[d]);
       }
+  };
+  auto exponentials = [&](int N) __attribute__((always_inline)) {
+    bool there = now.head < shared && per; /* a team may have a tile less than the other */
+    int4 range = make_int4(0, 0, FAR, 0);
+    if (there) range = ranges[now.t];
+    int i0 = now.t * GT;
+    float slope2 = 0;
+    if (KIND & BIAS) slope2 = a.slopes[g * shared + (there ? now.head : 0)] * LOG2E;
+#pragma unroll
+    for (int n = 0; n < 4; n++) {
+      int row = 8 * n;
+      f32x4 lse = lds_numbers<f32x4>(lds + 16 * half + (N + row * 4)), delta = lds_numbers<f32x4>(lds + 16 * half + (N + GT * 4 + row * 4));
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        float p, d;
+        pair<KIND>(a, slope2, i0 + row + 4 * half + e + offset - j, lse[e], delta[e], s[4 * n + e], dp[4 * n + e], p, d);
+        s[4 * n + e] = p, dp[4 * n + e] = d;
+      }
+    }
+    if (w0 < range.z || w0 + 32 > range.w) {
 #pragma unroll
       for (int n = 0; n < 4; n++) {
-        int row = 32 * x + 8 * n;
-        f32x4 lse = lds_numbers<f32x4>(lds + 16 * half + (N + row * 4)), delta = lds_numbers<f32x4>(lds + 16 * half + (N + KT * 4 + row * 4));
+        int row = 8 * n;
+        i32x4 from = {0, 0, 0, 0}, to = {a.Sk, a.Sk, a.Sk, a.Sk};
+        if (a.begin) from = lds_numbers<i32x4>(lds + 16 * half + (N + 2 * GT * 4 + row * 4));
+        if (a.end) to = lds_numbers<i32x4>(lds + 16 * half + (N + 3 * GT * 4 + row * 4));
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          float p, ds;
-          pair<KIND>(a, slope2, i0 + row + 4 * half + e + offset - j, lse[e], delta[e], s[4 * n + e], dp[4 * n + e], p, ds);
-          s[4 * n + e] = p, dp[4 * n + e] = ds;
-        }
-      }
-      if (!all) {
-#pragma unroll
-        for (int n = 0; n < 4; n++) {
-          int row = 32 * x + 8 * n;
-          i32x4 lo = {0, 0, 0, 0}, hi = {a.Sk, a.Sk, a.Sk, a.Sk};
-          if (a.begin) lo = lds_numbers<i32x4>(lds + 16 * half + (N + 2 * KT * 4 + row * 4));
-          if (a.end) hi = lds_numbers<i32x4>(lds + 16 * half + (N + 3 * KT * 4 + row * 4));
-#pragma unroll
-          for (int e = 0; e < 4; e++) {
-            int i = i0 + row + 4 * half + e;
-            bool seen = j >= lo[e] && j < hi[e] && i < a.Sq && (!a.causal || j - offset <= i);
-            s[4 * n + e] = seen ? s[4 * n + e] : 0.f;
-            dp[4 * n + e] = seen ? dp[4 * n + e] : 0.f;
-          }
-        }
-      }
-#pragma unroll
-      for (int m = 0; m < 2; m++) {
-        typename Vec<E>::v8 wp, ws;
-#pragma unroll
-        for (int e = 0; e < 8; e++) wp[e] = (E)s[8 * m + e], ws[e] = (E)dp[8 * m + e];
-#pragma unroll
-        for (int d = 0; d < DP / 32; d++) {
-          dv[d] = mfma(at.transposed(lds, D, 32 * x + 16 * m, d), wp, dv[d]);
-          dk[d] = mfma(at.transposed(lds, Q, 32 * x + 16 * m, d), ws, dk[d]);
+          int i = i0 + row + 4 * half + e;
+          bool seen = there && j >= from[e] && j < to[e] && i < a.Sq && (!a.causal || j - offset <= i);
+          s[4 * n + e] = seen ? s[4 * n + e] : 0.f;
+          dp[4 * n + e] = seen ? dp[4 * n + e] : 0.f;
         }
       }
     }
+#pragma unroll
+    for (int r = 0; r < 16; r++) wp[r / 8][r % 8] = (E)s[r], ws[r / 8][r % 8] = (E)dp[r];
+    advance(now);
   };
-  while (head < shared) {
-    step(Int<0>());
-    if (head < shared) step(Int<1>());
+  load(0);
+  load(1);
+  landed<LOADS>();
+  phase();
+  if (team) phase();
+  auto step = [&](int n, auto which, auto begun) __attribute__((always_inline)) {
+    constexpr int W = decltype(which)::value;
+    __builtin_amdgcn_s_setprio(1);
+    at.fresh();
+    if (begun.value) sums((W + 2) % 3 * TILE);
+    __builtin_amdgcn_sched_barrier(0);
+    scores(W * TILE, (3 + W) * TILE);
+    __builtin_amdgcn_s_setprio(0);
+    phase();
+    load((W + 2) % 3);
+    exponentials(6 * TILE + W * NUMBERS);
+    landed<LOADS>();
+    phase();
+  };
+  int n = 0;
+  if (steps) {
+    step(0, Int<0>(), Int<0>());
+    for (n = 1; n + 2 < steps; n += 3) {
+      step(n, Int<1>(), Int<1>());
+      step(n + 1, Int<2>(), Int<1>());
+      step(n + 2, Int<0>(), Int<1>());
+    }
+    if (n < steps) step(n++, Int<1>(), Int<1>());
+    if (n < steps) step(n++, Int<2>(), Int<1>());
+    sums((steps - 1) % 3 * TILE);
   }
-  if (j < a.Sk) {
+  if (!team) phase();
+  landed<0>();
+  join_sums(dk, mem, wave);
+  join_sums(dv, mem, wave);
+  if (!team && j < a.Sk) {
     store_column<E, DP>(dk, a.scale, (char *)a.dk.p + b * a.dk.batch + g * a.dk.head + j * a.dk.row, a.D);
     store_column<E, DP>(dv, 1.f, (char *)a.dv.p + b * a.dv.batch + g * a.dv.head + j * a.dv.row, a.D);
   }
+}
+
+/* Both in one launch: the tiles of keys first, then those of queries fill up what the last of them leave idle. */
+template <class E, int DP, int KIND> __global__ __launch_bounds__(THREADS, 2) void k_attention_grad(Attention a, int of_keys) {
+  __shared__ __attribute__((aligned(1024))) char mem[GradLds<DP>::BYTES];
+  __shared__ int part[8][2];
+  if ((int)blockIdx.x < of_keys) attention_dkv<E, DP, KIND>(a, (lds_char *)mem, part, blockIdx.x);
+  else attention_dq<E, DP, KIND>(a, (lds_char *)mem, part, blockIdx.x - of_keys);
 }
 
 /* ---- heads that the loads cannot take (rows that do not start at 16 bytes, a width that is no multiple of 8) go to the workspace ---- */
@@ -637,8 +802,8 @@ template <class E> static int forward(const oob_attention *p, Arena w, hipStream
   if (n) {
     by_kind(a, [&](auto kind) {
       constexpr int KIND = decltype(kind)::value;
-      if (a.D <= 64) k_attention<E, 64, KIND><<<n, WAVES * 64, 0, st>>>(a);
-      else k_attention<E, 128, KIND><<<n, WAVES * 64, 0, st>>>(a);
+      if (a.D <= 64) k_attention<E, 64, KIND><<<n, THREADS, 0, st>>>(a);
+      else k_attention<E, 128, KIND><<<n, THREADS, 0, st>>>(a);
     });
   }
   return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
@@ -648,7 +813,7 @@ static size_t backward_bytes(const oob_attention *p, const oob_attention_grad *q
   Attention a = attention_of(p);
   Arena w{nullptr, 0, 0};
   w.take((size_t)a.B * a.H * a.Sq * 8);
-  w.take((size_t)a.B * ((a.Sq + KT - 1) / KT) * sizeof(int4));
+  w.take((size_t)a.B * ((a.Sq + GT - 1) / GT) * sizeof(int4));
   for (const Heads &h : {a.k, a.v})
     if (!loadable(h, a.D)) w.take(packed_bytes(a.B, a.Sk, a.G, a.D));
   for (const Heads &h : {a.q, heads_of(q->dout, q->dout_stride)})
@@ -662,12 +827,12 @@ template <class E> static int backward(const oob_attention *p, const oob_attenti
   a.dq = heads_of(q->dq, q->dq_stride), a.dk = heads_of(q->dk, q->dk_stride), a.dv = heads_of(q->dv, q->dv_stride);
   int64_t rows = (int64_t)a.B * a.H * a.Sq;
   float *lse2 = (float *)w.take((size_t)rows * 8), *delta = lse2 + rows;
-  int4 *ranges = (int4 *)w.take((size_t)a.B * ((a.Sq + KT - 1) / KT) * sizeof(int4));
+  int4 *ranges = (int4 *)w.take((size_t)a.B * ((a.Sq + GT - 1) / GT) * sizeof(int4));
   a.lse2 = lse2, a.delta = delta, a.ranges = ranges;
   if (!w.ok()) return OOB_ECAPACITY;
   if (rows) {
     k_delta<E><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>(a, lse2, delta);
-    k_ranges<<<(unsigned)(a.B * ((a.Sq + KT - 1) / KT)), 64, 0, st>>>(a, ranges);
+    k_ranges<<<(unsigned)(a.B * (((a.Sq + GT - 1) / GT + 1) / 2)), 64, 0, st>>>(a, ranges);
   }
   pack(a.k, a.B, a.Sk, a.G, a.D, w, st);
   pack(a.v, a.B, a.Sk, a.G, a.D, w, st);
@@ -677,10 +842,8 @@ template <class E> static int backward(const oob_attention *p, const oob_attenti
   unsigned nq = (unsigned)((int64_t)a.B * a.H * ((a.Sq + ROWS - 1) / ROWS)), nk = (unsigned)((int64_t)a.B * a.G * ((a.Sk + ROWS - 1) / ROWS));
   by_kind(a, [&](auto kind) {
     constexpr int KIND = decltype(kind)::value;
-    if (nk && a.D <= 64) k_attention_dkv<E, 64, KIND><<<nk, WAVES * 64, 0, st>>>(a);
-    else if (nk) k_attention_dkv<E, 128, KIND><<<nk, WAVES * 64, 0, st>>>(a);
-    if (nq && a.D <= 64) k_attention_dq<E, 64, KIND><<<nq, WAVES * 64, 0, st>>>(a);
-    else if (nq) k_attention_dq<E, 128, KIND><<<nq, WAVES * 64, 0, st>>>(a);
+    if (nk + nq && a.D <= 64) k_attention_grad<E, 64, KIND><<<nk + nq, THREADS, 0, st>>>(a, (int)nk);
+    else if (nk + nq) k_attention_grad<E, 128, KIND><<<nk + nq, THREADS, 0, st>>>(a, (int)nk);
   });
   return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
 }
