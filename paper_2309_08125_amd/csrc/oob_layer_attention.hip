@@ -18,7 +18,7 @@ struct Attention {
   /* backward */
   Heads dout, dq, dk, dv;
   const float *lse2, *delta; /* [B][H][Sq]: lse log2 e (0 where there is none), do . o */
-  const int4 *ranges;  /* [B][tiles of 32 queries]: smallest begin, largest end, largest begin, smallest end */
+  const int4 *ranges;  /* [B][tiles of grad_tile queries]: smallest begin, largest end, largest begin, smallest end */
 };
 
 /* A workgroup is two teams of four waves on the same 128 rows (queries; keys in dk, dv): 32 rows a wave, the other side's tiles dealt to
@@ -27,7 +27,7 @@ struct Attention {
  * one wave in either phase.  (Waves w and w + 4 share a SIMD.) */
 constexpr int TEAM = 256, THREADS = 2 * TEAM, ROWS = 128;
 constexpr int KT = 64; /* keys of a tile in the forward pass */
-constexpr int GT = 32; /* rows of a tile in the backward pass */
+constexpr int grad_tile(int DP) { return DP == 64 ? 64 : 32; } /* rows of a tile in the backward pass: what its products leave registers for */
 constexpr float LOG2E = 1.44269504f, LN2 = 0.69314718f;
 constexpr int FAR = 0x3fffffff; /* the begin of a row that sees nothing */
 
@@ -63,7 +63,8 @@ template <int DP, int N> struct Rows {
   }
   /* rows lo <= first + r < hi; zeros for the others */
   __device__ void load(const char *base, int64_t stride, lds_char *to, int first, int lo, int hi) {
-    load(base, stride, to, first, [&](int at) { return at >= lo && at < hi; });
+    if (first >= lo && first + N <= hi) load(base, stride, to, first, [](int) { return true; });
+    else load(base, stride, to, first, [&](int at) { return at >= lo && at < hi; });
   }
   template <class F> __device__ void load(const char *base, int64_t stride, lds_char *to, int first, F in) {
     __amdgpu_buffer_rsrc_t r = buffer(base + first * stride);
@@ -213,7 +214,7 @@ __device__ inline void place(int heads, int B, int id, int &tile, int &head, int
  * A wave has 32 queries, one a lane pair: scores are formed transposed (keys in the registers, the query in the lane), so that a
  * query's running maximum and sum are its lane's own and the exponentials are, as they lie, the second operand of o^T += v^T p^T.
  * A step's products are the scores of its tile and o^T of the tile before. */
-template <class E, int DP, int KIND> __global__ __launch_bounds__(THREADS, DP == 64 ? 4 : 2) void k_attention(Attention a) {
+template <class E, int DP, int KIND> __global__ __launch_bounds__(THREADS, 2) void k_attention(Attention a) {
   using R = Rows<DP, KT>;
   __shared__ __attribute__((aligned(1024))) char mem[8 * R::BYTES];
   __shared__ int part[8][2];
@@ -323,10 +324,22 @@ template <class E, int DP, int KIND> __global__ __launch_bounds__(THREADS, DP ==
   if (team) phase();
   auto step = [&](int n, auto which, auto begun) __attribute__((always_inline)) {
     constexpr int W = decltype(which)::value;
-    __builtin_amdgcn_s_setprio(1);
     scores(W * R::BYTES);
     if (begun.value) outputs((3 - W) * R::BYTES);
-    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int g = 0; g < DP / 8 - 4; g++) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    if (begun.value) {
+#pragma unroll
+      for (int g = 0; g < DP / 8; g++) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, 4, 0);
+    }
     phase();
     load_k(n + 2, W);
     load_v(n + 1, W ^ 1);
@@ -392,16 +405,16 @@ template <class E> __global__ __launch_bounds__(256) void k_delta(Attention a, f
   }
 }
 
-__global__ __launch_bounds__(64) void k_ranges(Attention a, int4 *ranges) { /* two tiles a wave, one a half */
-  int tiles = (a.Sq + GT - 1) / GT, pairs = (tiles + 1) / 2, b = blockIdx.x / pairs, t = blockIdx.x % pairs * 2 + lane() / 32;
+__global__ __launch_bounds__(64) void k_ranges(Attention a, int4 *ranges, int rows) { /* tiles of 32 or 64 rows: two or one a wave */
+  int tiles = (a.Sq + rows - 1) / rows, per = 64 / rows, groups = (tiles + per - 1) / per, b = blockIdx.x / groups, t = blockIdx.x % groups * per + lane() / rows;
   int begin, end;
-  key_range(a, b, t * GT + lane() % 32, begin, end);
+  key_range(a, b, t * rows + lane() % rows, begin, end);
   int4 r = make_int4(begin, end, begin, end);
-  for (int k = 16; k > 0; k >>= 1) {
+  for (int k = rows / 2; k > 0; k >>= 1) {
     r.x = min(r.x, __shfl_xor(r.x, k)), r.y = max(r.y, __shfl_xor(r.y, k));
     r.z = max(r.z, __shfl_xor(r.z, k)), r.w = min(r.w, __shfl_xor(r.w, k));
   }
-  if (lane() % 32 == 0 && t < tiles) ranges[(int64_t)b * tiles + t] = r;
+  if (lane() % rows == 0 && t < tiles) ranges[(int64_t)b * tiles + t] = r;
 }
 
 /* What a pair (query, key) gives: p = e^(s - lse) and ds = p (dp - delta) ds/draw but for the scale, which the sums
@@ -430,15 +443,16 @@ template <int N> __device__ __forceinline__ void join_sums(f32x16 (&acc)[N], lds
       for (int r = 0; r < 16; r++) acc[d][r] += other[(d * 16 + r) * 64];
 }
 
-/* LDS of the backward pass: per team three tiles each of two streams (a tile is read in two steps), the numbers of a tile's 32 queries
+/* LDS of the backward pass: per team three tiles each of two streams (a tile is read in two steps), the numbers of a tile's queries
  * (lse, delta, begin, end); the join needs the first two streams' worth. */
 template <int DP> struct GradLds {
-  static constexpr int TILE = GT * DP * 2, NUMBERS = 4 * GT * 4, TEAM_BYTES = 6 * TILE + 3 * NUMBERS, BYTES = 2 * TEAM_BYTES;
+  static constexpr int GT = grad_tile(DP), TILE = GT * DP * 2, NUMBERS = 4 * GT * 4, TEAM_BYTES = 6 * TILE + 3 * NUMBERS, BYTES = 2 * TEAM_BYTES;
   static_assert(BYTES >= 4 * DP / 2 * 64 * 4, "the join");
 };
 
 /* dq: as in the forward pass a wave has 32 queries, one a lane pair; dp^T = v do^T beside s^T = k q^T, and dq^T += k^T ds^T of the tile before. */
 template <class E, int DP, int KIND> __device__ __forceinline__ void attention_dq(const Attention &a, lds_char *mem, int (*part)[2], int id) {
+  constexpr int GT = grad_tile(DP), X = GT / 32;
   using R = Rows<DP, GT>;
   constexpr int TILE = R::BYTES;
   int wave = uniform(threadIdx.x / 64), team = wave / 4, l = lane(), half = l >> 5;
@@ -479,40 +493,47 @@ template <class E, int DP, int KIND> __device__ __forceinline__ void attention_d
     rk.load(pk, a.k.row, lds + which * TILE, key0(n), lo, hi);
     rv.load(pv, a.v.row, lds + (3 + which) * TILE, key0(n), lo, hi);
   };
-  f32x16 s, dp;
-  typename Vec<E>::v8 ds[2]; /* of the step before */
+  f32x16 s[X], dp[X];
+  typename Vec<E>::v8 ds[2 * X]; /* of the step before */
   auto scores = [&](int K, int V) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < 16; r++) s[r] = dp[r] = 0;
+    for (int x = 0; x < X; x++) {
 #pragma unroll
-    for (int d = 0; d < DP / 16; d++) {
-      s = mfma(at.straight(lds, K, 0, d), q[d], s);
-      dp = mfma(at.straight(lds, V, 0, d), dout[d], dp);
+      for (int r = 0; r < 16; r++) s[x][r] = dp[x][r] = 0;
+#pragma unroll
+      for (int d = 0; d < DP / 16; d++) {
+        s[x] = mfma(at.straight(lds, K, 32 * x, d), q[d], s[x]);
+        dp[x] = mfma(at.straight(lds, V, 32 * x, d), dout[d], dp[x]);
+      }
     }
   };
   auto sums = [&](int K) __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < 2; x++)
+    for (int x = 0; x < 2 * X; x++)
 #pragma unroll
       for (int d = 0; d < DP / 32; d++) acc[d] = mfma(at.transposed(lds, K, 16 * x, d), ds[x], acc[d]);
   };
   auto exponentials = [&](int n) __attribute__((always_inline)) {
     int j0 = key0(n), j1 = j0 + 4 * half;
+    bool all = j0 >= full_lo && j0 + GT <= full_hi;
 #pragma unroll
-    for (int r = 0; r < 16; r++) {
-      float p, d;
-      pair<KIND>(a, slope2, i + offset - (j1 + 8 * (r >> 2) + (r & 3)), lse2, delta, s[r], dp[r], p, d);
-      dp[r] = d;
-    }
-    if (j0 < full_lo || j0 + GT > full_hi) {
+    for (int x = 0; x < X; x++) {
 #pragma unroll
       for (int r = 0; r < 16; r++) {
-        int j = j1 + 8 * (r >> 2) + (r & 3);
-        dp[r] = j >= begin && j < end ? dp[r] : 0.f;
+        float p, d;
+        pair<KIND>(a, slope2, i + offset - (j1 + 32 * x + 8 * (r >> 2) + (r & 3)), lse2, delta, s[x][r], dp[x][r], p, d);
+        dp[x][r] = d;
       }
-    }
+      if (!all) {
 #pragma unroll
-    for (int r = 0; r < 16; r++) ds[r / 8][r % 8] = (E)dp[r];
+        for (int r = 0; r < 16; r++) {
+          int j = j1 + 32 * x + 8 * (r >> 2) + (r & 3);
+          dp[x][r] = j >= begin && j < end ? dp[x][r] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 16; r++) ds[2 * x + r / 8][r % 8] = (E)dp[x][r];
+    }
   };
   load(0, 0);
   load(1, 1);
@@ -521,10 +542,22 @@ template <class E, int DP, int KIND> __device__ __forceinline__ void attention_d
   if (team) phase();
   auto step = [&](int n, auto which, auto begun) __attribute__((always_inline)) {
     constexpr int W = decltype(which)::value;
-    __builtin_amdgcn_s_setprio(1);
     if (begun.value) sums((W + 2) % 3 * TILE);
     scores(W * TILE, (3 + W) * TILE);
-    __builtin_amdgcn_s_setprio(0);
+    if (begun.value) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int g = 0; g < X * DP / 16 - 2; g++) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+#pragma unroll
+      for (int g = 0; g < X * DP / 8; g++) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+    }
     phase();
     load(n + 2, (W + 2) % 3);
     exponentials(n);
@@ -549,10 +582,11 @@ template <class E, int DP, int KIND> __device__ __forceinline__ void attention_d
   if (!team && i < a.Sq) store_column<E, DP>(acc, a.scale, (char *)a.dq.p + b * a.dq.batch + h * a.dq.head + i * a.dq.row, a.D);
 }
 
-/* dk, dv: a wave has 32 keys, one a lane pair, and meets the queries of every head that shares them, 32 at a time: s = q k^T and
+/* dk, dv: a wave has 32 keys, one a lane pair, and meets the queries of every head that shares them, a tile at a time: s = q k^T and
  * dp = do v^T (queries in the registers), and dv^T += do^T p, dk^T += q^T ds of the tile before.  The tiles are those between the first and
  * the last that see any of the workgroup's keys. */
 template <class E, int DP, int KIND> __device__ __forceinline__ void attention_dkv(const Attention &a, lds_char *mem, int (*part)[2], int id) {
+  constexpr int GT = grad_tile(DP), X = GT / 32;
   using R = Rows<DP, GT>;
   constexpr int TILE = R::BYTES, NUMBERS = GradLds<DP>::NUMBERS;
   int wave = uniform(threadIdx.x / 64), team = wave / 4, l = lane(), half = l >> 5;
@@ -618,20 +652,23 @@ template <class E, int DP, int KIND> __device__ __forceinline__ void attention_d
   };
   constexpr int LOADS = 2 * R::LOADS + 1;
 
-  f32x16 s, dp;
-  typename Vec<E>::v8 wp[2], ws[2]; /* of the step before */
+  f32x16 s[X], dp[X];
+  typename Vec<E>::v8 wp[2 * X], ws[2 * X]; /* of the step before */
   auto scores = [&](int Q, int D) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < 16; r++) s[r] = dp[r] = 0;
+    for (int x = 0; x < X; x++) {
 #pragma unroll
-    for (int d = 0; d < DP / 16; d++) {
-      s = mfma(at.straight(lds, Q, 0, d), k[d], s);
-      dp = mfma(at.straight(lds, D, 0, d), v[d], dp);
+      for (int r = 0; r < 16; r++) s[x][r] = dp[x][r] = 0;
+#pragma unroll
+      for (int d = 0; d < DP / 16; d++) {
+        s[x] = mfma(at.straight(lds, Q, 32 * x, d), k[d], s[x]);
+        dp[x] = mfma(at.straight(lds, D, 32 * x, d), v[d], dp[x]);
+      }
     }
   };
   auto sums = [&](int Q) __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < 2; x++)
+    for (int x = 0; x < 2 * X; x++)
 #pragma unroll
       for (int d = 0; d < DP / 32; d++) {
         dv[d] = mfma(at.transposed(lds, Q + 3 * TILE, 16 * x, d), wp[x], dv[d]);
@@ -645,35 +682,39 @@ template <class E, int DP, int KIND> __device__ __forceinline__ void attention_d
     int i0 = now.t * GT;
     float slope2 = 0;
     if (KIND & BIAS) slope2 = a.slopes[g * shared + (there ? now.head : 0)] * LOG2E;
+    bool all = w0 >= range.z && w0 + 32 <= range.w;
 #pragma unroll
-    for (int n = 0; n < 4; n++) {
-      int row = 8 * n;
-      f32x4 lse = lds_numbers<f32x4>(lds + 16 * half + (N + row * 4)), delta = lds_numbers<f32x4>(lds + 16 * half + (N + GT * 4 + row * 4));
-#pragma unroll
-      for (int e = 0; e < 4; e++) {
-        float p, d;
-        pair<KIND>(a, slope2, i0 + row + 4 * half + e + offset - j, lse[e], delta[e], s[4 * n + e], dp[4 * n + e], p, d);
-        s[4 * n + e] = p, dp[4 * n + e] = d;
-      }
-    }
-    if (w0 < range.z || w0 + 32 > range.w) {
+    for (int x = 0; x < X; x++) {
 #pragma unroll
       for (int n = 0; n < 4; n++) {
-        int row = 8 * n;
-        i32x4 from = {0, 0, 0, 0}, to = {a.Sk, a.Sk, a.Sk, a.Sk};
-        if (a.begin) from = lds_numbers<i32x4>(lds + 16 * half + (N + 2 * GT * 4 + row * 4));
-        if (a.end) to = lds_numbers<i32x4>(lds + 16 * half + (N + 3 * GT * 4 + row * 4));
+        int row = 32 * x + 8 * n;
+        f32x4 lse = lds_numbers<f32x4>(lds + 16 * half + (N + row * 4)), delta = lds_numbers<f32x4>(lds + 16 * half + (N + GT * 4 + row * 4));
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          int i = i0 + row + 4 * half + e;
-          bool seen = there && j >= from[e] && j < to[e] && i < a.Sq && (!a.causal || j - offset <= i);
-          s[4 * n + e] = seen ? s[4 * n + e] : 0.f;
-          dp[4 * n + e] = seen ? dp[4 * n + e] : 0.f;
+          float p, d;
+          pair<KIND>(a, slope2, i0 + row + 4 * half + e + offset - j, lse[e], delta[e], s[x][4 * n + e], dp[x][4 * n + e], p, d);
+          s[x][4 * n + e] = p, dp[x][4 * n + e] = d;
         }
       }
-    }
+      if (!all) {
 #pragma unroll
-    for (int r = 0; r < 16; r++) wp[r / 8][r % 8] = (E)s[r], ws[r / 8][r % 8] = (E)dp[r];
+        for (int n = 0; n < 4; n++) {
+          int row = 32 * x + 8 * n;
+          i32x4 from = {0, 0, 0, 0}, to = {a.Sk, a.Sk, a.Sk, a.Sk};
+          if (a.begin) from = lds_numbers<i32x4>(lds + 16 * half + (N + 2 * GT * 4 + row * 4));
+          if (a.end) to = lds_numbers<i32x4>(lds + 16 * half + (N + 3 * GT * 4 + row * 4));
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            int i = i0 + row + 4 * half + e;
+            bool seen = there && j >= from[e] && j < to[e] && i < a.Sq && (!a.causal || j - offset <= i);
+            s[x][4 * n + e] = seen ? s[x][4 * n + e] : 0.f;
+            dp[x][4 * n + e] = seen ? dp[x][4 * n + e] : 0.f;
+          }
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 16; r++) wp[2 * x + r / 8][r % 8] = (E)s[x][r], ws[2 * x + r / 8][r % 8] = (E)dp[x][r];
+    }
     advance(now);
   };
   load(0);
@@ -683,12 +724,26 @@ template <class E, int DP, int KIND> __device__ __forceinline__ void attention_d
   if (team) phase();
   auto step = [&](int n, auto which, auto begun) __attribute__((always_inline)) {
     constexpr int W = decltype(which)::value;
-    __builtin_amdgcn_s_setprio(1);
     at.fresh();
     if (begun.value) sums((W + 2) % 3 * TILE);
+    if (begun.value) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int g = 0; g < X * DP / 8 - 2; g++) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+    }
     __builtin_amdgcn_sched_barrier(0);
     scores(W * TILE, (3 + W) * TILE);
-    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+    for (int g = 0; g < X * DP / 8 - 2; g++) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
     phase();
     load((W + 2) % 3);
     exponentials(6 * TILE + W * NUMBERS);
@@ -813,7 +868,7 @@ static size_t backward_bytes(const oob_attention *p, const oob_attention_grad *q
   Attention a = attention_of(p);
   Arena w{nullptr, 0, 0};
   w.take((size_t)a.B * a.H * a.Sq * 8);
-  w.take((size_t)a.B * ((a.Sq + GT - 1) / GT) * sizeof(int4));
+  w.take((size_t)a.B * ((a.Sq + 31) / 32) * sizeof(int4));
   for (const Heads &h : {a.k, a.v})
     if (!loadable(h, a.D)) w.take(packed_bytes(a.B, a.Sk, a.G, a.D));
   for (const Heads &h : {a.q, heads_of(q->dout, q->dout_stride)})
@@ -827,12 +882,12 @@ template <class E> static int backward(const oob_attention *p, const oob_attenti
   a.dq = heads_of(q->dq, q->dq_stride), a.dk = heads_of(q->dk, q->dk_stride), a.dv = heads_of(q->dv, q->dv_stride);
   int64_t rows = (int64_t)a.B * a.H * a.Sq;
   float *lse2 = (float *)w.take((size_t)rows * 8), *delta = lse2 + rows;
-  int4 *ranges = (int4 *)w.take((size_t)a.B * ((a.Sq + GT - 1) / GT) * sizeof(int4));
+  int4 *ranges = (int4 *)w.take((size_t)a.B * ((a.Sq + 31) / 32) * sizeof(int4));
   a.lse2 = lse2, a.delta = delta, a.ranges = ranges;
   if (!w.ok()) return OOB_ECAPACITY;
   if (rows) {
     k_delta<E><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>(a, lse2, delta);
-    k_ranges<<<(unsigned)(a.B * (((a.Sq + GT - 1) / GT + 1) / 2)), 64, 0, st>>>(a, ranges);
+    k_ranges<<<(unsigned)(a.B * ((a.Sq + 63) / 64)), 64, 0, st>>>(a, ranges, grad_tile(a.D <= 64 ? 64 : 128));
   }
   pack(a.k, a.B, a.Sk, a.G, a.D, w, st);
   pack(a.v, a.B, a.Sk, a.G, a.D, w, st);
