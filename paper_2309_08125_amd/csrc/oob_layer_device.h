@@ -78,14 +78,17 @@ __device__ inline int64_t xcd_order(int64_t id, int64_t n) {
 
 /* Eight consecutive values of a row, `left` of them in it.  Rows start anywhere: memory takes 16-byte accesses at any address. */
 template <class E> struct Loose { typedef typename Vec<E>::v8 v8 __attribute__((aligned(sizeof(E)))); };
-template <class E> __device__ inline typename Vec<E>::v8 load8(const E *p, int64_t left) {
-  if (left >= 8) return *(const typename Loose<E>::v8 *)p;
+#define OOB_GLOBAL __attribute__((address_space(1)))
+template <class E> __device__ inline typename Vec<E>::v8 load8(const E *from, int64_t left) {
+  const OOB_GLOBAL E *p = (const OOB_GLOBAL E *)from;
+  if (left >= 8) return *(const OOB_GLOBAL typename Loose<E>::v8 *)p;
   typename Vec<E>::v8 v;
   for (int e = 0; e < 8; e++) v[e] = e < left ? p[e] : (E)0.f;
   return v;
 }
-template <class E> __device__ inline void store8(E *p, typename Vec<E>::v8 v, int64_t left) {
-  if (left >= 8) *(typename Loose<E>::v8 *)p = v;
+template <class E> __device__ inline void store8(E *to, typename Vec<E>::v8 v, int64_t left) {
+  OOB_GLOBAL E *p = (OOB_GLOBAL E *)to;
+  if (left >= 8) *(OOB_GLOBAL typename Loose<E>::v8 *)p = v;
   else
     for (int e = 0; e < 8; e++)
       if (e < left) p[e] = v[e];

@@ -26,17 +26,18 @@ struct NormGrad {
 
 /* Sums of N values over the WAVES waves that share a row, in every lane. */
 template <int WAVES, int N> __device__ inline void sum_row(float (&v)[N], float *part, int &turn) {
+  static_assert(N <= 6, "places");
   for (int k = 32; k > 0; k >>= 1)
     for (int i = 0; i < N; i++) v[i] += __shfl_xor(v[i], k);
   if (WAVES == 1) return;
-  float *p = part + turn * WAVES * 2; /* two places in turn: a place is written again only behind a barrier that everybody passed after reading it */
+  float *p = part + turn * WAVES * 6; /* two places in turn: a place is written again only behind a barrier that everybody passed after reading it */
   turn ^= 1;
   if (lane() == 0)
-    for (int i = 0; i < N; i++) p[threadIdx.x / 64 * 2 + i] = v[i];
+    for (int i = 0; i < N; i++) p[threadIdx.x / 64 * 6 + i] = v[i];
   __syncthreads();
   for (int i = 0; i < N; i++) {
     float s = 0;
-    for (int k = 0; k < WAVES; k++) s += p[k * 2 + i];
+    for (int k = 0; k < WAVES; k++) s += p[k * 6 + i];
     v[i] = s;
   }
 }
@@ -72,7 +73,7 @@ template <class E> __device__ inline void narrow(const float (&f)[8], typename V
  * waves: rows of one wave go four at a time. */
 template <class E, int WAVES, int V> __global__ __launch_bounds__(WAVES < 4 ? 256 : WAVES * 64) void k_norm(Norm n) {
   constexpr int ROWS = WAVES == 1 ? 4 : 1;
-  __shared__ float part[WAVES * 4];
+  __shared__ float part[WAVES * 12];
   int turn = 0;
   int c0 = (WAVES == 1 ? lane() : threadIdx.x) * 8;
   const int64_t C = n.C;
@@ -142,7 +143,7 @@ template <class E, int WAVES, int V> __global__ __launch_bounds__(WAVES < 4 ? 25
  * and the norm behind the block the same way from zhat.  A workgroup takes a run of rows and keeps the sums of its columns in registers. */
 template <class E, int WAVES, int V, bool POST, bool GATE> __global__ __launch_bounds__(WAVES * 64) void k_norm_grad(NormGrad g) {
   const Norm &n = g.n;
-  __shared__ float part[WAVES * 4];
+  __shared__ float part[WAVES * 12];
   int turn = 0;
   int c0 = threadIdx.x * 8;
   const int64_t C = n.C;
@@ -163,31 +164,46 @@ template <class E, int WAVES, int V, bool POST, bool GATE> __global__ __launch_b
       if (g.dxp) vd[k] = load8<E>((const E *)g.dxp + t * g.ld_dxp + c, C - c);
       if (POST || GATE) vz[k] = load8<E>((const E *)n.z + t * n.ldz + c, C - c);
     }
-    float mean = n.pre == OOB_NORM_LAYER ? n.mean[t] : 0.f, rstd = n.rstd[t];
-    float d[V][8], s[2] = {0, 0};
+    /* The statistics are those of x' as it was stored, not of what it was before: with y = x' - (the forward pass's mean), the row's
+     * mean is that mean + sum(y) / C, and all that is needed are the sums of y, y^2, c and c y. */
+    float mean = n.pre == OOB_NORM_LAYER ? n.mean[t] : 0.f;
+    float pmean = POST && n.post == OOB_NORM_LAYER ? n.pmean[t] : 0.f;
+    float d[V][8], s[POST ? 6 : 4] = {};
     for (int k = 0; k < V; k++) {
       int64_t c = c0 + k * WAVES * 512;
       typename Vec<E>::v8 w;
       if (n.w) w = load8<E>((const E *)n.w + c, C - c);
       for (int e = 0; e < 8; e++) {
-        float xhat = ((float)vx[k][e] - mean) * rstd, dh = (float)vh[k][e];
-        dw[k][e] += dh * xhat;
-        db[k][e] += dh;
-        float v = dh * (n.w ? (float)w[e] : 1.f);
+        float y = c + e < C ? (float)vx[k][e] - mean : 0.f;
+        float v = (float)vh[k][e] * (n.w ? (float)w[e] : 1.f);
         d[k][e] = v;
-        s[0] += v;
-        s[1] += v * xhat;
+        s[0] += y;
+        s[1] += y * y;
+        s[2] += v;
+        s[3] += v * y;
+        if (POST) {
+          float z = c + e < C ? (float)vz[k][e] - pmean : 0.f;
+          s[4] += z;
+          s[5] += z * z;
+        }
       }
     }
-    sum_row<WAVES, 2>(s, part, turn);
-    float m0 = n.pre == OOB_NORM_LAYER ? s[0] / C : 0.f, m1 = s[1] / C;
-    float pmean = 0, prstd = 0, q[2] = {0, 0};
-    if (POST) pmean = n.post == OOB_NORM_LAYER ? n.pmean[t] : 0.f, prstd = n.prstd[t];
+    sum_row<WAVES, POST ? 6 : 4>(s, part, turn);
+    float shift = n.pre == OOB_NORM_LAYER ? s[0] / C : 0.f;
+    float rstd = 1 / sqrtf(fmaxf(s[1] / C - shift * shift, 0.f) + n.eps);
+    float m0 = n.pre == OOB_NORM_LAYER ? s[2] / C : 0.f, m1 = rstd * (s[3] - shift * s[2]) / C;
+    float pshift = 0, prstd = 0, q[2] = {0, 0}; /* the norm behind the block: its mean without the rounding to one number, as above */
+    if (POST) {
+      pshift = n.post == OOB_NORM_LAYER ? s[4] / C : 0.f;
+      prstd = 1 / sqrtf(fmaxf(s[5] / C - pshift * pshift, 0.f) + n.eps);
+    }
     for (int k = 0; k < V; k++) {
       int64_t c = c0 + k * WAVES * 512;
       typename Vec<E>::v8 out, gate, pw, pb;
       for (int e = 0; e < 8; e++) {
-        float xhat = ((float)vx[k][e] - mean) * rstd;
+        float xhat = (((float)vx[k][e] - mean) - shift) * rstd; /* not less the sum of both: it would round */
+        dw[k][e] += (float)vh[k][e] * xhat;
+        db[k][e] += (float)vh[k][e];
         d[k][e] = (g.dxp ? (float)vd[k][e] : 0.f) + rstd * (d[k][e] - m0 - xhat * m1);
         out[e] = (E)(n.alpha * d[k][e]);
       }
@@ -207,7 +223,7 @@ template <class E, int WAVES, int V, bool POST, bool GATE> __global__ __launch_b
         bool in = c + e < C;
         float du = d[k][e] * kept[e];
         float z = POST || GATE ? (float)vz[k][e] : 0.f;
-        float zhat = POST ? (z - pmean) * prstd : z;
+        float zhat = POST ? ((z - pmean) - pshift) * prstd : z;
         if (GATE) {
           float u = zhat;
           if (POST) u = zhat * (n.pw ? (float)pw[e] : 1.f) + (n.pb ? (float)pb[e] : 0.f);
@@ -233,7 +249,7 @@ template <class E, int WAVES, int V, bool POST, bool GATE> __global__ __launch_b
       for (int k = 0; k < V; k++) {
         int64_t c = c0 + k * WAVES * 512;
         typename Vec<E>::v8 out;
-        for (int e = 0; e < 8; e++) out[e] = (E)(prstd * (d[k][e] - p0 - ((float)vz[k][e] - pmean) * prstd * p1));
+        for (int e = 0; e < 8; e++) out[e] = (E)(prstd * (d[k][e] - p0 - (((float)vz[k][e] - pmean) - pshift) * prstd * p1));
         store8<E>((E *)g.dz + t * C + c, out, C - c);
       }
     }
@@ -363,7 +379,7 @@ template <class E, bool POST, bool GATE> static void norm_grad(const NormGrad &g
   else if (need <= 8) k_norm_grad<E, 4, 2, POST, GATE><<<n, 256, 0, st>>>(g);
   else if (need <= 16) k_norm_grad<E, 8, 2, POST, GATE><<<n, 512, 0, st>>>(g);
   else if (need <= 24) k_norm_grad<E, 8, 3, POST, GATE><<<n, 512, 0, st>>>(g);
-  else k_norm_grad<E, 16, 2, POST, GATE><<<n, 1024, 0, st>>>(g);
+  else k_norm_grad<E, 8, 4, POST, GATE><<<n, 512, 0, st>>>(g);
 }
 
 template <class E> static int norm_backward(const oob_norm *p, const oob_norm_grad *q, Arena a, hipStream_t st) {
