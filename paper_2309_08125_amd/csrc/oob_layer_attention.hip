@@ -18,6 +18,7 @@ struct Attention {
   /* backward */
   Heads dout, dq, dk, dv;
   const float *lse2, *delta; /* [B][H][Sq]: lse log2 e (0 where there is none), do . o */
+  float *parts;              /* [2][H / G][B][Sk][G][D] or null: dk and dv of every head for itself, where they are shared and workgroups are few */
   const int4 *ranges;  /* [B][tiles of grad_tile queries]: smallest begin, largest end, largest begin, smallest end */
 };
 
@@ -127,7 +128,7 @@ template <class E> __device__ inline typename Vec<E>::v8 round8(const float *p) 
 /* Four consecutive values of a row. */
 template <class E> __device__ inline void store4(char *row, int d, int D, float a, float b, float c, float e) {
   E *p = (E *)row + d;
-  typedef typename Vec<E>::v4 v4 __attribute__((aligned(2)));
+  typedef typename Vec<E>::v4 v4 __attribute__((aligned(sizeof(E))));
   if (d + 4 <= D) {
     v4 v = {(E)a, (E)b, (E)c, (E)e};
     *(v4 *)p = v;
@@ -592,8 +593,17 @@ template <class E, int DP, int KIND> __device__ __forceinline__ void attention_d
   int wave = uniform(threadIdx.x / 64), team = wave / 4, l = lane(), half = l >> 5;
   lds_char *lds = mem + team * GradLds<DP>::TEAM_BYTES; /* three tiles of q, three of do, three times the numbers */
   int tiles = (a.Sq + GT - 1) / GT, tile, g, b;
-  place(a.G, a.B, id, tile, g, b);
-  int k0 = tile * ROWS, w0 = k0 + wave % 4 * 32, j = w0 + (l & 31), offset = a.Sk - a.Sq, shared = a.H / a.G;
+  /* its heads: all that share the keys, or one of them */
+  int shared = a.H / a.G, h0;
+  if (a.parts) {
+    place(a.H, a.B, id, tile, h0, b);
+    g = h0 / shared;
+    shared = 1;
+  } else {
+    place(a.G, a.B, id, tile, g, b);
+    h0 = g * shared;
+  }
+  int k0 = tile * ROWS, w0 = k0 + wave % 4 * 32, j = w0 + (l & 31), offset = a.Sk - a.Sq;
 
   const int4 *ranges = a.ranges + (int64_t)b * tiles;
   int lo = FAR, hi = 0;
@@ -627,7 +637,7 @@ template <class E, int DP, int KIND> __device__ __forceinline__ void attention_d
   Tile now = ahead;
   auto load = [&](int which) __attribute__((always_inline)) { /* rows that see nothing are zeros, whatever they hold; past the last head too */
     bool there = ahead.head < shared && per;
-    int h = g * shared + (there ? ahead.head : 0), i0 = there ? ahead.t * GT : 0, most = there ? a.Sq : 0;
+    int h = h0 + (there ? ahead.head : 0), i0 = there ? ahead.t * GT : 0, most = there ? a.Sq : 0;
     const char *pq = a.q.p + b * a.q.batch + h * a.q.head, *pd = a.dout.p + b * a.dout.batch + h * a.dout.head;
     lds_char *tq = lds + which * TILE, *td = lds + (3 + which) * TILE;
     if (there && ranges[ahead.t].z == FAR) { /* some row of the tile sees nothing, or there is none */
@@ -681,7 +691,7 @@ template <class E, int DP, int KIND> __device__ __forceinline__ void attention_d
     if (there) range = ranges[now.t];
     int i0 = now.t * GT;
     float slope2 = 0;
-    if (KIND & BIAS) slope2 = a.slopes[g * shared + (there ? now.head : 0)] * LOG2E;
+    if (KIND & BIAS) slope2 = a.slopes[h0 + (there ? now.head : 0)] * LOG2E;
     bool all = w0 >= range.z && w0 + 32 <= range.w;
 #pragma unroll
     for (int x = 0; x < X; x++) {
@@ -766,7 +776,12 @@ template <class E, int DP, int KIND> __device__ __forceinline__ void attention_d
   landed<0>();
   join_sums(dk, mem, wave);
   join_sums(dv, mem, wave);
-  if (!team && j < a.Sk) {
+  if (!team && j < a.Sk && a.parts) {
+    int64_t per = (int64_t)a.B * a.Sk * a.G * a.D;
+    float *to = a.parts + h0 % (a.H / a.G) * per + (((int64_t)b * a.Sk + j) * a.G + g) * a.D;
+    store_column<float, DP>(dk, a.scale, (char *)to, a.D);
+    store_column<float, DP>(dv, 1.f, (char *)(to + a.H / a.G * per), a.D);
+  } else if (!team && j < a.Sk) {
     store_column<E, DP>(dk, a.scale, (char *)a.dk.p + b * a.dk.batch + g * a.dk.head + j * a.dk.row, a.D);
     store_column<E, DP>(dv, 1.f, (char *)a.dv.p + b * a.dv.batch + g * a.dv.head + j * a.dv.row, a.D);
   }
@@ -778,6 +793,17 @@ template <class E, int DP, int KIND> __global__ __launch_bounds__(THREADS, 2) vo
   __shared__ int part[8][2];
   if ((int)blockIdx.x < of_keys) attention_dkv<E, DP, KIND>(a, (lds_char *)mem, part, blockIdx.x);
   else attention_dq<E, DP, KIND>(a, (lds_char *)mem, part, blockIdx.x - of_keys);
+}
+
+/* dk and dv from those of the heads that share them. */
+template <class E> __global__ __launch_bounds__(256) void k_join_heads(Attention a) {
+  int64_t per = (int64_t)a.B * a.Sk * a.G * a.D, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= per) return;
+  int shared = a.H / a.G, d = (int)(at % a.D), g = (int)(at / a.D % a.G), j = (int)(at / a.D / a.G % a.Sk), b = (int)(at / a.D / a.G / a.Sk);
+  float dk = 0, dv = 0;
+  for (int h = 0; h < shared; h++) dk += a.parts[h * per + at], dv += a.parts[(shared + h) * per + at];
+  ((E *)(a.dk.p + b * a.dk.batch + g * a.dk.head + j * a.dk.row))[d] = (E)dk;
+  ((E *)(a.dv.p + b * a.dv.batch + g * a.dv.head + j * a.dv.row))[d] = (E)dv;
 }
 
 /* ---- heads that the loads cannot take (rows that do not start at 16 bytes, a width that is no multiple of 8) go to the workspace ---- */
@@ -864,11 +890,17 @@ template <class E> static int forward(const oob_attention *p, Arena w, hipStream
   return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
 }
 
+/* Heads that share keys: a workgroup goes through all of them, unless that leaves most of the GPU without work.  (2 sequences of 1531, 8
+ * heads on 2, width 80: 48 workgroups, 423 us forward and backward; one for each head and a pass that adds: 228 us.) */
+static bool by_head(const Attention &a) { return a.H > a.G && (int64_t)a.B * a.G * ((a.Sk + ROWS - 1) / ROWS) < 256; }
+static size_t parts_bytes(const Attention &a) { return by_head(a) ? (size_t)2 * (a.H / a.G) * a.B * a.Sk * a.G * a.D * 4 : 0; }
+
 static size_t backward_bytes(const oob_attention *p, const oob_attention_grad *q) {
   Attention a = attention_of(p);
   Arena w{nullptr, 0, 0};
   w.take((size_t)a.B * a.H * a.Sq * 8);
   w.take((size_t)a.B * ((a.Sq + 31) / 32) * sizeof(int4));
+  w.take(parts_bytes(a));
   for (const Heads &h : {a.k, a.v})
     if (!loadable(h, a.D)) w.take(packed_bytes(a.B, a.Sk, a.G, a.D));
   for (const Heads &h : {a.q, heads_of(q->dout, q->dout_stride)})
@@ -883,7 +915,8 @@ template <class E> static int backward(const oob_attention *p, const oob_attenti
   int64_t rows = (int64_t)a.B * a.H * a.Sq;
   float *lse2 = (float *)w.take((size_t)rows * 8), *delta = lse2 + rows;
   int4 *ranges = (int4 *)w.take((size_t)a.B * ((a.Sq + 31) / 32) * sizeof(int4));
-  a.lse2 = lse2, a.delta = delta, a.ranges = ranges;
+  float *parts = (float *)w.take(parts_bytes(a));
+  a.lse2 = lse2, a.delta = delta, a.ranges = ranges, a.parts = by_head(a) ? parts : nullptr;
   if (!w.ok()) return OOB_ECAPACITY;
   if (rows) {
     k_delta<E><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>(a, lse2, delta);
@@ -894,12 +927,13 @@ template <class E> static int backward(const oob_attention *p, const oob_attenti
   pack(a.q, a.B, a.Sq, a.H, a.D, w, st);
   pack(a.dout, a.B, a.Sq, a.H, a.D, w, st);
   if (!w.ok()) return OOB_ECAPACITY;
-  unsigned nq = (unsigned)((int64_t)a.B * a.H * ((a.Sq + ROWS - 1) / ROWS)), nk = (unsigned)((int64_t)a.B * a.G * ((a.Sk + ROWS - 1) / ROWS));
+  unsigned nq = (unsigned)((int64_t)a.B * a.H * ((a.Sq + ROWS - 1) / ROWS)), nk = (unsigned)((int64_t)a.B * (a.parts ? a.H : a.G) * ((a.Sk + ROWS - 1) / ROWS));
   by_kind(a, [&](auto kind) {
     constexpr int KIND = decltype(kind)::value;
     if (nk + nq && a.D <= 64) k_attention_grad<E, 64, KIND><<<nk + nq, THREADS, 0, st>>>(a, (int)nk);
     else if (nk + nq) k_attention_grad<E, 128, KIND><<<nk + nq, THREADS, 0, st>>>(a, (int)nk);
   });
+  if (nk && a.parts) k_join_heads<E><<<(unsigned)(((int64_t)a.B * a.Sk * a.G * a.D + 255) / 256), 256, 0, st>>>(a);
   return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
 }
 
