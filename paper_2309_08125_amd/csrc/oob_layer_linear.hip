@@ -14,8 +14,9 @@ struct Product {
   int64_t ldr;
   void *C, *Z;
   int64_t ldc, ldz;
-  float *partial; /* [splits][M][N] sums in place of the epilogue, or null */
-  int act, splits;
+  float *partial; /* [splits][rest][tile][tile]: sums of the tiles whose k is split, in place of the epilogue */
+  int act, splits; /* splits: of the tiles from number `full` on */
+  int full, rest;
   int tiles_m, tiles_n;
 };
 
@@ -124,6 +125,13 @@ template <class E> __device__ inline void epilogue(const Product &g, int64_t m, 
   store8<E>((E *)g.C + m * g.ldc + n, out, left);
 }
 
+/* Where a tile lies: bands of eight rows of tiles, so that consecutive workgroups of an XCD share rows of both operands in its L2. */
+template <int TILE> __device__ inline void locate(const Product &g, int tile, int64_t &m0, int64_t &n0) {
+  constexpr int BAND = 8;
+  int band = tile / (BAND * g.tiles_n), high = g.tiles_m - band * BAND < BAND ? g.tiles_m - band * BAND : BAND, in = tile - band * BAND * g.tiles_n;
+  m0 = (int64_t)(band * BAND + in % high) * TILE, n0 = (int64_t)(in / high) * TILE;
+}
+
 template <class E, int TM, int TN, int WM, int WN, bool AK, bool BK>
 __global__ __launch_bounds__(WM *WN * 64, 2) void k_product(Product g) {
   constexpr int THREADS = WM * WN * 64, FM = TM / WM / 32, FN = TN / WN / 32;
@@ -134,19 +142,18 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_product(Product g) {
   __shared__ __attribute__((aligned(1024))) char mem[2 * STAGE > EPI ? 2 * STAGE : EPI];
   lds_char *lds = (lds_char *)mem;
 
-  /* tiles of C in bands of eight rows of tiles, so that consecutive workgroups of an XCD share rows of both operands in its L2 */
-  int64_t tiles = (int64_t)g.tiles_m * g.tiles_n;
-  int64_t id = xcd_order(blockIdx.x, tiles * g.splits);
-  int split = (int)(id / tiles);
-  id %= tiles;
-  constexpr int BAND = 8;
-  int64_t band = id / (BAND * (int64_t)g.tiles_n);
-  int high = (int)(g.tiles_m - band * BAND < BAND ? g.tiles_m - band * BAND : BAND);
-  int64_t in = id - band * BAND * g.tiles_n;
-  int64_t m0 = (band * BAND + in % high) * TM, n0 = in / high * TN;
+  int tile, split = 0, splits = 1;
+  if ((int)blockIdx.x < g.full) {
+    tile = (int)xcd_order(blockIdx.x, g.full);
+  } else {
+    int id = (int)xcd_order(blockIdx.x - g.full, (int64_t)g.rest * g.splits);
+    tile = g.full + id % g.rest, split = id / g.rest, splits = g.splits;
+  }
+  int64_t m0, n0;
+  locate<TM>(g, tile, m0, n0);
 
   int steps = (int)((g.K + KSTEP - 1) / KSTEP);
-  int first = (int)((int64_t)steps * split / g.splits), last = (int)((int64_t)steps * (split + 1) / g.splits);
+  int first = (int)((int64_t)steps * split / splits), last = (int)((int64_t)steps * (split + 1) / splits);
 
   TA ta;
   TB tb;
@@ -180,17 +187,29 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_product(Product g) {
       ta.load(pa, next, kleft);
       tb.load(pb, next + TA::BYTES, kleft);
     }
+    typename Vec<E>::v8 a[2][FM], b[2][FN];
+    auto fetch = [&](int s, int x) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < FM; i++) a[x][i] = fa.read(now, i, s);
+#pragma unroll
+      for (int j = 0; j < FN; j++) b[x][j] = fb.read(now + TA::BYTES, j, s);
+    };
+    fetch(0, 0);
 #pragma unroll
     for (int s = 0; s < 4; s++) {
-      typename Vec<E>::v8 a[FM], b[FN];
-#pragma unroll
-      for (int i = 0; i < FM; i++) a[i] = fa.read(now, i, s);
-#pragma unroll
-      for (int j = 0; j < FN; j++) b[j] = fb.read(now + TA::BYTES, j, s);
+      if (s < 3) fetch(s + 1, (s + 1) % 2);
 #pragma unroll
       for (int i = 0; i < FM; i++)
 #pragma unroll
-        for (int j = 0; j < FN; j++) acc[i][j] = mfma(b[j], a[i], acc[i][j]); /* lane: m, registers: n */
+        for (int j = 0; j < FN; j++) acc[i][j] = mfma(b[s % 2][j], a[s % 2][i], acc[i][j]); /* lane: m, registers: n */
+      /* reads of the next fragments between the products */
+      constexpr int READS = FM * (AK ? 1 : 2) + FN * (BK ? 1 : 2);
+      if (s == 0) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+#pragma unroll
+      for (int g = 0; g < FM * FN; g++) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        if (s < 3 && g < READS) __builtin_amdgcn_sched_group_barrier(0x100, (READS + FM * FN - 1) / (FM * FN), 0);
+      }
     }
   }
   __syncthreads();
@@ -217,10 +236,9 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_product(Product g) {
       float v[8];
       for (int e = 0; e < 8; e += 4) *(f32x4 *)(v + e) = *(__attribute__((address_space(3))) f32x4 *)(stage + row * PITCH + l % LPR * 8 + e);
       if (m < g.M && n < g.N) {
-        if (g.partial) {
-          float *to = g.partial + ((int64_t)split * g.M + m) * g.N + n;
-          for (int e = 0; e < 8; e++)
-            if (n + e < g.N) to[e] = v[e];
+        if (splits > 1) {
+          float *to = g.partial + ((int64_t)split * g.rest + (tile - g.full)) * TM * TN + (m - m0) * TN + (n - n0);
+          for (int e = 0; e < 8; e += 4) *(f32x4 *)(to + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
         } else {
           epilogue<E>(g, m, n, v);
         }
@@ -231,15 +249,20 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_product(Product g) {
   }
 }
 
-/* Joins the parts of a product whose k was split. */
-template <class E> __global__ __launch_bounds__(256) void k_join(Product g) {
-  int64_t per = (g.N + 7) / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  int64_t m = id / per, n = id % per * 8;
-  if (m >= g.M) return;
+/* Joins the parts of the tiles whose k was split. */
+template <class E, int TILE> __global__ __launch_bounds__(256) void k_join(Product g) {
+  constexpr int PER = TILE * TILE / 8 / 256; /* workgroups a tile, eight values a thread */
+  int tile = blockIdx.x / PER, at = (blockIdx.x % PER * 256 + threadIdx.x) * 8;
+  int64_t m, n;
+  locate<TILE>(g, g.full + tile, m, n);
+  m += at / TILE, n += at % TILE;
+  if (m >= g.M || n >= g.N) return;
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 4
   for (int s = 0; s < g.splits; s++) {
-    const float *p = g.partial + ((int64_t)s * g.M + m) * g.N + n;
-    for (int e = 0; e < 8; e++) v[e] += n + e < g.N ? p[e] : 0.f;
+    const float *p = g.partial + ((int64_t)s * g.rest + tile) * TILE * TILE + at;
+    f32x4 lo = *(const f32x4 *)p, hi = *(const f32x4 *)(p + 4);
+    for (int e = 0; e < 4; e++) v[e] += lo[e], v[4 + e] += hi[e];
   }
   epilogue<E>(g, m, n, v);
 }
@@ -316,27 +339,35 @@ struct Operand { const void *p; int64_t ld, rows, cols; }; /* stored rows x cols
 /* What the loads to LDS can take: 16-byte pieces of rows that end with the row, offsets within a tile below 2^31. */
 static bool loadable(const Operand &o) { return o.cols % 8 == 0 && multiple(o.p, 16) && o.ld % 8 == 0 && o.ld < (1 << 21); }
 
-struct Shape { int tile, splits; };
+struct Shape { int tile, splits, full, rest; };
 
-/* Which tile and how many parts of k.  A step of the large tile costs a compute unit as much as four of the middle one, but reads half
- * as much per product; below 256 tiles units stand idle.  So: the largest tile that gives (nearly) every unit one; the smallest,
- * with k split until there are two workgroups a unit and no part has under four steps, where none does. */
+/* Which tile, and which tiles' k is split into how many parts.  The large tile reads half as much per product as the middle one (4096 x
+ * 12288 x 6144: 497 against 565 us), a workgroup of it takes a compute unit.  What is left of the last round of 256 is split so that all
+ * units share it (4096 x 6144 x 12288, 384 tiles: 571 us in two rounds, 518 us in one and a half and the join).  Below that the middle tile,
+ * two workgroups a unit (4096 x 8192 x 2048: 163 us, the small one 245); where neither gives most units one, the small tile with k split
+ * until there are two workgroups a unit and no part has under four steps (1024 x 2048 x 2048: 19 us, the middle one 26). */
 static Shape choose(int64_t M, int64_t N, int64_t K) {
   auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
-  int64_t steps = (K + KSTEP - 1) / KSTEP;
-  if (tiles(256) >= 192) return {256, 1};
-  if (tiles(128) >= 192) return {128, 1};
-  int64_t n = tiles(64), s = 1;
+  int64_t steps = (K + KSTEP - 1) / KSTEP, n = tiles(256), rest = n % 256;
+  int64_t s = rest ? 256 / rest : 1;
+  if (s > steps / 40) s = steps / 40; /* a part of fewer steps costs less than its join */
+  if (s > 8) s = 8;
+  if (rest && s >= 2 && (n > 256 || rest * s >= 192)) return {256, (int)s, (int)(n - rest), (int)rest};
+  if (n >= 192) return {256, 1, (int)n, 0};
+  n = tiles(128);
+  if (n >= 192) return {128, 1, (int)n, 0};
+  n = tiles(64), s = 1;
   while (n * s < 512 && steps / (s * 2) >= 4 && s < 32) s *= 2;
-  return {64, (int)s};
+  return s == 1 ? Shape{64, 1, (int)n, 0} : Shape{64, (int)s, 0, (int)n};
 }
+static size_t partial_bytes(const Shape &s) { return s.rest ? (size_t)s.splits * s.rest * s.tile * s.tile * 4 : 0; }
 
 static size_t product_workspace(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K) {
   Arena w{nullptr, 0, 0};
   if (!loadable(a)) w.take((size_t)a.rows * up(a.cols, 8) * 2);
   if (!loadable(b)) w.take((size_t)b.rows * up(b.cols, 8) * 2);
   Shape s = choose(M, N, K);
-  if (s.splits > 1) w.take((size_t)s.splits * M * N * 4);
+  w.take(partial_bytes(s));
   return w.used;
 }
 
@@ -350,11 +381,12 @@ static Operand pack(const Operand &o, Arena &w, hipStream_t st) {
 }
 
 template <class E, bool AK, bool BK> static void launch(const Product &g, int tile, hipStream_t st) {
-  unsigned n = (unsigned)((int64_t)g.tiles_m * g.tiles_n * g.splits);
+  unsigned n = (unsigned)(g.full + (int64_t)g.rest * g.splits);
   if (tile == 256) k_product<E, 256, 256, 2, 4, AK, BK><<<n, 512, 0, st>>>(g);
   else if (tile == 128) k_product<E, 128, 128, 2, 2, AK, BK><<<n, 256, 0, st>>>(g);
   else k_product<E, 64, 64, 2, 2, AK, BK><<<n, 256, 0, st>>>(g);
-  if (g.splits > 1) k_join<E><<<(unsigned)((g.M * ((g.N + 7) / 8) + 255) / 256), 256, 0, st>>>(g);
+  if (g.rest && tile == 256) k_join<E, 256><<<(unsigned)g.rest * 32, 256, 0, st>>>(g);
+  else if (g.rest) k_join<E, 64><<<(unsigned)g.rest * 2, 256, 0, st>>>(g);
 }
 
 /* The product with its operands as they are stored: ak (bk) says that k is contiguous.  The arena comes by value: what one product
@@ -365,8 +397,8 @@ template <class E> static int product(Operand a, bool ak, Operand b, bool bk, Pr
   a = pack(a, w, st);
   b = pack(b, w, st);
   g.A = a.p, g.lda = a.ld, g.B = b.p, g.ldb = b.ld;
-  g.splits = s.splits;
-  g.partial = s.splits > 1 ? (float *)w.take((size_t)s.splits * g.M * g.N * 4) : nullptr;
+  g.splits = s.splits, g.full = s.full, g.rest = s.rest;
+  g.partial = (float *)w.take(partial_bytes(s));
   if (!w.ok()) return OOB_ECAPACITY;
   g.tiles_m = (int)((g.M + s.tile - 1) / s.tile), g.tiles_n = (int)((g.N + s.tile - 1) / s.tile);
   if (ak && bk) launch<E, true, true>(g, s.tile, st);
