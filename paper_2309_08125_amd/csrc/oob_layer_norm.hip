@@ -83,13 +83,23 @@ template <class E, int WAVES, int V> __global__ __launch_bounds__(WAVES < 4 ? 25
     if (n.w) w[k] = load8<E>((const E *)n.w + c, C - c);
     if (n.b) b[k] = load8<E>((const E *)n.b + c, C - c);
   }
-  for (int64_t t = (int64_t)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x / 64 : 0); t < n.T; t += (int64_t)gridDim.x * ROWS) {
-    float x[V][8], u[V][8];
+  typename Vec<E>::v8 vx[V], vz[V];
+  auto load = [&](int64_t t) __attribute__((always_inline)) {
     for (int k = 0; k < V; k++) {
       int64_t c = c0 + k * WAVES * 512;
-      widen<E>(load8<E>((const E *)n.x + t * n.ldx + c, C - c), x[k]);
-      if (n.z) widen<E>(load8<E>((const E *)n.z + t * n.ldz + c, C - c), u[k]);
+      vx[k] = load8<E>((const E *)n.x + t * n.ldx + c, C - c);
+      if (n.z) vz[k] = load8<E>((const E *)n.z + t * n.ldz + c, C - c);
     }
+  };
+  int64_t t = (int64_t)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x / 64 : 0), stride = (int64_t)gridDim.x * ROWS;
+  if (t < n.T) load(t);
+  for (; t < n.T; t += stride) {
+    float x[V][8], u[V][8];
+    for (int k = 0; k < V; k++) {
+      widen<E>(vx[k], x[k]);
+      if (n.z) widen<E>(vz[k], u[k]);
+    }
+    if (t + stride < n.T) load(t + stride); /* on its way while this row is worked on */
     if (n.z) {
       if (n.post != OOB_NORM_NONE) {
         float mean, rstd;
@@ -342,8 +352,10 @@ static Norm norm_of(const oob_norm *p) {
 }
 
 template <class E> static void norm(const Norm &n, hipStream_t st) {
-  /* rows of up to 2048 by one wave: no barrier; wider ones by as many waves as keep a lane's part in 48 registers */
-  int64_t need = (n.C + 511) / 512, rows = n.T < 2048 ? n.T : 2048, rows4 = n.T < 8192 ? (n.T + 3) / 4 : 2048;
+  /* Rows of up to 2048 by one wave: no barrier; wider ones by as many waves as keep a lane's part in 32 registers.  768 workgroups that go
+   * through the rows with the weights in registers and the next row on its way (4096 x 12288, bfloat16: 95 us with dropout and 81 without,
+   * 4.2 and 5.0 TB/s, a large copy's rate; 121 and 104 us by 2048 workgroups without the row ahead). */
+  int64_t need = (n.C + 511) / 512, rows = n.T < 768 ? n.T : 768, rows4 = n.T < 8192 ? (n.T + 3) / 4 : 2048;
   if (need <= 1) k_norm<E, 1, 1><<<(unsigned)rows4, 256, 0, st>>>(n);
   else if (need <= 2) k_norm<E, 1, 2><<<(unsigned)rows4, 256, 0, st>>>(n);
   else if (need <= 4) k_norm<E, 1, 4><<<(unsigned)rows4, 256, 0, st>>>(n);
@@ -355,10 +367,12 @@ template <class E> static void norm(const Norm &n, hipStream_t st) {
 
 struct Runs { int64_t workgroups, rows, per_gate; };
 
-/* Workgroups of the backward pass: about two a compute unit.  Where there are gates, a workgroup's rows belong to one gate, or, with
+/* Workgroups of the backward pass: enough waves to fill the GPU, and no more: each leaves a row of sums per weight (4096 x 12288: 131 us
+ * with 256 workgroups of eight waves, 141 with 512; 4096 x 4096: 47 us with 512 of four, 61 with 256; what is read and written at a copy's
+ * rate would take 100 and 33 us; loading the next row ahead gained nothing).  Where there are gates, a workgroup's rows belong to one gate, or, with
  * more gates than workgroups, to whole gates. */
-static Runs runs_of(int64_t T, int64_t gates) {
-  const int64_t most = 512;
+static Runs runs_of(int64_t T, int64_t C, int64_t gates) {
+  const int64_t most = C > 4096 ? 256 : 512;
   if (gates > most) {
     int64_t per = (gates + most - 1) / most, rows = per * (T / gates);
     return {(T + rows - 1) / rows, rows, 0};
@@ -383,7 +397,7 @@ template <class E, bool POST, bool GATE> static void norm_grad(const NormGrad &g
 }
 
 template <class E> static int norm_backward(const oob_norm *p, const oob_norm_grad *q, Arena a, hipStream_t st) {
-  Runs r = runs_of(p->T, p->gates);
+  Runs r = runs_of(p->T, p->C, p->gates);
   bool post = p->post != OOB_NORM_NONE, gate = p->gates > 0;
   int kinds = post ? 4 : 2;
   NormGrad g{};
@@ -410,7 +424,7 @@ template <class E> static int norm_backward(const oob_norm *p, const oob_norm_gr
 }
 
 static size_t norm_bytes(const oob_norm *p) {
-  Runs r = runs_of(p->T, p->gates);
+  Runs r = runs_of(p->T, p->C, p->gates);
   Arena a{nullptr, 0, 0};
   a.take((size_t)r.workgroups * (p->post != OOB_NORM_NONE ? 4 : 2) * p->C * 4);
   if (p->gates && r.per_gate) a.take((size_t)r.workgroups * p->C * 4);
