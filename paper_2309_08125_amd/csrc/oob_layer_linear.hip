@@ -22,12 +22,15 @@ struct Product {
 
 constexpr int KSTEP = 64; /* depth of a step: 128-byte rows of k */
 
+/* 1 / (1 + e^-x).  The reciprocal instruction (1 unit of 2^-23) in place of a division, which is ten: results are rounded to 16 bits. */
+__device__ inline float sigmoid(float x) { return __builtin_amdgcn_rcpf(1 + __builtin_amdgcn_exp2f(x * -1.44269504f)); }
+
 __device__ inline float activate(float z, int act) {
   switch (act) {
     case OOB_ACT_RELU: return z > 0 ? z : (z != z ? z : 0.f);
-    case OOB_ACT_SILU: return z / (1 + __expf(-z));
+    case OOB_ACT_SILU: return z * sigmoid(z);
     case OOB_ACT_GELU: return 0.5f * z * (1 + erff(z * 0.70710678f));
-    case OOB_ACT_GELU_TANH: return z / (1 + __expf(-1.5957691216f * (z + 0.044715f * z * z * z)));
+    case OOB_ACT_GELU_TANH: return z * sigmoid(1.5957691216f * (z + 0.044715f * z * z * z)); /* 0.5 (1 + tanh(u)) = sigmoid(2 u) */
     default: return z;
   }
 }
@@ -36,11 +39,10 @@ __device__ inline float activate(float z, int act) {
 __device__ inline float slope(float z, int act) {
   switch (act) {
     case OOB_ACT_RELU: return z > 0 ? 1.f : 0.f;
-    case OOB_ACT_SILU: { float e = 1 / (1 + __expf(-z)); return e * (1 + z * (1 - e)); }
+    case OOB_ACT_SILU: { float e = sigmoid(z); return e * (1 + z * (1 - e)); }
     case OOB_ACT_GELU: return 0.5f * (1 + erff(z * 0.70710678f)) + z * 0.39894228f * __expf(-0.5f * z * z);
     case OOB_ACT_GELU_TANH: {
-      /* 0.5 (1 + tanh(u)) = 1 / (1 + exp(-2 u)) = e;  its derivative is 2 e (1 - e) u' */
-      float e = 1 / (1 + __expf(-1.5957691216f * (z + 0.044715f * z * z * z)));
+      float e = sigmoid(1.5957691216f * (z + 0.044715f * z * z * z)); /* its derivative is 2 e (1 - e) u' */
       return e + z * 2 * e * (1 - e) * 0.7978845608f * (1 + 0.134145f * z * z);
     }
     default: return 1.f;
@@ -288,31 +290,37 @@ struct ActGrad {
   int64_t ld_dy, ld_z, ld_dz, T, N;
   float *sums; /* [runs][N] or null */
   int64_t rows; /* of a run */
-  int act;
 };
 
-template <class E> __global__ __launch_bounds__(256) void k_act_grad(ActGrad g) {
+template <class E, int ACT> __global__ __launch_bounds__(256) void k_act_grad(ActGrad g) {
   __shared__ float part[4][512 + 8];
   int64_t n = (int64_t)blockIdx.x * 512 + lane() * 8, left = g.N - n;
   int64_t t1 = ((int64_t)blockIdx.y + 1) * g.rows < g.T ? ((int64_t)blockIdx.y + 1) * g.rows : g.T;
   float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (left > 0)
-#pragma unroll 4
-    for (int64_t t = (int64_t)blockIdx.y * g.rows + threadIdx.x / 64; t < t1; t += 4) {
-      typename Vec<E>::v8 d = load8<E>((const E *)g.dy + t * g.ld_dy + n, left), out;
+  const int64_t stop = left > 0 ? t1 : 0;
+  for (int64_t t0 = (int64_t)blockIdx.y * g.rows + threadIdx.x / 64; t0 < stop; t0 += 16) {
+    typename Vec<E>::v8 d[4], z[4], out; /* four rows on their way before the first is worked on */
+#pragma unroll
+    for (int u = 0; u < 4; u++)
+      if (t0 + 4 * u < stop) {
+        d[u] = load8<E>((const E *)g.dy + (t0 + 4 * u) * g.ld_dy + n, left);
+        if (g.dz && ACT != OOB_ACT_NONE) z[u] = load8<E>((const E *)g.z + (t0 + 4 * u) * g.ld_z + n, left);
+      }
+#pragma unroll
+    for (int u = 0; u < 4; u++) {
+      if (t0 + 4 * u >= stop) continue;
       if (g.dz) {
-        typename Vec<E>::v8 z = d;
-        if (g.act != OOB_ACT_NONE) z = load8<E>((const E *)g.z + t * g.ld_z + n, left);
         for (int e = 0; e < 8; e++) {
-          float v = (float)d[e] * slope((float)z[e], g.act);
+          float v = (float)d[u][e] * slope(ACT == OOB_ACT_NONE ? 0.f : (float)z[u][e], ACT);
           out[e] = (E)v;
           sum[e] += v; /* before the rounding: the bias's gradient does not see it */
         }
-        store8<E>((E *)g.dz + t * g.ld_dz + n, out, 8); /* past N: zeros */
+        store8<E>((E *)g.dz + (t0 + 4 * u) * g.ld_dz + n, out, 8); /* past N: zeros */
       } else {
-        for (int e = 0; e < 8; e++) sum[e] += (float)d[e];
+        for (int e = 0; e < 8; e++) sum[e] += (float)d[u][e];
       }
     }
+  }
   if (!g.sums) return;
   for (int e = 0; e < 8; e++) part[threadIdx.x / 64][lane() * 8 + e] = sum[e];
   __syncthreads();
@@ -460,10 +468,17 @@ template <class E> static int linear_grad(const oob_linear_grad *p, Arena w, hip
     ActGrad a{};
     a.dy = p->dy, a.ld_dy = p->dy_stride, a.z = p->z, a.ld_z = p->z_stride;
     a.dz = makes ? const_cast<void *>(dz.p) : nullptr, a.ld_dz = dz.ld;
-    a.T = p->T, a.N = p->N, a.sums = sums, a.act = p->act;
+    a.T = p->T, a.N = p->N, a.sums = sums;
     int64_t runs = runs_of(p->T, p->N);
     a.rows = (p->T + runs - 1) / runs;
-    k_act_grad<E><<<dim3((unsigned)((p->N + 511) / 512), (unsigned)runs), 256, 0, st>>>(a);
+    dim3 grid((unsigned)((p->N + 511) / 512), (unsigned)runs);
+    switch (p->act) {
+      case OOB_ACT_RELU: k_act_grad<E, OOB_ACT_RELU><<<grid, 256, 0, st>>>(a); break;
+      case OOB_ACT_GELU: k_act_grad<E, OOB_ACT_GELU><<<grid, 256, 0, st>>>(a); break;
+      case OOB_ACT_GELU_TANH: k_act_grad<E, OOB_ACT_GELU_TANH><<<grid, 256, 0, st>>>(a); break;
+      case OOB_ACT_SILU: k_act_grad<E, OOB_ACT_SILU><<<grid, 256, 0, st>>>(a); break;
+      default: k_act_grad<E, OOB_ACT_NONE><<<grid, 256, 0, st>>>(a);
+    }
     if (sums) k_sum_rows<E><<<(unsigned)((p->N + 63) / 64), 256, 0, st>>>(sums, runs, p->N, (E *)p->db);
   }
   int rc = hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;

@@ -352,17 +352,17 @@ static Norm norm_of(const oob_norm *p) {
 }
 
 template <class E> static void norm(const Norm &n, hipStream_t st) {
-  /* Rows of up to 2048 by one wave: no barrier; wider ones by as many waves as keep a lane's part in 32 registers.  768 workgroups that go
-   * through the rows with the weights in registers and the next row on its way (4096 x 12288, bfloat16: 95 us with dropout and 81 without,
+  /* Rows of up to 2048 by one wave: no barrier; wider ones by as many waves as keep a lane's part in 32 registers.  Workgroups (768 of eight
+   * waves) go through the rows with the weights in registers and the next row on its way (4096 x 12288, bfloat16: 95 us with dropout and 81 without,
    * 4.2 and 5.0 TB/s, a large copy's rate; 121 and 104 us by 2048 workgroups without the row ahead). */
-  int64_t need = (n.C + 511) / 512, rows = n.T < 768 ? n.T : 768, rows4 = n.T < 8192 ? (n.T + 3) / 4 : 2048;
+  int64_t need = (n.C + 511) / 512, rows = n.T < 2048 ? n.T : 2048, wide = n.T < 768 ? n.T : 768, rows4 = n.T < 8192 ? (n.T + 3) / 4 : 2048;
   if (need <= 1) k_norm<E, 1, 1><<<(unsigned)rows4, 256, 0, st>>>(n);
   else if (need <= 2) k_norm<E, 1, 2><<<(unsigned)rows4, 256, 0, st>>>(n);
   else if (need <= 4) k_norm<E, 1, 4><<<(unsigned)rows4, 256, 0, st>>>(n);
   else if (need <= 8) k_norm<E, 4, 2><<<(unsigned)rows, 256, 0, st>>>(n);
   else if (need <= 16) k_norm<E, 4, 4><<<(unsigned)rows, 256, 0, st>>>(n);
-  else if (need <= 24) k_norm<E, 8, 3><<<(unsigned)rows, 512, 0, st>>>(n);
-  else k_norm<E, 8, 4><<<(unsigned)rows, 512, 0, st>>>(n);
+  else if (need <= 24) k_norm<E, 8, 3><<<(unsigned)wide, 512, 0, st>>>(n);
+  else k_norm<E, 8, 4><<<(unsigned)wide, 512, 0, st>>>(n);
 }
 
 struct Runs { int64_t workgroups, rows, per_gate; };
