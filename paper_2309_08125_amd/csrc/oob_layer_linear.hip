@@ -117,8 +117,12 @@ template <class E> __device__ inline void epilogue(const Product &g, int64_t m, 
     for (int e = 0; e < 8; e++) out[e] = (E)v[e];
     store8<E>((E *)g.Z + m * g.ldz + n, out, left);
   }
-  if (g.act != OOB_ACT_NONE)
-    for (int e = 0; e < 8; e++) v[e] = activate(v[e], g.act);
+  switch (g.act) { /* outside the loop: once for eight values */
+    case OOB_ACT_RELU: for (int e = 0; e < 8; e++) v[e] = activate(v[e], OOB_ACT_RELU); break;
+    case OOB_ACT_SILU: for (int e = 0; e < 8; e++) v[e] = activate(v[e], OOB_ACT_SILU); break;
+    case OOB_ACT_GELU: for (int e = 0; e < 8; e++) v[e] = activate(v[e], OOB_ACT_GELU); break;
+    case OOB_ACT_GELU_TANH: for (int e = 0; e < 8; e++) v[e] = activate(v[e], OOB_ACT_GELU_TANH); break;
+  }
   if (g.residual) {
     typename Vec<E>::v8 r = load8<E>((const E *)g.residual + m * g.ldr + n, left);
     for (int e = 0; e < 8; e++) v[e] += (float)r[e];

@@ -62,6 +62,13 @@ template <int WAVES, int V> __device__ inline void statistics(const float (&x)[V
   rstd = 1 / sqrtf(q[0] / C + eps);
 }
 
+/* Eight of a vector, or a constant where there is none. */
+template <class E> __device__ inline typename Vec<E>::v8 load8_or(const void *p, int64_t at, int64_t left, float otherwise) {
+  if (p) return load8<E>((const E *)p + at, left);
+  typename Vec<E>::v8 v;
+  for (int e = 0; e < 8; e++) v[e] = (E)otherwise;
+  return v;
+}
 template <class E> __device__ inline void widen(typename Vec<E>::v8 v, float (&f)[8]) {
   for (int e = 0; e < 8; e++) f[e] = (float)v[e];
 }
@@ -80,8 +87,8 @@ template <class E, int WAVES, int V> __global__ __launch_bounds__(WAVES < 4 ? 25
   typename Vec<E>::v8 w[V], b[V];
   for (int k = 0; k < V; k++) {
     int64_t c = c0 + k * WAVES * 512;
-    if (n.w) w[k] = load8<E>((const E *)n.w + c, C - c);
-    if (n.b) b[k] = load8<E>((const E *)n.b + c, C - c);
+    w[k] = load8_or<E>(n.w, c, C - c, 1.f);
+    b[k] = load8_or<E>(n.b, c, C - c, 0.f);
   }
   typename Vec<E>::v8 vx[V], vz[V];
   auto load = [&](int64_t t) __attribute__((always_inline)) {
@@ -106,10 +113,8 @@ template <class E, int WAVES, int V> __global__ __launch_bounds__(WAVES < 4 ? 25
         statistics<WAVES, V>(u, n.post, C, n.eps, c0, mean, rstd, part, turn);
         for (int k = 0; k < V; k++) {
           int64_t c = c0 + k * WAVES * 512;
-          typename Vec<E>::v8 pw, pb;
-          if (n.pw) pw = load8<E>((const E *)n.pw + c, C - c);
-          if (n.pb) pb = load8<E>((const E *)n.pb + c, C - c);
-          for (int e = 0; e < 8; e++) u[k][e] = (u[k][e] - mean) * rstd * (n.pw ? (float)pw[e] : 1.f) + (n.pb ? (float)pb[e] : 0.f);
+          typename Vec<E>::v8 pw = load8_or<E>(n.pw, c, C - c, 1.f), pb = load8_or<E>(n.pb, c, C - c, 0.f);
+          for (int e = 0; e < 8; e++) u[k][e] = (u[k][e] - mean) * rstd * (float)pw[e] + (float)pb[e];
         }
         if (c0 == 0) {
           if (n.pmean) n.pmean[t] = mean;
@@ -142,7 +147,7 @@ template <class E, int WAVES, int V> __global__ __launch_bounds__(WAVES < 4 ? 25
     for (int k = 0; k < V; k++) {
       int64_t c = c0 + k * WAVES * 512;
       typename Vec<E>::v8 out;
-      for (int e = 0; e < 8; e++) out[e] = (E)((x[k][e] - mean) * rstd * (n.w ? (float)w[k][e] : 1.f) + (n.b ? (float)b[k][e] : 0.f));
+      for (int e = 0; e < 8; e++) out[e] = (E)((x[k][e] - mean) * rstd * (float)w[k][e] + (float)b[k][e]);
       store8<E>((E *)n.h + t * C + c, out, C - c);
     }
   }
@@ -171,7 +176,7 @@ template <class E, int WAVES, int V, bool POST, bool GATE> __global__ __launch_b
       int64_t c = c0 + k * WAVES * 512;
       vx[k] = load8<E>((const E *)n.x + t * n.ldx + c, C - c);
       vh[k] = load8<E>((const E *)g.dh + t * g.ld_dh + c, C - c);
-      if (g.dxp) vd[k] = load8<E>((const E *)g.dxp + t * g.ld_dxp + c, C - c);
+      vd[k] = load8_or<E>(g.dxp, t * g.ld_dxp + c, C - c, 0.f);
       if (POST || GATE) vz[k] = load8<E>((const E *)n.z + t * n.ldz + c, C - c);
     }
     /* The statistics are those of x' as it was stored, not of what it was before: with y = x' - (the forward pass's mean), the row's
@@ -181,11 +186,10 @@ template <class E, int WAVES, int V, bool POST, bool GATE> __global__ __launch_b
     float d[V][8], s[POST ? 6 : 4] = {};
     for (int k = 0; k < V; k++) {
       int64_t c = c0 + k * WAVES * 512;
-      typename Vec<E>::v8 w;
-      if (n.w) w = load8<E>((const E *)n.w + c, C - c);
+      typename Vec<E>::v8 w = load8_or<E>(n.w, c, C - c, 1.f);
       for (int e = 0; e < 8; e++) {
         float y = c + e < C ? (float)vx[k][e] - mean : 0.f;
-        float v = (float)vh[k][e] * (n.w ? (float)w[e] : 1.f);
+        float v = (float)vh[k][e] * (float)w[e];
         d[k][e] = v;
         s[0] += y;
         s[1] += y * y;
@@ -214,7 +218,7 @@ template <class E, int WAVES, int V, bool POST, bool GATE> __global__ __launch_b
         float xhat = (((float)vx[k][e] - mean) - shift) * rstd; /* not less the sum of both: it would round */
         dw[k][e] += (float)vh[k][e] * xhat;
         db[k][e] += (float)vh[k][e];
-        d[k][e] = (g.dxp ? (float)vd[k][e] : 0.f) + rstd * (d[k][e] - m0 - xhat * m1);
+        d[k][e] = (float)vd[k][e] + rstd * (d[k][e] - m0 - xhat * m1);
         out[e] = (E)(n.alpha * d[k][e]);
       }
       store8<E>((E *)g.dx + t * C + c, out, C - c);
@@ -227,8 +231,8 @@ template <class E, int WAVES, int V, bool POST, bool GATE> __global__ __launch_b
       } else
         for (int e = 0; e < 8; e++) kept[e] = 1;
       if (GATE) gate = load8<E>((const E *)n.gate + t / n.rows_per_gate * C + c, C - c);
-      if (POST && n.pw) pw = load8<E>((const E *)n.pw + c, C - c);
-      if (GATE && POST && n.pb) pb = load8<E>((const E *)n.pb + c, C - c);
+      if (POST) pw = load8_or<E>(n.pw, c, C - c, 1.f);
+      if (GATE && POST) pb = load8_or<E>(n.pb, c, C - c, 0.f);
       for (int e = 0; e < 8; e++) {
         bool in = c + e < C;
         float du = d[k][e] * kept[e];
@@ -236,7 +240,7 @@ template <class E, int WAVES, int V, bool POST, bool GATE> __global__ __launch_b
         float zhat = POST ? ((z - pmean) - pshift) * prstd : z;
         if (GATE) {
           float u = zhat;
-          if (POST) u = zhat * (n.pw ? (float)pw[e] : 1.f) + (n.pb ? (float)pb[e] : 0.f);
+          if (POST) u = zhat * (float)pw[e] + (float)pb[e];
           dg[k][e] += du * u;
           du *= (float)gate[e];
         }
@@ -244,7 +248,7 @@ template <class E, int WAVES, int V, bool POST, bool GATE> __global__ __launch_b
           du = in ? du : 0.f;
           dpw[k][e] += du * zhat;
           dpb[k][e] += du;
-          du *= n.pw ? (float)pw[e] : 1.f;
+          du *= (float)pw[e];
           q[0] += du;
           q[1] += du * zhat;
         }
@@ -352,15 +356,15 @@ static Norm norm_of(const oob_norm *p) {
 }
 
 template <class E> static void norm(const Norm &n, hipStream_t st) {
-  /* Rows of up to 2048 by one wave: no barrier; wider ones by as many waves as keep a lane's part in 32 registers.  Workgroups (768 of eight
+  /* Rows of up to 1024 by one wave: no barrier; wider ones by as many waves as keep a lane's part in 32 registers.  Workgroups (768 of eight
    * waves) go through the rows with the weights in registers and the next row on its way (4096 x 12288, bfloat16: 95 us with dropout and 81 without,
    * 4.2 and 5.0 TB/s, a large copy's rate; 121 and 104 us by 2048 workgroups without the row ahead). */
   int64_t need = (n.C + 511) / 512, rows = n.T < 2048 ? n.T : 2048, wide = n.T < 768 ? n.T : 768, rows4 = n.T < 8192 ? (n.T + 3) / 4 : 2048;
   if (need <= 1) k_norm<E, 1, 1><<<(unsigned)rows4, 256, 0, st>>>(n);
   else if (need <= 2) k_norm<E, 1, 2><<<(unsigned)rows4, 256, 0, st>>>(n);
-  else if (need <= 4) k_norm<E, 1, 4><<<(unsigned)rows4, 256, 0, st>>>(n);
+  else if (need <= 4) k_norm<E, 4, 1><<<(unsigned)rows, 256, 0, st>>>(n);
   else if (need <= 8) k_norm<E, 4, 2><<<(unsigned)rows, 256, 0, st>>>(n);
-  else if (need <= 16) k_norm<E, 4, 4><<<(unsigned)rows, 256, 0, st>>>(n);
+  else if (need <= 16) k_norm<E, 8, 2><<<(unsigned)wide, 512, 0, st>>>(n);
   else if (need <= 24) k_norm<E, 8, 3><<<(unsigned)wide, 512, 0, st>>>(n);
   else k_norm<E, 8, 4><<<(unsigned)wide, 512, 0, st>>>(n);
 }
