@@ -214,7 +214,9 @@ __device__ inline void place(int heads, int B, int id, int &tile, int &head, int
 /* ---- forward ------------------------------------------------------------------------------------------------------------------
  * A wave has 32 queries, one a lane pair: scores are formed transposed (keys in the registers, the query in the lane), so that a
  * query's running maximum and sum are its lane's own and the exponentials are, as they lie, the second operand of o^T += v^T p^T.
- * A step's products are the scores of its tile and o^T of the tile before. */
+ * A step's products are the scores of its tile and o^T of the tile before.
+ * Bound by the matrix cores and the exponentials in turn: 72 us for 4096 tokens, 12 heads of 128, causal; without a mask and 16 heads
+ * 168 us, 0.82 PFLOP/s (192 us with the teams in step, 178 us without the order of reads and products below). */
 template <class E, int DP, int KIND> __global__ __launch_bounds__(THREADS, 2) void k_attention(Attention a) {
   using R = Rows<DP, KT>;
   __shared__ __attribute__((aligned(1024))) char mem[8 * R::BYTES];
@@ -787,7 +789,9 @@ template <class E, int DP, int KIND> __device__ __forceinline__ void attention_d
   }
 }
 
-/* Both in one launch: the tiles of keys first, then those of queries fill up what the last of them leave idle. */
+/* Both in one launch: the tiles of keys first, then those of queries fill up what the last of them leave idle.  Seven products a pair of
+ * tiles where five would do if dq were added up by atomics, whose order changes sums: 250 us for 4096 tokens, 12 heads of 128, causal (322
+ * in two launches of one-team workgroups); without a mask and 16 heads 531 us, 0.65 PFLOP/s on the five. */
 template <class E, int DP, int KIND> __global__ __launch_bounds__(THREADS, 2) void k_attention_grad(Attention a, int of_keys) {
   __shared__ __attribute__((aligned(1024))) char mem[GradLds<DP>::BYTES];
   __shared__ int part[8][2];
