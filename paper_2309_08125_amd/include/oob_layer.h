@@ -33,7 +33,9 @@ enum { OOB_BF16 = 0, OOB_FP16 = 1, OOB_FP32 = 2 };
 /* ---- matrix product with bias, activation and residual --------------------------------------
  * z = x w^T + bias;  y = act(z) + residual.
  *   x [T][K], w [N][K], bias [N] or NULL, residual [T][N] or NULL (may be y itself, with its stride),
- *   y [T][N] out, z [T][N] out or NULL: what the backward pass needs where act is not NONE */
+ *   y [T][N] out, z [T][N] out or NULL: what the backward pass needs where act is not NONE
+ * RELU max(z, 0); GELU z Phi(z), by the error function; GELU_TANH its form with tanh(sqrt(2 / pi) (z +
+ * 0.044715 z^3)); SILU z / (1 + e^-z). */
 enum { OOB_ACT_NONE = 0, OOB_ACT_RELU = 1, OOB_ACT_GELU = 2, OOB_ACT_GELU_TANH = 3, OOB_ACT_SILU = 4, OOB_ACTS = 5 };
 
 typedef struct oob_linear {

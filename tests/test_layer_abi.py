@@ -42,7 +42,7 @@ def test_linear_refuses(bad):
 
 
 def test_linear_workspaces():
-    lib().oob_layer_linear(None, None, 0, None) == P.OOB_EINVAL
+    assert lib().oob_layer_linear(None, None, 0, None) == P.OOB_EINVAL
     ok = make(L.oob_linear, **LINEAR)
     assert lib().oob_layer_linear(C.byref(ok), FAKE + 8, 1 << 40, None) == P.OOB_EINVAL  # workspace off 256 bytes
     odd = make(L.oob_linear, **{**LINEAR, "K": 7, "x_stride": 7, "w_stride": 7})        # rows that do not start at 16 bytes: packed
