@@ -110,8 +110,9 @@ int oob_layer_norm_backward(const oob_norm *p, const oob_norm_grad *g, void *wor
  * such ranges.
  *   s_ij = scale q_i . k_j;  cap > 0: s_ij = cap tanh(s_ij / cap);  slopes [H] (or NULL): s_ij -= slope_h
  *   |i + Sk - Sq - j|;  o_i = sum_j softmax_j(s_ij) v_j;  lse_i = log sum_j e^s_ij
- * A query that sees no key has o = 0, lse = -inf and no part in any gradient, whatever it holds.  Keys that no
- * query of a tile of 128 sees are not read; others have to be finite, also for queries that do not see them.
+ * A query that sees no key has o = 0, lse = -inf and no part in any gradient, whatever it holds.  Keys that none of the
+ * queries 128 t .. 128 t + 127 sees have no part in theirs, whatever they hold; others have to be finite, also for the
+ * queries among those that do not see them.
  * q, o [B][Sq][H][D], k, v [B][Sk][G][D]: strides of a sequence, a row and a head, the last axis
  * contiguous. */
 #define OOB_ATTENTION_MAX_D 128

@@ -344,8 +344,8 @@ def attention(q, k, v, scale=None, causal=False, key_begin=None, key_end=None, s
     q [B, Sq, H, D], k, v [B, Sk, G, D] of any strides with a contiguous last axis, H a multiple of G; bfloat16 or float16, D up to
     128.  scale: D ** -0.5 where None.  key_begin, key_end: int32 [B, Sq] or None; document, prefix and window masks are such ranges
     (document_ranges, prefix_ranges).  slopes: float32 [H] or None; cap 0: none.  A query that sees no key gets 0 and lse -inf,
-    whatever it holds; keys that no query of a 128-row tile sees may hold anything, others have to be finite.  lse [B, H, Sq] in
-    float32 goes to attention_backward."""
+    whatever it holds; keys that no query of a 128-row tile sees (between those that it does, too) may hold anything, others have to be
+    finite.  lse [B, H, Sq] in float32 goes to attention_backward."""
     _load()
     if not (q.dim() == 4):
         raise ValueError("q: [batch, length, heads, width]")

@@ -1,0 +1,58 @@
+"""The operators of a transformer layer where values are extreme, masked or missing."""
+import pytest
+import torch
+
+from test_gpu_layer import HALF, P, attention_case, rand, tell  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def ranges(B, S, spans):
+    """key_begin, key_end [B, S] from (first query, behind the last, first key, behind the last); the others see nothing."""
+    begin, end = torch.zeros(2, B, S, dtype=torch.int32)
+    for q0, q1, k0, k1 in spans:
+        begin[:, q0:q1], end[:, q0:q1] = k0, k1
+    return begin.cuda(), end.cuda()
+
+
+# ---- attention: keys between the ranges of a tile's queries ---------------------------------------------------
+PADDED = [(0, 40, 0, 40), (64, 100, 64, 100), (128, 190, 128, 190), (192, 193, 192, 193), (256, 300, 256, 300)]  # documents, each padded to 64s
+SCATTERED = [(0, 1, 3, 4), (1, 2, 290, 300), (2, 5, 70, 71), (5, 130, 128, 160), (130, 300, 0, 300)]  # holes of any size; a tile that sees all
+LONE = [(17, 18, 100, 101), (200, 201, 63, 65)]  # hardly anything seen at all
+
+
+@pytest.mark.parametrize("spans", [PADDED, SCATTERED, LONE])
+@pytest.mark.parametrize("D", [64, 80, 128])
+@pytest.mark.parametrize("poison", [float("nan"), float("inf"), -float("inf")])
+def test_attention_keys_that_no_query_of_a_tile_sees(P, poison, D, spans):
+    B, S, H, G = 2, 300, 4, 2
+    begin, end = ranges(B, S, spans)
+    if spans is SCATTERED:  # the second tile's queries see everything: the first's alone
+        begin[:, 128:], end[:, 128:] = 0, 0
+    seen = torch.zeros(S, dtype=torch.bool, device="cuda")
+    for b, e in zip(begin[0].tolist(), end[0].tolist()):
+        seen[b:e] = True
+    sees = (end > begin)[0]
+    for t in HALF:
+        q, do = rand(B, S, H, D, t=t), rand(B, S, H, D, t=t)
+        k, v = rand(B, S, G, D, t=t), rand(B, S, G, D, t=t)
+        results = []
+        for value in (0.0, poison):
+            for a in (k, v):
+                a[:, ~seen] = value
+            for a in (q, do):
+                a[:, ~sees] = value
+            for kind in ({}, dict(causal=True, slopes=torch.full((H,), 0.1, device="cuda"), cap=9.0)):
+                o, lse = P.attention(q, k, v, key_begin=begin, key_end=end, **kind)
+                results.append((o, lse, *P.attention_backward(do, q, k, v, o, lse, key_begin=begin, key_end=end, **kind)))
+        for clean, dirty in zip(results[:2], results[2:]):
+            assert all(torch.equal(a, b) for a, b in zip(clean, dirty)) and all(torch.isfinite(a).all() for a in (dirty[0], *dirty[2:]))
+            assert not dirty[3][:, ~seen].any() and not dirty[4][:, ~seen].any() and not dirty[0][:, ~sees].any() and not dirty[2][:, ~sees].any()
+
+
+@pytest.mark.parametrize("spans", [PADDED, SCATTERED, LONE])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_ranges_with_holes(P, D, spans):
+    begin, end = ranges(1, 300, spans)
+    attention_case(P, 1, 300, 300, 4, 2, D, torch.bfloat16, begin=begin, end=end)
+    attention_case(P, 1, 300, 300, 2, 2, D, torch.float16, begin=begin, causal=True, slopes=True)
