@@ -1,5 +1,6 @@
 /* Matrix products of a transformer layer: y = act(x W^T + b) + r, and its gradients. */
 #include "oob_layer_device.h"
+#include "oob_layer_sizes.h"
 
 namespace layer {
 
@@ -23,8 +24,6 @@ struct Product {
   int full, rest;
   int tiles_m, tiles_n;
 };
-
-constexpr int KSTEP = 64; /* depth of a step: 128-byte rows of k */
 
 /* 1 / (1 + e^-x).  The reciprocal instruction (1 unit of 2^-23) in place of a division, which is ten: results are rounded to 16 bits. */
 __device__ inline float sigmoid(float x) { return __builtin_amdgcn_rcpf(1 + __builtin_amdgcn_exp2f(x * -1.44269504f)); }
@@ -352,37 +351,20 @@ template <class E> __global__ __launch_bounds__(256) void k_sum_rows(const float
 /* ---- host ------------------------------------------------------------------------------------------------------------------ */
 struct Operand { const void *p; int64_t ld, rows, cols; }; /* stored rows x cols, ld elements apart */
 
-/* What the loads to LDS can take: 16-byte pieces of rows that end with the row, offsets within a tile below 2^31. */
+/* What the loads to LDS can take: 16-byte pieces of rows that end with the row, no long way between rows. */
 static bool loadable(const Operand &o) { return o.cols % 8 == 0 && multiple(o.p, 16) && o.ld % 8 == 0 && o.ld < (1 << 21); }
 
-struct Shape { int tile, splits, full, rest; };
-
-/* Which tile, and which tiles' k is split into how many parts.  The large tile reads half as much per product as the middle one (4096 x
- * 12288 x 6144: 497 against 565 us), a workgroup of it takes a compute unit.  What is left of the last round of 256 is split so that all
- * units share it (4096 x 6144 x 12288, 384 tiles: 571 us in two rounds, 518 us in one and a half and the join).  Below that the middle tile,
- * two workgroups a unit (4096 x 8192 x 2048: 163 us, the small one 245); where neither gives most units one, the small tile with k split
- * until there are two workgroups a unit and no part has under four steps (1024 x 2048 x 2048: 19 us, the middle one 26). */
-static Shape choose(int64_t M, int64_t N, int64_t K) {
-  auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
-  int64_t steps = (K + KSTEP - 1) / KSTEP, n = tiles(256), rest = n % 256;
-  int64_t s = rest ? 256 / rest : 1;
-  if (s > steps / 40) s = steps / 40; /* a part of fewer steps costs less than its join */
-  if (s > 8) s = 8;
-  if (rest && s >= 2 && (n > 256 || rest * s >= 192)) return {256, (int)s, (int)(n - rest), (int)rest};
-  if (n >= 192) return {256, 1, (int)n, 0};
-  n = tiles(128);
-  if (n >= 192) return {128, 1, (int)n, 0};
-  n = tiles(64), s = 1;
-  while (n * s < 512 && steps / (s * 2) >= 4 && s < 32) s *= 2;
-  return s == 1 ? Shape{64, 1, (int)n, 0} : Shape{64, (int)s, 0, (int)n};
-}
 static size_t partial_bytes(const Shape &s) { return s.rest ? (size_t)s.splits * s.rest * s.tile * s.tile * 4 : 0; }
 
-static size_t product_workspace(const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K) {
+/* As the product meets it: itself or its copy, ak: k contiguous. */
+static Extent extent(const Operand &o, bool k_contiguous) { return {k_contiguous, o.rows, loadable(o) ? o.ld : up(o.cols, 8)}; }
+static int largest_tile(const Operand &a, bool ak, const Operand &b, bool bk) { return largest_tile(extent(a, ak), extent(b, bk)); }
+
+static size_t product_workspace(const Operand &a, bool ak, const Operand &b, bool bk, int64_t M, int64_t N, int64_t K) {
   Arena w{nullptr, 0, 0};
   if (!loadable(a)) w.take((size_t)a.rows * up(a.cols, 8) * 2);
   if (!loadable(b)) w.take((size_t)b.rows * up(b.cols, 8) * 2);
-  Shape s = choose(M, N, K);
+  Shape s = choose(M, N, K, largest_tile(a, ak, b, bk));
   w.take(partial_bytes(s));
   return w.used;
 }
@@ -409,7 +391,9 @@ template <class E, bool AK, bool BK> static void launch(const Product &g, int ti
  * takes is free again for the next on the stream, as the workspace's size has it. */
 template <class E> static int product(Operand a, bool ak, Operand b, bool bk, Product g, Arena w, hipStream_t st) {
   if (g.M == 0 || g.N == 0) return OOB_OK;
-  Shape s = choose(g.M, g.N, g.K);
+  int largest = largest_tile(a, ak, b, bk);
+  if (!largest) return OOB_EINVAL;
+  Shape s = choose(g.M, g.N, g.K, largest);
   a = pack(a, w, st);
   b = pack(b, w, st);
   g.A = a.p, g.lda = a.ld, g.B = b.p, g.ldb = b.ld;
@@ -438,7 +422,7 @@ static int64_t runs_of(int64_t T, int64_t N) { /* runs of rows of k_act_grad: ab
 }
 
 static size_t linear_bytes(const oob_linear *p) {
-  return product_workspace({p->x, p->x_stride, p->T, p->K}, {p->w, p->w_stride, p->N, p->K}, p->T, p->N, p->K);
+  return product_workspace({p->x, p->x_stride, p->T, p->K}, true, {p->w, p->w_stride, p->N, p->K}, true, p->T, p->N, p->K);
 }
 
 template <class E> static int linear(const oob_linear *p, Arena w, hipStream_t st) {
@@ -458,12 +442,23 @@ static Operand dz_of(const oob_linear_grad *p, Arena &w) {
   return {w.take((size_t)p->T * ld * 2), ld, p->T, ld};
 }
 
+/* Whether the products' loads reach their rows. */
+static bool rows_ok(const oob_linear *p) {
+  return largest_tile({p->x, p->x_stride, p->T, p->K}, true, {p->w, p->w_stride, p->N, p->K}, true) > 0;
+}
+static bool rows_ok(const oob_linear_grad *p) {
+  Arena none{nullptr, 0, 0};
+  Operand dz = dz_of(p, none);
+  return (!p->dx || !p->T || largest_tile(dz, true, {p->w, p->w_stride, p->N, p->K}, false) > 0) &&
+         (!p->dw || largest_tile(dz, false, {p->x, p->x_stride, p->T, p->K}, false) > 0);
+}
+
 static size_t grad_bytes(const oob_linear_grad *p) {
   Arena w{nullptr, 0, 0};
   Operand dz = dz_of(p, w);
   if (p->db) w.take((size_t)runs_of(p->T, p->N) * p->N * 4);
-  size_t dx = p->dx ? product_workspace(dz, {p->w, p->w_stride, p->N, p->K}, p->T, p->K, p->N) : 0;
-  size_t dw = p->dw ? product_workspace(dz, {p->x, p->x_stride, p->T, p->K}, p->N, p->K, p->T) : 0;
+  size_t dx = p->dx ? product_workspace(dz, true, {p->w, p->w_stride, p->N, p->K}, false, p->T, p->K, p->N) : 0;
+  size_t dw = p->dw ? product_workspace(dz, false, {p->x, p->x_stride, p->T, p->K}, false, p->N, p->K, p->T) : 0;
   return w.used + (dx > dw ? dx : dw);
 }
 
@@ -519,7 +514,7 @@ extern "C" int oob_layer_linear(const oob_linear *p, void *workspace, size_t byt
   if (!p->x || !p->w || !p->y || p->x_stride < p->K || p->w_stride < p->K || p->y_stride < p->N) return OOB_EINVAL;
   if ((p->residual && p->residual_stride < p->N) || (p->z && p->z_stride < p->N)) return OOB_EINVAL;
   if (!even(p->x) || !even(p->w) || !even(p->y) || !even(p->bias) || !even(p->residual) || !even(p->z)) return OOB_EINVAL;
-  if (!multiple(workspace, 256)) return OOB_EINVAL;
+  if (!rows_ok(p) || !multiple(workspace, 256)) return OOB_EINVAL;
   size_t need = linear_bytes(p);
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
   Arena w{(char *)workspace, bytes, 0};
@@ -537,7 +532,7 @@ extern "C" int oob_layer_linear_backward(const oob_linear_grad *p, void *workspa
   if (p->T && p->dx && (!p->w || p->w_stride < p->K || p->dx_stride < p->K)) return OOB_EINVAL;
   if (p->dw && ((p->T && (!p->x || p->x_stride < p->K)) || p->dw_stride < p->K)) return OOB_EINVAL;
   if (!even(p->dy) || !even(p->x) || !even(p->w) || !even(p->z) || !even(p->dx) || !even(p->dw) || !even(p->db)) return OOB_EINVAL;
-  if (!multiple(workspace, 256)) return OOB_EINVAL;
+  if (!rows_ok(p) || !multiple(workspace, 256)) return OOB_EINVAL;
   size_t need = grad_bytes(p);
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
   Arena w{(char *)workspace, bytes, 0};

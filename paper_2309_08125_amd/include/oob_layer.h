@@ -34,13 +34,15 @@ enum { OOB_BF16 = 0, OOB_FP16 = 1, OOB_FP32 = 2 };
  * z = x w^T + bias;  y = act(z) + residual.
  *   x [T][K], w [N][K], bias [N] or NULL, residual [T][N] or NULL (may be y itself, with its stride),
  *   y [T][N] out, z [T][N] out or NULL: what the backward pass needs where act is not NONE
+ * Rows of below 2^24 values are accepted whatever their number.  Longer ones of x, w, and for the gradients dy: as long as the first 64
+ * of them (fewer, where there are fewer), each rounded up to 8 values, lie within 2^31 bytes; otherwise OOB_EINVAL.
  * RELU max(z, 0); GELU z Phi(z), by the error function; GELU_TANH its form with tanh(sqrt(2 / pi) (z +
  * 0.044715 z^3)); SILU z / (1 + e^-z). */
 enum { OOB_ACT_NONE = 0, OOB_ACT_RELU = 1, OOB_ACT_GELU = 2, OOB_ACT_GELU_TANH = 3, OOB_ACT_SILU = 4, OOB_ACTS = 5 };
 
 typedef struct oob_linear {
   int dtype, act;          /* OOB_BF16 or OOB_FP16; OOB_ACT_* */
-  int64_t T, N, K;         /* T >= 0, N, K >= 1, each below 2^31 */
+  int64_t T, N, K;         /* T >= 0, N, K >= 1, each below 2^31 (see below for long rows) */
   const void *x, *w, *bias, *residual;
   void *y, *z;
   int64_t x_stride, w_stride, residual_stride, y_stride, z_stride;
