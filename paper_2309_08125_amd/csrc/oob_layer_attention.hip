@@ -901,8 +901,8 @@ static bool attention_ok(const oob_attention *p) {
   if ((p->dtype != OOB_BF16 && p->dtype != OOB_FP16) || p->B < 0 || p->Sq < 0 || p->Sk < 0 || p->H < 1 || p->G < 1 || p->H % p->G != 0) return false;
   if (p->D < 1 || p->D > OOB_ATTENTION_MAX_D || p->Sq >= (1 << 29) || p->Sk >= (1 << 29)) return false;
   if (!(p->scale > 0) || !(p->cap >= 0) || !(p->scale < INFINITY) || !(p->cap < INFINITY)) return false;
-  int64_t wgs = (int64_t)p->B * p->H * ((p->Sq > p->Sk ? p->Sq : p->Sk) / 16 + 1);
-  if (wgs >= ((int64_t)1 << 31)) return false;
+  const int64_t most = (int64_t)1 << 31, heads = (int64_t)p->B * p->H, wgs = (p->Sq > p->Sk ? p->Sq : p->Sk) / 16 + 1;
+  if (heads >= most || heads * wgs >= most) return false;
   for (const int64_t(*s)[3] : {&p->q_stride, &p->k_stride, &p->v_stride, &p->o_stride})
     for (int i = 0; i < 3; i++)
       if ((*s)[i] < 0) return false;

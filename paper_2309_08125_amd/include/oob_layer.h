@@ -121,7 +121,7 @@ int oob_layer_norm_backward(const oob_norm *p, const oob_norm_grad *g, void *wor
 
 typedef struct oob_attention {
   int dtype;                    /* OOB_BF16 or OOB_FP16 */
-  int B, Sq, Sk, H, G, D;       /* B, Sq, Sk >= 0 (below 2^29); H a multiple of G >= 1; 1 <= D <= 128 */
+  int B, Sq, Sk, H, G, D;       /* B, Sq, Sk >= 0, Sq, Sk below 2^29; H a multiple of G >= 1; 1 <= D <= 128; B H (max(Sq, Sk) / 16 + 1) below 2^31 */
   int causal;
   float scale, cap;             /* scale > 0; cap 0: none */
   const void *q, *k, *v;

@@ -7,7 +7,7 @@ import pytest
 
 import paper_2309_08125_amd as P
 from paper_2309_08125_amd import layer as L
-from test_layer_abi import FAKE, LINEAR, lib, make
+from test_layer_abi import FAKE, LINEAR, attention, lib, make
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2309_08125_amd", "csrc")
 WRAPPERS = r"""
@@ -66,3 +66,11 @@ def test_rows_that_the_loads_do_not_reach_are_refused():
                 dict(K=long, x_stride=long, dw_stride=long, dw=FAKE), dict(N=long, dy_stride=long, z=FAKE, z_stride=long, act=3, dx=FAKE)):
         g = make(L.oob_linear_grad, **{**grad, **bad})
         assert lib().oob_layer_linear_backward(C.byref(g), FAKE, 1 << 50, None) == P.OOB_EINVAL, bad
+
+
+@pytest.mark.parametrize("bad", [dict(B=1 << 30, H=1 << 30, G=1, Sq=240, Sk=8), dict(B=1 << 29), dict(B=(1 << 31) - 1), dict(B=1 << 15, H=1 << 16, G=1)])
+def test_attention_sizes_whose_products_pass_their_integers_are_refused(bad):
+    """The first passes 64 bits to the very 0."""
+    p = attention(**bad)
+    assert lib().oob_layer_attention(C.byref(p), FAKE, 1 << 62, None) == P.OOB_EINVAL
+    assert lib().oob_layer_attention_workspace_size(C.byref(p)) == 0
