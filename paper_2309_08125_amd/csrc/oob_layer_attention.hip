@@ -886,6 +886,8 @@ static Heads heads_of(const void *p, const int64_t (&stride)[3]) { return {(cons
 static bool loadable(const Heads &h, int D) {
   return D % 8 == 0 && multiple(h.p, 16) && h.batch % 16 == 0 && h.row % 16 == 0 && h.head % 16 == 0 && h.row < (1 << 24);
 }
+/* Whether the loads' 32-bit offsets (up to 31 rows of a lane's own, 48 beside the bounds) reach the rows, copied where they have to be. */
+static bool reachable(const Heads &h, int S, int N, int D) { return loadable(h, D) || (S < 32 ? S : 32) * (N * up(D, 8) * 2) < (int64_t)1 << 31; }
 static size_t packed_bytes(int B, int S, int N, int D) { return (size_t)B * S * N * up(D, 8) * 2; }
 
 static void pack(Heads &h, int B, int S, int N, int D, Arena &w, hipStream_t st) {
@@ -925,6 +927,15 @@ template <class F> static void by_kind(const Attention &a, F f) {
   else if (a.cap > 0) f(Int<CAP>());
   else if (a.slopes) f(Int<BIAS>());
   else f(Int<0>());
+}
+
+static bool rows_ok(const oob_attention *p) {
+  Attention a = attention_of(p);
+  return reachable(a.k, a.Sk, a.G, a.D) && reachable(a.v, a.Sk, a.G, a.D);
+}
+static bool rows_ok(const oob_attention *p, const oob_attention_grad *q) {
+  Attention a = attention_of(p);
+  return rows_ok(p) && reachable(a.q, a.Sq, a.H, a.D) && reachable(heads_of(q->dout, q->dout_stride), a.Sq, a.H, a.D);
 }
 
 static size_t forward_bytes(const oob_attention *p) {
@@ -1017,7 +1028,7 @@ extern "C" size_t oob_layer_attention_workspace_size(const oob_attention *p) { r
 extern "C" int oob_layer_attention(const oob_attention *p, void *workspace, size_t bytes, void *stream) {
   if (!p || !attention_ok(p) || !multiple(workspace, 256)) return OOB_EINVAL;
   if (p->B == 0 || p->Sq == 0) return OOB_OK;
-  if (!p->q || !p->o || (p->Sk > 0 && (!p->k || !p->v))) return OOB_EINVAL;
+  if (!p->q || !p->o || (p->Sk > 0 && (!p->k || !p->v)) || !rows_ok(p)) return OOB_EINVAL;
   size_t need = forward_bytes(p);
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
   Arena w{(char *)workspace, bytes, 0};
@@ -1031,6 +1042,7 @@ extern "C" size_t oob_layer_attention_backward_workspace_size(const oob_attentio
 extern "C" int oob_layer_attention_backward(const oob_attention *p, const oob_attention_grad *q, void *workspace, size_t bytes, void *stream) {
   if (!p || !q || !attention_ok(p) || !grads_ok(p, q) || !multiple(workspace, 256)) return OOB_EINVAL;
   if (p->B == 0) return OOB_OK;
+  if (!rows_ok(p, q)) return OOB_EINVAL;
   size_t need = backward_bytes(p, q);
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
   Arena w{(char *)workspace, bytes, 0};

@@ -74,3 +74,18 @@ def test_attention_sizes_whose_products_pass_their_integers_are_refused(bad):
     p = attention(**bad)
     assert lib().oob_layer_attention(C.byref(p), FAKE, 1 << 62, None) == P.OOB_EINVAL
     assert lib().oob_layer_attention_workspace_size(C.byref(p)) == 0
+
+
+def test_attention_heads_whose_copies_the_loads_do_not_reach_are_refused():
+    """2^19 heads of 128 values: copied rows of 2^27 bytes, 40 of them.  The backward pass reads q and dout the same way."""
+    N, odd = 1 << 19, (1 << 30, (1 << 26) + 1, 128)
+    sizes = dict(B=1, Sq=40, Sk=40, H=N, D=128)
+    for bad in (dict(G=N, k_stride=odd), dict(G=N, v_stride=odd)):
+        p = attention(**sizes, **bad)
+        assert lib().oob_layer_attention(C.byref(p), FAKE, 1 << 62, None) == P.OOB_EINVAL, bad
+    strides = lambda *s: [(C.c_int64 * 3)(*x) for x in s]  # noqa: E731
+    even = (1 << 30, 128 * 8, 128)
+    for bad, dout in ((dict(q_stride=odd), even), ({}, odd)):
+        p = attention(**sizes, G=1, **bad)
+        g = L.oob_attention_grad(FAKE, FAKE, FAKE, FAKE, *strides(dout, even, even, even))
+        assert lib().oob_layer_attention_backward(C.byref(p), C.byref(g), FAKE, 1 << 62, None) == P.OOB_EINVAL, (bad, dout)
