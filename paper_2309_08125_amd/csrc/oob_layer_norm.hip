@@ -153,6 +153,9 @@ template <class E, int WAVES, int V> __global__ __launch_bounds__(WAVES < 4 ? 25
   }
 }
 
+/* From a variance that its rounding may have made negative; a NaN stays one (fmaxf would give 0). */
+__device__ inline float inverse_deviation(float variance, float eps) { return 1 / sqrtf((variance < 0 ? 0.f : variance) + eps); }
+
 /* Backward.  With xhat = (x' - mean) rstd and c = dh w:  d = dx' + rstd (c - mean(c) - xhat mean(c xhat))  (rms: without mean(c)),
  * dx = alpha d, dw = sum dh xhat, db = sum dh.  Behind it, where there is more than the residual sum: du = d gate keep, dgate = sum d u,
  * and the norm behind the block the same way from zhat.  A workgroup takes a run of rows and keeps the sums of its columns in registers. */
@@ -204,12 +207,12 @@ template <class E, int WAVES, int V, bool POST, bool GATE> __global__ __launch_b
     }
     sum_row<WAVES, POST ? 6 : 4>(s, part, turn);
     float shift = n.pre == OOB_NORM_LAYER ? s[0] / C : 0.f;
-    float rstd = 1 / sqrtf(fmaxf(s[1] / C - shift * shift, 0.f) + n.eps);
+    float rstd = inverse_deviation(s[1] / C - shift * shift, n.eps);
     float m0 = n.pre == OOB_NORM_LAYER ? s[2] / C : 0.f, m1 = rstd * (s[3] - shift * s[2]) / C;
     float pshift = 0, prstd = 0, q[2] = {0, 0}; /* the norm behind the block: its mean without the rounding to one number, as above */
     if (POST) {
       pshift = n.post == OOB_NORM_LAYER ? s[4] / C : 0.f;
-      prstd = 1 / sqrtf(fmaxf(s[5] / C - pshift * pshift, 0.f) + n.eps);
+      prstd = inverse_deviation(s[5] / C - pshift * pshift, n.eps);
     }
     for (int k = 0; k < V; k++) {
       int64_t c = c0 + k * WAVES * 512;

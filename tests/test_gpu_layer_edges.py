@@ -56,3 +56,30 @@ def test_attention_ranges_with_holes(P, D, spans):
     begin, end = ranges(1, 300, spans)
     attention_case(P, 1, 300, 300, 4, 2, D, torch.bfloat16, begin=begin, end=end)
     attention_case(P, 1, 300, 300, 2, 2, D, torch.float16, begin=begin, causal=True, slopes=True)
+
+
+# ---- NaN in, NaN out ----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("t", HALF + [torch.float32])
+@pytest.mark.parametrize("C", [64, 1000, 9000])
+def test_norm_gradients_of_a_row_that_holds_a_nan(P, C, t):
+    """xhat of the row is NaN in every column: so are the weights' gradients, which add it up; other rows do not see it."""
+    T, bad = 5, 2
+    x, z, w, pw, dh = rand(T, C, t=t), rand(T, C, t=t), rand(C, t=t, mean=1.0), rand(C, t=t, mean=1.0), rand(T, C, t=t)
+    for pre in ("rms", "layer"):
+        kind = dict(weight=w, pre=pre)
+        _, _, saved = P.residual_norm(x, **kind)
+        clean = P.residual_norm_backward(None, dh, x, None, saved, **kind)
+        y = x.clone()
+        y[bad, C // 3] = float("nan")
+        _, h, saved = P.residual_norm(y, **kind)
+        d = P.residual_norm_backward(None, dh, y, None, saved, **kind)
+        assert torch.isnan(h[bad]).all() and torch.isnan(d["x"][bad]).all() and torch.isnan(d["weight"]).all()
+        rest = [i for i in range(T) if i != bad]
+        assert torch.equal(d["x"][rest], clean["x"][rest])
+    for post in ("rms", "layer"):  # the norm behind the block alone: the stream stays finite
+        kind = dict(weight=w, post=post, post_weight=pw)
+        xp, _, saved = P.residual_norm(x, z, **kind)
+        y = z.clone()
+        y[bad, C // 3] = float("nan")
+        d = P.residual_norm_backward(None, dh, xp, y, saved, **kind)
+        assert torch.isnan(d["post_weight"]).all() and torch.isnan(d["z"][bad]).all() and torch.isfinite(d["weight"]).all()
