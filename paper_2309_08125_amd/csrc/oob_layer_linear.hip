@@ -41,7 +41,7 @@ __device__ inline float activate(float z, int act) {
 /* act'(z) */
 __device__ inline float slope(float z, int act) {
   switch (act) {
-    case OOB_ACT_RELU: return z > 0 ? 1.f : 0.f;
+    case OOB_ACT_RELU: return z > 0 ? 1.f : (z != z ? z : 0.f);
     case OOB_ACT_SILU: { float e = sigmoid(z); return e * (1 + z * (1 - e)); }
     case OOB_ACT_GELU: return 0.5f * (1 + erff(z * 0.70710678f)) + z * 0.39894228f * __expf(-0.5f * z * z);
     case OOB_ACT_GELU_TANH: {

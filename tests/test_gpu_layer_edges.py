@@ -83,3 +83,12 @@ def test_norm_gradients_of_a_row_that_holds_a_nan(P, C, t):
         y[bad, C // 3] = float("nan")
         d = P.residual_norm_backward(None, dh, xp, y, saved, **kind)
         assert torch.isnan(d["post_weight"]).all() and torch.isnan(d["z"][bad]).all() and torch.isfinite(d["weight"]).all()
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_linear_gradients_of_a_nan(P, act):
+    x, w, z, dy = rand(3, 16), rand(24, 16), rand(3, 24), rand(3, 24)
+    z[1, 5] = float("nan")
+    dx, dw, db = P.linear_backward(dy, x, w, z, act=act)
+    assert torch.isnan(dx[1]).all() and torch.isfinite(dx[[0, 2]]).all()
+    assert torch.isnan(dw[5]).all() and torch.isnan(db[5]) and int(torch.isnan(db).sum()) == 1
