@@ -38,8 +38,10 @@ __device__ inline float activate(float z, int act) {
   }
 }
 
-/* act'(z) */
+/* act'(z).  Beyond +-1000 the smooth ones are 1 and 0 to the last bit, and their formulas would meet 0 times infinity: z of float16 is an
+ * infinity from 65520 on, its square one of bfloat16 from 2^64 on. */
 __device__ inline float slope(float z, int act) {
+  if (act != OOB_ACT_NONE && act != OOB_ACT_RELU) z = __builtin_elementwise_minimum(__builtin_elementwise_maximum(z, -1000.f), 1000.f); /* NaN stays */
   switch (act) {
     case OOB_ACT_RELU: return z > 0 ? 1.f : (z != z ? z : 0.f);
     case OOB_ACT_SILU: { float e = sigmoid(z); return e * (1 + z * (1 - e)); }

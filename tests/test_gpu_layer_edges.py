@@ -92,3 +92,25 @@ def test_linear_gradients_of_a_nan(P, act):
     dx, dw, db = P.linear_backward(dy, x, w, z, act=act)
     assert torch.isnan(dx[1]).all() and torch.isfinite(dx[[0, 2]]).all()
     assert torch.isnan(dw[5]).all() and torch.isnan(db[5]) and int(torch.isnan(db).sum()) == 1
+
+
+# ---- activations where z is large ---------------------------------------------------------------------------
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("t", HALF)
+def test_slope_where_it_is_constant(P, act, t):
+    """1 above, 0 below, as far as z goes: float16 stores a z beyond 65504 as an infinity."""
+    big = torch.tensor([200.0, 60000.0, float("inf")] + ([1e13, 1e20, 3e38] if t == torch.bfloat16 else []), device="cuda").to(t)
+    z = torch.cat([big, -big])[None]
+    dy, x, w = torch.full_like(z, 3.0), rand(1, 8, t=t), rand(z.shape[1], 8, t=t)
+    assert P.linear_backward(dy, x, w, z, act=act)[2].tolist() == [3.0] * len(big) + [0.0] * len(big)
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_linear_whose_z_passes_float16(P, act):
+    x, w = rand(4, 16, t=torch.float16), rand(24, 16, t=torch.float16)
+    x[:, 0], w[:, 0] = 1000.0, torch.where(torch.arange(24) % 2 == 0, -100.0, 0.0).cuda()
+    y, z = P.linear(x, w, act=act, keep=True)
+    assert torch.isinf(z[:, ::2]).all() and not y[:, ::2].any()
+    dy = rand(4, 24, t=torch.float16)
+    for got in P.linear_backward(dy, x, w, z, act=act):
+        assert torch.isfinite(got).all()
