@@ -28,11 +28,29 @@ struct Product {
 /* 1 / (1 + e^-x).  The reciprocal instruction (1 unit of 2^-23) in place of a division, which is ten: results are rounded to 16 bits. */
 __device__ inline float sigmoid(float x) { return __builtin_amdgcn_rcpf(1 + __builtin_amdgcn_exp2f(x * -1.44269504f)); }
 
+/* Phi(z), the normal distribution's, and bell = e^(-z^2 / 2).  Phi(-|z|) = bell t Q(t) with t = 1 / (1 + 0.32 |z|): Q is the polynomial of degree
+ * 7 whose largest relative error over |z| <= 60 is least (4e-7, 8e-7 in 32 bits; found by linear programming on 1500 points).  1 + erf(z / sqrt(2))
+ * has no digit left below z = -5.6, and erfcf takes 92 us for the gradient of 4096 x 6144 (its bias's alone) where this takes 43. */
+__device__ inline float phi(float z, float &bell) {
+  float t = __builtin_amdgcn_rcpf(1 + 0.32f * fabsf(z));
+  float q = 0.03451068627f;
+  q = q * t - 0.12242049668f;
+  q = q * t + 0.10613986935f;
+  q = q * t + 0.01553882127f;
+  q = q * t + 0.09740863787f;
+  q = q * t + 0.11342795430f;
+  q = q * t + 0.12773489272f;
+  q = q * t + 0.12765983351f;
+  bell = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+  float tail = bell * t * q;
+  return z < 0 ? tail : 1 - tail;
+}
+
 __device__ inline float activate(float z, int act) {
   switch (act) {
     case OOB_ACT_RELU: return z > 0 ? z : (z != z ? z : 0.f);
     case OOB_ACT_SILU: return z * sigmoid(z);
-    case OOB_ACT_GELU: return 0.5f * z * (1 + erff(z * 0.70710678f));
+    case OOB_ACT_GELU: { float bell; return z * phi(z, bell); }
     case OOB_ACT_GELU_TANH: return z * sigmoid(1.5957691216f * (z + 0.044715f * z * z * z)); /* 0.5 (1 + tanh(u)) = sigmoid(2 u) */
     default: return z;
   }
@@ -45,7 +63,7 @@ __device__ inline float slope(float z, int act) {
   switch (act) {
     case OOB_ACT_RELU: return z > 0 ? 1.f : (z != z ? z : 0.f);
     case OOB_ACT_SILU: { float e = sigmoid(z); return e * (1 + z * (1 - e)); }
-    case OOB_ACT_GELU: return 0.5f * (1 + erff(z * 0.70710678f)) + z * 0.39894228f * __expf(-0.5f * z * z);
+    case OOB_ACT_GELU: { float bell, p = phi(z, bell); return p + z * 0.39894228f * bell; }
     case OOB_ACT_GELU_TANH: {
       float e = sigmoid(1.5957691216f * (z + 0.044715f * z * z * z)); /* its derivative is 2 e (1 - e) u' */
       return e + z * 2 * e * (1 - e) * 0.7978845608f * (1 + 0.134145f * z * z);

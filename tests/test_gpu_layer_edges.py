@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from layer_oracle import TINY, U, within
 from test_gpu_layer import HALF, P, attention_case, rand, tell  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -114,3 +115,18 @@ def test_linear_whose_z_passes_float16(P, act):
     dy = rand(4, 24, t=torch.float16)
     for got in P.linear_backward(dy, x, w, z, act=act):
         assert torch.isfinite(got).all()
+
+
+@pytest.mark.parametrize("t", HALF)
+def test_gelu_keeps_its_digits(P, t):
+    """Values and slopes relative to themselves, far into the tail: products of one term, so that z is exact."""
+    z = torch.cat([torch.linspace(-6, 6, 777), torch.linspace(-12, -6, 100) if t == torch.bfloat16 else torch.zeros(0)]).cuda().to(t)
+    one = torch.ones(1, 1, device="cuda", dtype=t)
+    y = P.linear(z[:, None], one, act="gelu")[:, 0]
+    Z = z.double()
+    phi = 0.5 * torch.special.erfc(-Z * 0.5 ** 0.5)
+    # the argument's rounding: 2 a^2 2^-23 of erfc(a), a <= 8.5; the rest a few units of 2^-23
+    within(y, Z * phi, (U[t] + 1e-4) * (Z * phi).abs() + TINY[t], "y")
+    slope = P.linear_backward(torch.ones_like(z)[None], one, z[:, None], z[None], act="gelu")[2]
+    bell = Z * torch.exp(-0.5 * Z * Z) / (2 * torch.pi) ** 0.5
+    within(slope, phi + bell, U[t] * (phi + bell).abs() + 1e-4 * (phi + bell.abs()) + TINY[t], "slope")
