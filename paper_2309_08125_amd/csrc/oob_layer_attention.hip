@@ -913,6 +913,9 @@ static bool attention_ok(const oob_attention *p) {
   return multiple(p->key_begin, 4) && multiple(p->key_end, 4) && multiple(p->slopes, 4) && multiple(p->lse, 4);
 }
 
+/* Whether a result's rows are each its own: an axis of stride 0 has them all in one place. */
+static bool apart(const int64_t (&stride)[3], int B, int S, int N) { return (stride[0] || B < 2) && (stride[1] || S < 2) && (stride[2] || N < 2); }
+
 static Attention attention_of(const oob_attention *p) {
   Attention a{};
   a.q = heads_of(p->q, p->q_stride), a.k = heads_of(p->k, p->k_stride), a.v = heads_of(p->v, p->v_stride), a.o = heads_of(p->o, p->o_stride);
@@ -1015,6 +1018,7 @@ static bool grads_ok(const oob_attention *p, const oob_attention_grad *q) {
       if ((*s)[i] < 0) return false;
   for (const void *x : {q->dout, (const void *)q->dq, (const void *)q->dk, (const void *)q->dv})
     if (!multiple(x, 2)) return false;
+  if (!apart(q->dq_stride, p->B, p->Sq, p->H) || !apart(q->dk_stride, p->B, p->Sk, p->G) || !apart(q->dv_stride, p->B, p->Sk, p->G)) return false;
   if (p->B > 0 && p->Sq > 0 && (!p->q || !p->o || !p->lse || !q->dout || !q->dq)) return false;
   return !(p->B > 0 && p->Sk > 0 && (!p->k || !p->v || !q->dk || !q->dv));
 }
@@ -1028,7 +1032,7 @@ extern "C" size_t oob_layer_attention_workspace_size(const oob_attention *p) { r
 extern "C" int oob_layer_attention(const oob_attention *p, void *workspace, size_t bytes, void *stream) {
   if (!p || !attention_ok(p) || !multiple(workspace, 256)) return OOB_EINVAL;
   if (p->B == 0 || p->Sq == 0) return OOB_OK;
-  if (!p->q || !p->o || (p->Sk > 0 && (!p->k || !p->v)) || !rows_ok(p)) return OOB_EINVAL;
+  if (!p->q || !p->o || (p->Sk > 0 && (!p->k || !p->v)) || !rows_ok(p) || !apart(p->o_stride, p->B, p->Sq, p->H)) return OOB_EINVAL;
   size_t need = forward_bytes(p);
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
   Arena w{(char *)workspace, bytes, 0};

@@ -116,7 +116,7 @@ int oob_layer_norm_backward(const oob_norm *p, const oob_norm_grad *g, void *wor
  * queries 128 t .. 128 t + 127 sees have no part in theirs, whatever they hold; others have to be finite, also for the
  * queries among those that do not see them.
  * q, o [B][Sq][H][D], k, v [B][Sk][G][D]: strides of a sequence, a row and a head, the last axis
- * contiguous.  k, v, and for the gradients q and dout, are copied where they do not start at 16 bytes, a stride is no multiple of
+ * contiguous; 0 for an axis of inputs that repeats, not of results (OOB_EINVAL).  k, v, and for the gradients q and dout, are copied where they do not start at 16 bytes, a stride is no multiple of
  * that or D none of 8, or rows lie 2^24 bytes apart; the heads of 32 rows (fewer, where there are fewer) then have to take less than 2^31 bytes. */
 #define OOB_ATTENTION_MAX_D 128
 

@@ -357,8 +357,8 @@ def attention(q, k, v, scale=None, causal=False, key_begin=None, key_end=None, s
 
 
 def attention_backward(do, q, k, v, o, lse, scale=None, causal=False, key_begin=None, key_end=None, slopes=None, cap=0.0, out=None):
-    """(dq, dk, dv) of attention from `do`, the gradient of o.  out: three tensors to write them to, of any strides with a contiguous
-    last axis (the parts of one tensor, say)."""
+    """(dq, dk, dv) of attention from `do`, the gradient of o.  out: three tensors to write them to, of any strides but 0 with a
+    contiguous last axis (the parts of one tensor, say)."""
     _load()
     args = _attention_args(q, k, v, o, lse, scale, causal, key_begin, key_end, slopes, cap)
     B, Sq, H, D = q.shape

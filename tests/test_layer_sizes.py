@@ -89,3 +89,17 @@ def test_attention_heads_whose_copies_the_loads_do_not_reach_are_refused():
         p = attention(**sizes, G=1, **bad)
         g = L.oob_attention_grad(FAKE, FAKE, FAKE, FAKE, *strides(dout, even, even, even))
         assert lib().oob_layer_attention_backward(C.byref(p), C.byref(g), FAKE, 1 << 62, None) == P.OOB_EINVAL, (bad, dout)
+
+
+def test_attention_results_that_lie_on_themselves_are_refused():
+    """Expanded tensors: strides of 0.  Inputs may be such."""
+    for bad in ((0, 64, 16), (512, 0, 16), (512, 64, 0)):
+        p = attention(B=2, o_stride=bad)
+        assert lib().oob_layer_attention(C.byref(p), FAKE, 1 << 40, None) == P.OOB_EINVAL, bad
+        for n in range(3):
+            g = L.oob_attention_grad(FAKE, FAKE, FAKE, FAKE, *[(C.c_int64 * 3)(*(bad if k == n else (512, 64, 16))) for k in (3, 0, 1, 2)])
+            assert lib().oob_layer_attention_backward(C.byref(attention(B=2)), C.byref(g), FAKE, 1 << 40, None) == P.OOB_EINVAL, (bad, n)
+    expanded = attention(B=2, q_stride=(0, 64, 16), k_stride=(0, 0, 16), v_stride=(512, 64, 0))
+    g = L.oob_attention_grad(FAKE, FAKE, FAKE, FAKE, *[(C.c_int64 * 3)(*s) for s in ((0, 0, 0), (512, 64, 16), (512, 64, 16), (512, 64, 16))])
+    assert lib().oob_layer_attention_backward_workspace_size(C.byref(expanded), C.byref(g)) > 0
+    assert lib().oob_layer_attention_workspace_size(C.byref(attention(B=1, o_stride=(0, 64, 16)))) == 0  # one sequence: its stride is not used
