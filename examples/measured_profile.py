@@ -69,22 +69,39 @@ class LayerShare:
         return d["x"], d["z"], grads
 
 
+def captured(layer, x, z, dx, dy, seed=0):
+    """(graph, results) of the forward pass and of the backward pass on these tensors."""
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):  # once outside a graph: libraries and kernels are loaded
+        layer.backward(dx, dy, layer.forward(x, z, seed)[2])
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graphs[0]):
+        out = layer.forward(x, z, seed)
+    with torch.cuda.graph(graphs[1], pool=graphs[0].pool()):
+        grads = layer.backward(dx, dy, out[2])
+    return (graphs[0], out), (graphs[1], grads)
+
+
 def measure(layer, hidden, runs=10):
-    """(forward, backward) of the share in ns."""
+    """(forward, backward) of the share in ns of the GPU: graphs, replayed in a row behind one another, since the calls of a small share
+    take the host longer than their kernels run."""
     x, z, dx, dy = (torch.randn(layer.B, layer.S, hidden, device="cuda").bfloat16() for _ in range(4))
-    marks = [torch.cuda.Event(enable_timing=True) for _ in range(2 * runs + 1)]
-    for k in range(-3, runs):
-        if k == 0:
-            marks[0].record()
-        _, _, kept = layer.forward(x, z, seed=k + 3)
-        if k >= 0:
-            marks[2 * k + 1].record()
-        layer.backward(dx, dy, kept)
-        if k >= 0:
-            marks[2 * k + 2].record()
-    torch.cuda.synchronize()
-    ms = np.array([marks[i].elapsed_time(marks[i + 1]) for i in range(2 * runs)]).reshape(runs, 2)
-    return [int(v * 1e6) for v in np.median(ms, axis=0)]
+    ns = []
+    passes = captured(layer, x, z, dx, dy)
+    for graph, _ in passes:
+        marks = [[torch.cuda.Event(enable_timing=True) for _ in range(2)] for _ in range(3)]
+        for _ in range(3):
+            graph.replay()
+        for first, last in marks:
+            first.record()
+            for _ in range(runs):
+                graph.replay()
+            last.record()
+        torch.cuda.synchronize()
+        ns.append(int(np.median([first.elapsed_time(last) for first, last in marks]) / runs * 1e6))
+    return ns
 
 
 def profile(hidden, heads, layers, gpus, B, S, documents, emb=3, state_bytes=None, runs=10):

@@ -49,3 +49,36 @@ def test_example_measures_and_plans(capsys):
     said = capsys.readouterr().out
     assert res["feasible"].all() and (res["T"] > 0).all()
     assert "layer on 1 GPU(s): forward" in said and "layer on 3 GPU(s): heads do not divide" in said and "2 nodes:" in said
+
+
+def test_profile_is_the_gpus_time_not_the_calls(monkeypatch):
+    """Calls that take the host 2 ms each do not enter: a pass of this share runs for some 0.1 ms."""
+    import time
+
+    import measured_profile as E
+
+    layer = E.LayerShare(128, 4, 2, 1, 64, [[64]])
+    for name in ("residual_norm", "residual_norm_backward"):
+        call = getattr(E.P, name)
+        monkeypatch.setattr(E.P, name, lambda *a, call=call, **k: (time.sleep(2e-3), call(*a, **k))[1])
+    assert all(0 < ns < 2_000_000 for ns in E.measure(layer, 128, runs=5))
+
+
+def test_captured_passes_give_what_the_calls_give():
+    import measured_profile as E
+
+    B, S, C = 2, 96, 128
+    layer = E.LayerShare(C, 4, 2, B, S, [[40, 30], [96]])
+    x, z, dx, dy = (torch.randn(B, S, C, device="cuda").bfloat16() for _ in range(4))
+    (forward, out), (backward, grads) = E.captured(layer, x, z, dx, dy, seed=3)
+    for _ in range(4):
+        for t in (x, z, dx, dy):
+            t.copy_(torch.randn(B, S, C, device="cuda"))
+        want = layer.forward(x, z, 3)
+        want_grads = layer.backward(dx, dy, want[2])
+        torch.cuda.synchronize()
+        forward.replay()
+        backward.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out[:2] + grads[:2], want[:2] + want_grads[:2]))
+        assert all(torch.equal(grads[2][n], g) for n, g in want_grads[2].items())
