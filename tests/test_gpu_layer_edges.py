@@ -3,7 +3,8 @@ import pytest
 import torch
 
 from layer_oracle import TINY, U, within
-from test_gpu_layer import HALF, P, attention_case, rand, tell  # noqa: F401
+from test_gpu_layer import HALF, P, attention_case, linear_case, norm_case, rand, tell  # noqa: F401
+from test_layer_sizes import LARGE
 
 pytestmark = pytest.mark.gpu
 
@@ -130,3 +131,30 @@ def test_gelu_keeps_its_digits(P, t):
     slope = P.linear_backward(torch.ones_like(z)[None], one, z[:, None], z[None], act="gelu")[2]
     bell = Z * torch.exp(-0.5 * Z * Z) / (2 * torch.pi) ** 0.5
     within(slope, phi + bell, U[t] * (phi + bell).abs() + 1e-4 * (phi + bell.abs()) + TINY[t], "slope")
+
+
+# ---- sizes that reach every launch --------------------------------------------------------------------------
+@pytest.mark.parametrize("t", HALF)
+@pytest.mark.parametrize("T,N,K", LARGE)
+def test_linear_tiles(P, T, N, K, t):
+    linear_case(P, T, N, K, "silu" if t == torch.bfloat16 else "none", t)
+
+
+@pytest.mark.parametrize("H,D", [(16, 64), (24, 128), (16, 80)])
+@pytest.mark.parametrize("Sq,Sk", [(130, 130), (20, 130), (33, 200), (200, 33)])
+def test_attention_heads_that_share_keys_in_one_workgroup(P, H, D, Sq, Sk):
+    """From 256 workgroups of keys on, one goes through all heads that share them: teams on different heads where a head has one tile."""
+    B, G = 32, 8
+    assert B * G * -(-Sk // 128) >= 256 and H > G
+    attention_case(P, B, Sq, Sk, H, G, D, torch.bfloat16, causal=True)
+    attention_case(P, B, Sq, Sk, H, G, D, torch.float16, slopes=True, cap=7.0)
+    begin, end = ranges(B, Sq, [(0, 9, 0, 9), (12, 17, 5, 30)] + ([(40, 130, 20, 130), (150, 200, 0, 33)] if Sq > 33 else []))
+    attention_case(P, B, Sq, Sk, H, G, D, torch.bfloat16, begin=begin, end=end)
+
+
+@pytest.mark.parametrize("T,C", [(8300, 130), (8200, 1000), (2100, 1500), (2100, 4000), (900, 4500), (900, 8200), (800, 12296)])
+def test_norm_of_more_rows_than_workgroups(P, T, C):
+    for t in HALF + [torch.float32]:
+        norm_case(P, T, C, t)
+        norm_case(P, T, C, t, pre="rms", post="layer", gates=2, alpha=0.5, p=0.25)
+    norm_case(P, T, C, torch.bfloat16, post="rms", gates=T // 2)

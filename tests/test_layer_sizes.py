@@ -55,6 +55,24 @@ def test_offsets_of_a_tile_stay_below_the_buffers_end(sizes):
             assert tile <= most and full + rest == -(-M // tile) * -(-N // tile) and (splits > 1) == (rest > 0)
 
 
+# (T, N, K) of a product and its gradients: (tile, parts of k, whole tiles, split tiles) of y, dx and dw.  The GPU tests run these.
+LARGE = {
+    (4000, 6100, 5128): ((256, 2, 256, 128), (256, 2, 256, 80), (256, 1, 504, 0)),  # whole and split tiles in one launch, joined
+    (5200, 2501, 2499): ((256, 1, 210, 0), (256, 1, 210, 0), (256, 2, 0, 100)),     # all tiles split; rows that have to be copied
+    (2000, 2000, 2000): ((128, 1, 256, 0), (128, 1, 256, 0), (128, 1, 256, 0)),
+    (1990, 1985, 2003): ((128, 1, 256, 0), (128, 1, 256, 0), (128, 1, 256, 0)),
+    (300, 260, 2100): ((64, 8, 0, 25), (64, 1, 165, 0), (64, 1, 165, 0)),
+}
+
+
+def test_sizes_of_the_gpu_tests_reach_every_kind_of_launch(sizes):
+    got = {s: tuple(chosen(sizes, *mnk) for mnk in ((s[0], s[1], s[2]), (s[0], s[2], s[1]), (s[1], s[2], s[0]))) for s in LARGE}
+    assert got == LARGE
+    for product in range(3):  # each product (its layout is its own kernel) in the middle and the large tile
+        assert {c[product][0] for c in got.values()} == {64, 128, 256}
+    assert any(c[0][1] > 1 and c[0][0] == 256 for c in got.values()) and any(c[1][1] > 1 for c in got.values()) and any(c[2][1] > 1 for c in got.values())
+
+
 def test_rows_that_the_loads_do_not_reach_are_refused():
     long = 1 << 25
     p = make(L.oob_linear, **{**LINEAR, "T": 1, "N": 64, "K": long, "x_stride": long, "w_stride": long, "y_stride": 64})
