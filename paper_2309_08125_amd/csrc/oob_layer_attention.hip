@@ -255,8 +255,9 @@ __device__ inline void place(int heads, int B, int id, int &tile, int &head, int
  * A wave has 32 queries, one a lane pair: scores are formed transposed (keys in the registers, the query in the lane), so that a
  * query's running maximum and sum are its lane's own and the exponentials are, as they lie, the second operand of o^T += v^T p^T.
  * A step's products are the scores of its tile and o^T of the tile before.
- * Bound by the matrix cores and the exponentials in turn: 72 us for 4096 tokens, 12 heads of 128, causal; without a mask and 16 heads
- * 168 us, 0.82 PFLOP/s (192 us with the teams in step, 178 us without the order of reads and products below). */
+ * Bound by the matrix cores and the exponentials in turn, and in every other step by a wait of the compiler's own for all loads before the
+ * reads: 75 us for 4096 tokens, 12 heads of 128, causal; without a mask and 16 heads 139 us, 0.99 PFLOP/s (14 % more with the teams in step, 6 %
+ * more without the order of reads and products below). */
 template <class E, int DP, int KIND> __global__ __launch_bounds__(THREADS, 2) void k_attention(Attention a) {
   using R = Rows<DP, KT>;
   __shared__ __attribute__((aligned(1024))) char mem[8 * R::BYTES];
@@ -366,7 +367,7 @@ template <class E, int DP, int KIND> __global__ __launch_bounds__(THREADS, 2) vo
       for (int r = 0; r < 8; r++) {
         float e = exp2_(s[x / 2][8 * (x % 2) + r] * c - from);
         sum += e;
-        p[x][r] = (E)e;
+        p[x][r] = (E)e; /* the matrix cores take 16 bits; the sum does not see this rounding */
       }
   };
   load_k(0, 0);
@@ -442,7 +443,8 @@ template <class E, int DP, int KIND> __global__ __launch_bounds__(THREADS, 2) vo
 }
 
 /* ---- backward --------------------------------------------------------------------------------------------------------------- */
-/* delta = do . o and lse in powers of 2: 16 lanes a row, eight values each. */
+/* delta = do . o and lse in powers of 2: 16 lanes a row, eight values each.  o is read as it was returned, rounded: forming it again would be
+ * the forward pass. */
 template <class E> __global__ __launch_bounds__(256) void k_delta(Attention a, float *lse2, float *delta) {
   int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16, rows = (int64_t)a.B * a.H * a.Sq;
   if (row >= rows) return;
@@ -471,7 +473,8 @@ __global__ __launch_bounds__(64) void k_ranges(Attention a, int4 *ranges, int ro
 }
 
 /* What a pair (query, key) gives: p = e^(s - lse) and ds = p (dp - delta) ds/draw but for the scale, which the sums
- * get at the end. */
+ * get at the end.  Both are rounded to the type for the products behind: the matrix cores take 16 bits.  (float16: ds without the scale has to
+ * stay below 65504, and keeps more of its small values than with it.) */
 template <int KIND> __device__ inline void pair(const Attention &a, float slope2, int distance, float lse2, float delta, float raw, float dp, float &p, float &ds) {
   float by;
   p = exp2_(score<KIND>(a, slope2, raw, distance, by) - lse2);
@@ -846,8 +849,10 @@ template <class E, int DP, int KIND> __device__ __forceinline__ void attention_d
 }
 
 /* Both in one launch: the tiles of keys first, then those of queries fill up what the last of them leave idle.  Seven products a pair of
- * tiles where five would do if dq were added up by atomics, whose order changes sums: 250 us for 4096 tokens, 12 heads of 128, causal (322
- * in two launches of one-team workgroups); without a mask and 16 heads 531 us, 0.65 PFLOP/s on the five. */
+ * tiles where five would do if dq were added up by atomics, whose order changes sums: with delta and ranges 264 us for 4096 tokens, 12 heads of
+ * 128, causal (a quarter more in two launches of one-team workgroups); without a mask and 16 heads 543 us, 0.63 PFLOP/s on the five.  For heads of 128
+ * the steps of dk and dv are short of registers (34 spilled, 73 with a distance bias, 93 with a cap too) and wait for all loads three times: for the
+ * ranges of the tile that is loaded next, for those of the present one, and for what was spilled. */
 template <class E, int DP, int KIND> __global__ __launch_bounds__(THREADS, 2) void k_attention_grad(Attention a, int of_keys) {
   __shared__ __attribute__((aligned(1024))) char mem[GradLds<DP>::BYTES];
   __shared__ int part[8][2];

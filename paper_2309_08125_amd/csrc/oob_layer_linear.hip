@@ -7,9 +7,10 @@ namespace layer {
 /* ---- the product -------------------------------------------------------------------------------------------------------
  * C[m][n] = sum_k A(m, k) B(n, k), each operand stored with k contiguous (rows of k) or with m (n) contiguous (rows of m per k): the
  * forward product and both gradients are one kernel, the m-contiguous operand read from LDS by transposing reads, no transposed copy.
- * Tiles go to LDS by loads that pass no registers, a step ahead of the products; a wave's fragments are read one sub-step ahead (4096 x
- * 6144 x 12288: 571 us, 601 without).  Bound by the matrix cores and the barrier a step: 1.0 to 1.3 PFLOP/s at the sizes of a 12288-wide
- * layer on 8 GPUs, a library's plain product there 0.97 to 1.6. */
+ * Tiles go to LDS by loads that pass no registers, asked for a step ahead of the products; a wave's fragments are read one sub-step ahead (5 %).
+ * In the gradients' products a step ahead is not reached: before the first transposing read of a step the compiler waits for all loads in
+ * flight, since it cannot tell the LDS that they write from the LDS that is read.  4096 x 6144 x 12288: forward 504 us with its join (1.23 PFLOP/s,
+ * matrix cores busy 63 % of the time, the rest mostly the barrier a step), dx 550 (1.12, 46 %), dw 590 (1.05, 48 %). */
 struct Product {
   const void *A, *B;
   int64_t lda, ldb; /* elements between rows */
@@ -136,7 +137,7 @@ template <class E> __device__ inline void epilogue(const Product &g, int64_t m, 
     for (int e = 0; e < 8; e++) v[e] += e < left ? (float)b[e] : 0.f;
   }
   typename Vec<E>::v8 out;
-  if (g.Z) {
+  if (g.Z) { /* rounded to the type, as y is: half the memory between the passes; act' sees the rounding, act does not */
     for (int e = 0; e < 8; e++) out[e] = (E)v[e];
     store8<E>((E *)g.Z + m * g.ldz + n, out, left);
   }
@@ -339,8 +340,8 @@ template <class E, int ACT> __global__ __launch_bounds__(256) void k_act_grad(Ac
       if (g.dz) {
         for (int e = 0; e < 8; e++) {
           float v = (float)d[u][e] * slope(ACT == OOB_ACT_NONE ? 0.f : (float)z[u][e], ACT);
-          out[e] = (E)v;
-          sum[e] += v; /* before the rounding: the bias's gradient does not see it */
+          out[e] = (E)v; /* the matrix cores take 16 bits: dx and dw see this rounding */
+          sum[e] += v;   /* the bias's gradient does not */
         }
         store8<E>((E *)g.dz + (t0 + 4 * u) * g.ld_dz + n, out, 8); /* past N: zeros */
       } else {

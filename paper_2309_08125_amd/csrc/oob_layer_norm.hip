@@ -361,8 +361,9 @@ static Norm norm_of(const oob_norm *p) {
 
 template <class E> static void norm(const Norm &n, hipStream_t st) {
   /* Rows of up to 1024 by one wave: no barrier; wider ones by as many waves as keep a lane's part in 32 registers.  Workgroups (768 of eight
-   * waves) go through the rows with the weights in registers and the next row on its way (4096 x 12288, bfloat16: 95 us with dropout and 81 without,
-   * 4.2 and 5.0 TB/s, a large copy's rate; 121 and 104 us by 2048 workgroups without the row ahead). */
+   * waves) go through the rows with the weights in registers and the next row on its way (4096 x 12288, bfloat16: 87 us with dropout and 82 without,
+   * 4.6 and 4.9 TB/s, a large copy's rate; a quarter more by 2048 workgroups without the row ahead).  Four vectors a lane of 32-bit values do not
+   * fit the registers: rows over 12 288 in float32 take 282 us (4096 x 16384, 3.8 TB/s). */
   int64_t need = (n.C + 511) / 512, rows = n.T < 2048 ? n.T : 2048, wide = n.T < 768 ? n.T : 768, rows4 = n.T < 8192 ? (n.T + 3) / 4 : 2048;
   if (need <= 1) k_norm<E, 1, 1><<<(unsigned)rows4, 256, 0, st>>>(n);
   else if (need <= 2) k_norm<E, 1, 2><<<(unsigned)rows4, 256, 0, st>>>(n);
@@ -375,7 +376,7 @@ template <class E> static void norm(const Norm &n, hipStream_t st) {
 
 struct Runs { int64_t workgroups, rows, per_gate; };
 
-/* Workgroups of the backward pass: enough waves to fill the GPU, and no more: each leaves a row of sums per weight (4096 x 12288: 131 us
+/* Workgroups of the backward pass: enough waves to fill the GPU, and no more: each leaves a row of sums per weight (4096 x 12288: 130 us
  * with 256 workgroups of eight waves, 141 with 512; 4096 x 4096: 47 us with 512 of four, 61 with 256; what is read and written at a copy's
  * rate would take 100 and 33 us; loading the next row ahead gained nothing).  Where there are gates, a workgroup's rows belong to one gate, or, with
  * more gates than workgroups, to whole gates. */

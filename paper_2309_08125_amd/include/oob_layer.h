@@ -37,7 +37,7 @@ enum { OOB_BF16 = 0, OOB_FP16 = 1, OOB_FP32 = 2 };
  * Rows of below 2^24 values are accepted whatever their number.  Longer ones of x, w, and for the gradients dy: as long as the first 64
  * of them (fewer, where there are fewer), each rounded up to 8 values, lie within 2^31 bytes; otherwise OOB_EINVAL.
  * RELU max(z, 0); GELU z Phi(z), by the error function; GELU_TANH its form with tanh(sqrt(2 / pi) (z +
- * 0.044715 z^3)); SILU z / (1 + e^-z). */
+ * 0.044715 z^3)); SILU z / (1 + e^-z).  A NaN gives NaN, in value and slope. */
 enum { OOB_ACT_NONE = 0, OOB_ACT_RELU = 1, OOB_ACT_GELU = 2, OOB_ACT_GELU_TANH = 3, OOB_ACT_SILU = 4, OOB_ACTS = 5 };
 
 typedef struct oob_linear {
@@ -86,7 +86,8 @@ typedef struct oob_norm {
   const void *x, *z, *weight, *bias, *post_weight, *post_bias, *gate;
   int64_t x_stride, z_stride;
   void *xp, *h;             /* [T][C] out */
-  float *saved;             /* [4][T] out: mean and 1 / deviation of pre, of post; or NULL */
+  float *saved;             /* [4][T] out ([2][T] where post is NONE): mean and 1 / deviation of pre, of post; or NULL.  The
+                             * backward pass reads the means of LAYER norms */
 } oob_norm;
 
 int oob_layer_norm(const oob_norm *p, void *stream);
@@ -114,7 +115,8 @@ int oob_layer_norm_backward(const oob_norm *p, const oob_norm_grad *g, void *wor
  *   |i + Sk - Sq - j|;  o_i = sum_j softmax_j(s_ij) v_j;  lse_i = log sum_j e^s_ij
  * A query that sees no key has o = 0, lse = -inf and no part in any gradient, whatever it holds.  Keys that none of the
  * queries 128 t .. 128 t + 127 sees have no part in theirs, whatever they hold; others have to be finite, also for the
- * queries among those that do not see them.
+ * queries among those that do not see them.  The backward pass rounds p_ij (dout_i . v_j - dout_i . o_i) to the type: with
+ * OOB_FP16 it has to stay below 65504.
  * q, o [B][Sq][H][D], k, v [B][Sk][G][D]: strides of a sequence, a row and a head, the last axis
  * contiguous; 0 for an axis of inputs that repeats, not of results (OOB_EINVAL).  k, v, and for the gradients q and dout, are copied where they do not start at 16 bytes, a stride is no multiple of
  * that or D none of 8, or rows lie 2^24 bytes apart; the heads of 32 rows (fewer, where there are fewer) then have to take less than 2^31 bytes. */

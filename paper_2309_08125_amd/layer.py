@@ -1,7 +1,8 @@
 """Binding of include/oob_layer.h: the operators of a transformer layer on torch tensors.
 
 Argument checks, output tensors and workspaces only: every step runs in the HIP kernels of liboob_plan.so.  Work is
-enqueued on torch's current stream of the tensors' device; nothing waits.  There is no CPU fallback.
+enqueued on torch's current stream of the tensors' device; nothing waits.  There is no CPU fallback.  No call builds an
+autograd graph: what a call makes requires no gradient, whatever its inputs do; gradients are the *_backward calls' results.
 """
 from __future__ import annotations
 
@@ -149,7 +150,7 @@ def _act(act):
 def linear(x, w, bias=None, act="none", residual=None, keep=False):
     """y = act(x w^T + bias) + residual.  x [..., K], w [N, K], bias [N], residual [..., N]: bfloat16 or float16, rows of any
     stride.  keep=True: (y, z) with z = x w^T + bias, which linear_backward wants where there is an activation (z is None without
-    one)."""
+    one).  No autograd graph is built: gradients are linear_backward's."""
     _load()
     code = _act(act)
     if not (x.is_cuda and w.dim() == 2):
@@ -250,7 +251,7 @@ def residual_norm(x, z=None, weight=None, bias=None, pre="layer", post="none", p
     x: the residual stream [..., C]; z: the block's output, or None (xp is x: the first norm of a model); pre: "layer" or "rms" with
     weight and bias [C]; post: "none" or a norm with post_weight and post_bias; gate [C] or [G, C]: one for each G-th of the rows;
     dropout: dropout(post(z), p, seed, offset), element by element of the rows.  bfloat16, float16 or float32.  saved: statistics
-    that the backward pass wants."""
+    that the backward pass wants.  No autograd graph is built: gradients are residual_norm_backward's."""
     _load()
     h, xp = x.new_empty(x.shape), x if z is None else x.new_empty(x.shape)
     width = x.shape[-1] if x.dim() else 0
@@ -284,7 +285,8 @@ def residual_norm_backward(dxp, dh, xp, z, saved, weight=None, bias=None, pre="l
 
 def dropout(x, p, seed, offset=0, out=None):
     """keep / (1 - p) * x for a contiguous tensor of any shape (bfloat16, float16, float32); out may be x.  The mask comes from
-    (seed, offset + element) alone and is never stored: the backward pass is the same call on the gradient."""
+    (seed, offset + element) alone and is never stored: the backward pass is the same call on the gradient (no autograd
+    graph is built)."""
     _load()
     if not (x.is_cuda and x.is_contiguous()):
         raise ValueError("x has to be contiguous and on the GPU")
@@ -345,7 +347,7 @@ def attention(q, k, v, scale=None, causal=False, key_begin=None, key_end=None, s
     128.  scale: D ** -0.5 where None.  key_begin, key_end: int32 [B, Sq] or None; document, prefix and window masks are such ranges
     (document_ranges, prefix_ranges).  slopes: float32 [H] or None; cap 0: none.  A query that sees no key gets 0 and lse -inf,
     whatever it holds; keys that no query of a 128-row tile sees (between those that it does, too) may hold anything, others have to be
-    finite.  lse [B, H, Sq] in float32 goes to attention_backward."""
+    finite.  lse [B, H, Sq] in float32 goes to attention_backward: no autograd graph is built."""
     _load()
     if not (q.dim() == 4):
         raise ValueError("q: [batch, length, heads, width]")
