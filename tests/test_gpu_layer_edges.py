@@ -158,3 +158,33 @@ def test_norm_of_more_rows_than_workgroups(P, T, C):
         norm_case(P, T, C, t)
         norm_case(P, T, C, t, pre="rms", post="layer", gates=2, alpha=0.5, p=0.25)
     norm_case(P, T, C, torch.bfloat16, post="rms", gates=T // 2)
+
+
+def test_linear_of_long_rows(P):
+    """Rows of 2^24 - 8 values: offsets within a tile up to the buffer's end, all three products."""
+    T, N, K, t = 3, 64, (1 << 24) - 8, torch.bfloat16
+    x, w, dy = rand(T, K, t=t), rand(N, K, t=t), rand(T, N, t=t)
+    y = P.linear(x, w)
+    dx, dw, _ = P.linear_backward(dy, x, w, need=("x", "w"))
+    want = torch.zeros(T, N, device="cuda", dtype=torch.float64)
+    for k in range(0, K, 1 << 20):
+        xs, ws = x[:, k: k + (1 << 20)].double(), w[:, k: k + (1 << 20)].double()
+        want += xs @ ws.t()
+        for got, val, terms in ((dx, dy.double() @ ws, N), (dw, dy.double().t() @ xs, T)):
+            within(got[:, k: k + (1 << 20)], val, U[t] * val.abs() + 1e-5 * terms, "dx" if got is dx else "dw")
+    # 32-bit sums of n = 2^24 terms of deviation 1 in 32 parts: partial sums of some 1000 are rounded by 3e-5, n / 32 times a part, at random
+    within(y, want, U[t] * want.abs() + 1.0, "y")
+
+
+def test_attention_of_expanded_inputs(P):
+    """Keys and values that all sequences (or heads) share through strides of 0: results and gradients are those of their copies."""
+    B, S, H, D = 3, 150, 4, 64
+    for t, one in ((torch.bfloat16, (1, S, 2, D)), (torch.float16, (B, S, 1, D))):
+        q, do, k, v = rand(B, S, H, D, t=t), rand(B, S, H, D, t=t), rand(*one, t=t).expand(B, S, 2, D), rand(*one, t=t).expand(B, S, 2, D)
+        results = []
+        for a, b in ((k, v), (k.contiguous(), v.contiguous())):
+            o, lse = P.attention(q, a, b, causal=True)
+            results.append((o, lse, *P.attention_backward(do, q, a, b, o, lse, causal=True)))
+        assert all(torch.equal(a, b) for a, b in zip(*results))
+        with pytest.raises(RuntimeError):
+            P.attention_backward(do, q, k, v, *results[0][:2], causal=True, out=(torch.empty_like(q), k.clone().expand(B, S, 2, D), torch.empty(one, dtype=t, device="cuda").expand(B, S, 2, D)))
