@@ -196,7 +196,8 @@ __device__ inline void join_ranges(int &lo, int &hi, int (*part)[2]) {
 /* The ranges of a workgroup's queries may leave keys between the first and the last that none of them sees (padding between documents,
  * say).  Those are read as zeros: 0 times what they hold need not be 0.  Ranges that all begin with the first key or all end with the last
  * leave none, nor do those of which each touches that of the query before; only for others the tiles are looked at (2 x 4096 tokens, 16 heads
- * of 128, documents of 360 padded to 384: 75 to 76 us forward, 209 to 210 backward; of 60 to 64: 69 to 74 and 197 to 204). */
+ * of 128, documents of 360 padded to 384: 75 to 76 us forward, 209 to 210 backward; of 60 to 64: 69 to 74 and 197 to 204; without holes the
+ * question takes 1 us of a call: 4096 tokens, 12 heads of 64, a window of 512: 28.4 to 29.8). */
 struct Holes { int2 of[ROWS]; int any[8]; };
 
 /* Before join_ranges, whose barrier this needs. */
