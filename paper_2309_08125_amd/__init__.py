@@ -17,3 +17,7 @@ from .layer import (  # noqa: F401
     ACTIVATIONS, LAYER_SYMBOLS, attention, attention_backward, document_ranges, dropout, linear, linear_backward, prefix_ranges,
     residual_norm, residual_norm_backward,
 )
+from .expert import (  # noqa: F401
+    EXPERT_SYMBOLS, clip_gradients, expert_linear, expert_linear_backward, expert_rows, expert_sum, expert_sum_backward, gradient_norm, route,
+    route_backward,
+)

@@ -1,0 +1,172 @@
+/* The weighted sum of what a token's experts gave, and its gradients. */
+#include "oob_expert.h"
+#include "oob_layer_device.h"
+
+namespace layer {
+namespace {
+
+/* A token takes `width` threads of a workgroup (a power of two), eight columns each at a time. */
+struct Sum {
+  oob_expert_sum_t p;
+  int width;
+  const void *dout;
+  void *dy;
+  int64_t ld_dout, ld_dy;
+  float *dweights;
+};
+constexpr int TOGETHER = 8; /* rows of y that are on their way at once */
+
+/* Place and weight of a choice; -1: it has no part. */
+__device__ inline int64_t place_of(const oob_expert_sum_t &p, int64_t t, int j, float &w) {
+  int64_t r = j < p.k ? p.place[t * p.k + j] : -1;
+  if (r < 0 || r >= p.R) r = -1;
+  w = r < 0 ? 0.f : p.weights ? p.weights[t * p.k + j] : 1.f;
+  return r;
+}
+
+template <class E> __global__ __launch_bounds__(256) void k_sum(Sum g) {
+  const oob_expert_sum_t &p = g.p;
+  int64_t t = (int64_t)blockIdx.x * (256 / g.width) + threadIdx.x / g.width;
+  int64_t c = ((int64_t)blockIdx.y * g.width + threadIdx.x % g.width) * 8, left = p.C - c;
+  if (t >= p.T || left <= 0) return;
+  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  typename Vec<E>::v8 res;
+  if (p.residual) res = load8<E>((const E *)p.residual + t * p.residual_stride + c, left);
+  for (int j0 = 0; j0 < p.k; j0 += TOGETHER) {
+    typename Vec<E>::v8 y[TOGETHER];
+    float w[TOGETHER];
+    int64_t r[TOGETHER];
+#pragma unroll
+    for (int j = 0; j < TOGETHER; j++) {
+      r[j] = place_of(p, t, j0 + j, w[j]);
+      if (r[j] >= 0) y[j] = load8<E>((const E *)p.y + r[j] * p.y_stride + c, left);
+    }
+#pragma unroll
+    for (int j = 0; j < TOGETHER; j++)
+      if (r[j] >= 0)
+        for (int e = 0; e < 8; e++) sum[e] += w[j] * (float)y[j][e];
+  }
+  typename Vec<E>::v8 out;
+  for (int e = 0; e < 8; e++) out[e] = (E)(p.residual ? sum[e] + (float)res[e] : sum[e]);
+  store8<E>((E *)p.out + t * p.out_stride + c, out, left);
+}
+
+/* dy[place] = w dout, dweights = dout . y[place]: a token's row of dout is read once for every TOGETHER choices. */
+template <class E> __global__ __launch_bounds__(256) void k_sum_grad(Sum g) {
+  __shared__ float part[4][TOGETHER];
+  const oob_expert_sum_t &p = g.p;
+  int64_t t = (int64_t)blockIdx.x * (256 / g.width) + threadIdx.x / g.width;
+  bool live = t < p.T;
+  int at = threadIdx.x % g.width;
+  for (int j0 = 0; j0 < p.k; j0 += TOGETHER) {
+    float w[TOGETHER], dot[TOGETHER];
+    int64_t r[TOGETHER];
+#pragma unroll
+    for (int j = 0; j < TOGETHER; j++) {
+      dot[j] = 0, r[j] = -1;
+      if (live) r[j] = place_of(p, t, j0 + j, w[j]);
+    }
+    for (int64_t c = (int64_t)at * 8; live && c < p.C; c += g.width * 8) {
+      int64_t left = p.C - c;
+      typename Vec<E>::v8 y[TOGETHER], d = load8<E>((const E *)g.dout + t * g.ld_dout + c, left);
+      if (g.dweights)
+#pragma unroll
+        for (int j = 0; j < TOGETHER; j++)
+          if (r[j] >= 0) y[j] = load8<E>((const E *)p.y + r[j] * p.y_stride + c, left);
+#pragma unroll
+      for (int j = 0; j < TOGETHER; j++) {
+        if (r[j] < 0) continue;
+        if (g.dweights)
+          for (int e = 0; e < 8; e++) dot[j] += e < left ? (float)d[e] * (float)y[j][e] : 0.f;
+        if (g.dy) {
+          typename Vec<E>::v8 out;
+          for (int e = 0; e < 8; e++) out[e] = (E)(w[j] * (float)d[e]);
+          store8<E>((E *)g.dy + r[j] * g.ld_dy + c, out, left);
+        }
+      }
+    }
+    if (!g.dweights) continue;
+    int run = g.width < 64 ? g.width : 64;
+#pragma unroll
+    for (int j = 0; j < TOGETHER; j++)
+      for (int o = 1; o < run; o *= 2) dot[j] += __shfl_xor(dot[j], o);
+    if (g.width > 64) { /* one token a workgroup: its waves' sums in their order */
+      __syncthreads();
+      if (lane() == 0)
+        for (int j = 0; j < TOGETHER; j++) part[threadIdx.x / 64][j] = dot[j];
+      __syncthreads();
+      if (at == 0)
+        for (int j = 0; j < TOGETHER; j++) {
+          dot[j] = part[0][j];
+          for (int wave = 1; wave < g.width / 64; wave++) dot[j] += part[wave][j];
+        }
+    }
+    if (live && at == 0)
+#pragma unroll
+      for (int j = 0; j < TOGETHER; j++)
+        if (j0 + j < p.k) g.dweights[t * p.k + j0 + j] = r[j] < 0 ? 0.f : dot[j];
+  }
+}
+
+bool sum_ok(const oob_expert_sum_t *p, bool forward) {
+  const int64_t most = (int64_t)1 << 31;
+  if (!p || (p->dtype != OOB_BF16 && p->dtype != OOB_FP16 && p->dtype != OOB_FP32) || p->k < 1 || p->k > OOB_EXPERT_MAX_CHOICES) return false;
+  if (p->T < 0 || p->R < 0 || p->C < 1 || p->T >= most || p->R >= most || p->C >= most) return false;
+  if (p->T == 0) return true;
+  size_t of = p->dtype == OOB_FP32 ? 4 : 2;
+  if (!p->place || !multiple(p->place, 4) || !multiple(p->weights, 4)) return false;
+  if (p->R && (!p->y || p->y_stride < p->C || !multiple(p->y, of))) return false;
+  if (!forward) return true;
+  if (p->residual && (p->residual_stride < p->C || !multiple(p->residual, of))) return false;
+  return p->out && p->out_stride >= p->C && multiple(p->out, of);
+}
+
+/* Threads of a token: those that its columns need, up to a workgroup. */
+int width_of(int64_t C) {
+  int w = 1;
+  while (w < 256 && w * 8 < C) w *= 2;
+  return w;
+}
+
+template <class E> void sum(const Sum &g, hipStream_t st) {
+  int64_t per = 256 / g.width;
+  dim3 grid((unsigned)((g.p.T + per - 1) / per), (unsigned)((g.p.C + g.width * 8 - 1) / (g.width * 8)));
+  k_sum<E><<<grid, 256, 0, st>>>(g);
+}
+template <class E> void sum_grad(const Sum &g, hipStream_t st) {
+  int64_t per = 256 / g.width;
+  k_sum_grad<E><<<(unsigned)((g.p.T + per - 1) / per), 256, 0, st>>>(g);
+}
+
+}  // namespace
+}  // namespace layer
+
+using namespace layer;
+
+extern "C" int oob_expert_sum(const oob_expert_sum_t *p, void *stream) {
+  if (!sum_ok(p, true)) return OOB_EINVAL;
+  if (p->T == 0) return OOB_OK;
+  Sum g{};
+  g.p = *p, g.width = width_of(p->C);
+  if ((p->C + g.width * 8 - 1) / (g.width * 8) > 65535) return OOB_EINVAL; /* rows of 2^27 values */
+  hipStream_t st = (hipStream_t)stream;
+  if (p->dtype == OOB_BF16) sum<bf16>(g, st);
+  else if (p->dtype == OOB_FP16) sum<fp16>(g, st);
+  else sum<float>(g, st);
+  return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
+}
+
+extern "C" int oob_expert_sum_backward(const oob_expert_sum_t *p, const void *dout, int64_t dout_stride, void *dy, int64_t dy_stride, float *dweights,
+                                       void *stream) {
+  if (!sum_ok(p, false)) return OOB_EINVAL;
+  if (p->T == 0) return OOB_OK;
+  size_t of = p->dtype == OOB_FP32 ? 4 : 2;
+  if (!dout || dout_stride < p->C || !multiple(dout, of) || (!dy && !dweights)) return OOB_EINVAL;
+  if ((dy && (dy_stride < p->C || !multiple(dy, of))) || !multiple(dweights, 4)) return OOB_EINVAL;
+  Sum g{*p, width_of(p->C), dout, dy, dout_stride, dy_stride, dweights};
+  hipStream_t st = (hipStream_t)stream;
+  if (p->dtype == OOB_BF16) sum_grad<bf16>(g, st);
+  else if (p->dtype == OOB_FP16) sum_grad<fp16>(g, st);
+  else sum_grad<float>(g, st);
+  return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
+}
