@@ -60,164 +60,283 @@ struct Experts {
   const int32_t *rows; /* gathered: row r of A is that of token rows[r] / per */
   int per;
   int64_t T, expert_stride; /* elements of B between experts */
+  int ids; /* numbers of tiles: as many as there can be */
 };
 
-/* Rows of k that lie anywhere: each lane's offsets come from the rows' tokens. */
-template <class E, int ROWS, int THREADS> struct Gathered : Tile<E, ROWS, THREADS, true> {
-  __device__ void init(int64_t ld, int64_t left, const int32_t *rows, int per, int64_t T) {
-    for (int i = 0; i < this->LOADS; i++) {
-      int p = (i * THREADS + threadIdx.x) * 16, r = p / 128, c = (p / 16 % 8) ^ (r / 2 % 8);
-      this->at[i] = c * 8;
-      int64_t t = r < left ? rows[r] : -1;
-      t = t < 0 ? -1 : t / per;
-      this->off[i] = t >= 0 && t < T ? (uint32_t)(t * ld * 2 + c * 16) : OOB_LAYER_OUT;
+/* An operand's tile of ROWS x KSTEP on its way to LDS, laid out as Tile has it: the 16 bytes that a lane takes with its i-th load lie a fixed way from those
+ * of its first, so that it holds one offset, not one for each. */
+template <class E, int ROWS, int THREADS, bool KC> struct Strip {
+  static constexpr int BYTES = ROWS * KSTEP * 2, LOADS = BYTES / (THREADS * 16), APART = KC ? THREADS * 16 / 128 : THREADS * 16 / (ROWS * 2);
+  static_assert(APART % (KC ? 16 : 4) == 0, "the exchange of chunks is the same for all of a lane's loads");
+  uint32_t off, way; /* byte offset of the first from the start of the step, bytes to the next */
+  int k, row, left;  /* first k of the 16 bytes (k contiguous) or row of k; row of m (k contiguous), rows there are */
+
+  __device__ void init(int64_t ld, int64_t rows) { /* rows: of m (n), from the tile's first on */
+    int p = threadIdx.x * 16;
+    left = (int)(rows < ROWS ? rows : ROWS), way = (uint32_t)(APART * ld * 2);
+    if (KC) {
+      int r = p / 128, c = (p / 16 % 8) ^ (r / 2 % 8);
+      k = c * 8, row = r, off = (uint32_t)(r * ld * 2 + c * 16);
+    } else {
+      constexpr int CH = ROWS / 8;
+      int r = p / (ROWS * 2), c = (p / 16 % CH) ^ (ROWS == 64 ? r / 2 % 2 * 4 : r % 4 * 4);
+      k = r, row = 0, off = c * 8 < left ? (uint32_t)(r * ld * 2 + c * 16) : OOB_LAYER_OUT;
+    }
+  }
+  /* Asks for the step that starts at `base`; kleft: values of k there are from here on, 0 or less: zeros land, nothing is read. */
+  __device__ void load(const char *base, lds_char *to, int kleft) {
+    __amdgpu_buffer_rsrc_t r = buffer(base);
+    int wave = uniform(threadIdx.x / 64);
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+      bool in = KC ? k < kleft && row + i * APART < left : k + i * APART < kleft;
+      load_lds(r, to + (i * THREADS + wave * 64) * 16, in ? off : OOB_LAYER_OUT, i * way);
     }
   }
 };
 
-/* The sums of one tile over `steps` steps: as in the dense product. */
-template <class E, int TM, int TN, int WM, int WN, bool AK, bool BK, class TA, class TB>
-__device__ inline void multiply(TA &ta, TB &tb, const char *pa, const char *pb, int64_t da, int64_t db, int64_t kleft, int steps, lds_char *lds,
-                                f32x16 (&acc)[TM / WM / 32][TN / WN / 32]) {
-  constexpr int FM = TM / WM / 32, FN = TN / WN / 32, STAGE = TA::BYTES + TB::BYTES;
+/* Rows of k that lie anywhere: each lane's offsets come from the rows' tokens. */
+template <class E, int ROWS, int THREADS> struct Gathered {
+  static constexpr int BYTES = ROWS * KSTEP * 2, LOADS = BYTES / (THREADS * 16);
+  uint32_t off[LOADS];
+  int k;
+  __device__ void init(int64_t ld, int64_t left, const int32_t *rows, int per, int64_t T) {
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+      int p = (i * THREADS + threadIdx.x) * 16, r = p / 128, c = (p / 16 % 8) ^ (r / 2 % 8);
+      k = c * 8; /* the same for all */
+      int64_t t = r < left ? rows[r] : -1;
+      t = t < 0 ? -1 : t / per;
+      off[i] = t >= 0 && t < T ? (uint32_t)(t * ld * 2 + c * 16) : OOB_LAYER_OUT;
+    }
+  }
+  __device__ void load(const char *base, lds_char *to, int kleft) {
+    __amdgpu_buffer_rsrc_t r = buffer(base);
+    int wave = uniform(threadIdx.x / 64);
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) load_lds(r, to + (i * THREADS + wave * 64) * 16, k < kleft ? off[i] : OOB_LAYER_OUT);
+  }
+};
+
+/* The sums of one tile over `steps` steps of k, the first two of which are on their way to LDS; load(buffer) asks for the next.  Two buffers, two arrays: the compiler then
+ * knows that a read of one does not wait for the loads to the other.  A step's last products run behind the barrier that frees its buffer: while they
+ * do, the first fragments of the next step are read and the loads of the one after are asked for.  At the end nobody reads the buffers any more. */
+template <class E, int TM, int TN, int WM, int WN, bool AK, bool BK, class TA, class TB, class L>
+__device__ __forceinline__ void multiply(L &load, int steps, lds_char *even, lds_char *odd, f32x16 (&acc)[TM / WM / 32][TN / WN / 32]) {
+  constexpr int FM = TM / WM / 32, FN = TN / WN / 32, READS = FM * (AK ? 1 : 2) + FN * (BK ? 1 : 2), LOADS = TA::LOADS + TB::LOADS;
   int wave = uniform(threadIdx.x / 64), wm = wave / WN, wn = wave % WN;
   Fragment<E, TM, FM, AK> fa;
   Fragment<E, TN, FN, BK> fb;
   fa.init(wm * FM * 32);
   fb.init(wn * FN * 32);
+#pragma unroll
   for (int i = 0; i < FM; i++)
-    for (int j = 0; j < FN; j++)
-      for (int r = 0; r < 16; r++) acc[i][j][r] = 0;
-  if (steps > 0) {
-    ta.load(pa, lds, kleft);
-    tb.load(pb, lds + TA::BYTES, kleft);
-  }
-  for (int t = 0; t < steps; t++) {
-    wait_barrier(); /* the step's loads have landed, and nobody reads the other buffer any more */
-    lds_char *now = lds + t % 2 * STAGE, *next = lds + (t + 1) % 2 * STAGE;
-    pa += da, pb += db, kleft -= KSTEP;
-    if (t + 1 < steps) {
-      ta.load(pa, next, kleft);
-      tb.load(pb, next + TA::BYTES, kleft);
+#pragma unroll
+    for (int j = 0; j < FN; j++) acc[i][j] = f32x16{0};
+  using V = typename Vec<E>::v8;
+  V a0[FM], b0[FN], a1[FM], b1[FN];
+  auto fetch = [&](lds_char *from, int s, V(&a)[FM], V(&b)[FN]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FM; i++) a[i] = fa.read(from, i, s);
+#pragma unroll
+    for (int j = 0; j < FN; j++) b[j] = fb.read(from + TA::BYTES, j, s);
+  };
+  auto products = [&](V(&a)[FM], V(&b)[FN]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FM; i++)
+#pragma unroll
+      for (int j = 0; j < FN; j++) acc[i][j] = mfma(b[j], a[i], acc[i][j]); /* lane: m, registers: n */
+  };
+  constexpr int EVERY = (READS + FM * FN - 1) / (FM * FN);
+  auto order = [&]() __attribute__((always_inline)) { /* reads of the next fragments between the products */
+#pragma unroll
+    for (int g = 0; g < FM * FN; g++) {
+      if (g * EVERY < READS) __builtin_amdgcn_sched_group_barrier(0x100, EVERY, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
     }
-    typename Vec<E>::v8 a[2][FM], b[2][FN];
-    auto fetch = [&](int s, int x) __attribute__((always_inline)) {
+  };
+  auto front = [&](lds_char *now) __attribute__((always_inline)) { /* products 0 .. 2 of a step, reads of 1 .. 3 */
+    __builtin_amdgcn_sched_barrier(0);
+    fetch(now, 1, a1, b1);
+    products(a0, b0);
+    order();
+    fetch(now, 2, a0, b0);
+    products(a1, b1);
+    order();
+    fetch(now, 3, a1, b1);
+    products(a0, b0);
+    order();
+  };
+  auto back = [&](lds_char *now, lds_char *next) __attribute__((always_inline)) { /* product 3, read 0 of the next step */
+    wait_barrier(); /* the next step's loads have landed, and nobody reads this buffer any more */
+    fetch(next, 0, a0, b0);
+    load(now);
+    products(a1, b1);
 #pragma unroll
-      for (int i = 0; i < FM; i++) a[x][i] = fa.read(now, i, s);
-#pragma unroll
-      for (int j = 0; j < FN; j++) b[x][j] = fb.read(now + TA::BYTES, j, s);
-    };
-    fetch(0, 0);
-#pragma unroll
-    for (int s = 0; s < 4; s++) {
-      if (s < 3) fetch(s + 1, (s + 1) % 2);
-#pragma unroll
-      for (int i = 0; i < FM; i++)
-#pragma unroll
-        for (int j = 0; j < FN; j++) acc[i][j] = mfma(b[s % 2][j], a[s % 2][i], acc[i][j]); /* lane: m, registers: n */
-      constexpr int READS = FM * (AK ? 1 : 2) + FN * (BK ? 1 : 2); /* reads of the next fragments between the products */
-      if (s == 0) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-#pragma unroll
-      for (int g = 0; g < FM * FN; g++) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        if (s < 3 && g < READS) __builtin_amdgcn_sched_group_barrier(0x100, (READS + FM * FN - 1) / (FM * FN), 0);
-      }
+    for (int g = 0; g < FM * FN; g++) {
+      if (g * EVERY < READS) __builtin_amdgcn_sched_group_barrier(0x100, EVERY, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x10, (LOADS + FM * FN - 1) / (FM * FN), 0);
     }
+  };
+  wait_barrier();
+  fetch(even, 0, a0, b0);
+  front(even);
+  /* the loop begins where all loads are waited for: the compiler does so at its head whatever is on the way */
+  for (int t = 2; t < steps; t += 2) {
+    back(even, odd);
+    front(odd);
+    back(odd, even);
+    front(even);
   }
-  __syncthreads();
+  if (steps % 2 == 0) {
+    back(even, odd);
+    front(odd);
+  }
+  products(a1, b1);
+  wait_barrier(); /* the loads past the last step have landed: the next tile's may be asked for */
 }
 
-/* A tile's sums through the epilogue: rows m0 .. m0 + left - 1 of C, 32 at a time through the wave's own part of LDS, so that a row of C
- * is written in one go. */
-template <class E, int TM, int TN, int WM, int WN>
-__device__ inline void finish(const Product &g, f32x16 (&acc)[TM / WM / 32][TN / WN / 32], lds_char *lds, int64_t m0, int64_t left, int64_t n0) {
-  constexpr int FM = TM / WM / 32, FN = TN / WN / 32, PITCH = FN * 32 + 4, LPR = FN * 4, RPP = 64 / LPR;
+/* A tile's sums through the epilogue, from the registers that the products leave them in: a lane has a row and, of 16 neighbouring columns, two times four.
+ * An exchange between the halves of the wave makes them eight in a row, 16 bytes of C a store.  Nothing goes through LDS, so that the next tile's
+ * first loads are on their way meanwhile. */
+template <class E, int ACT, int TM, int TN, int WM, int WN>
+__device__ __forceinline__ void finish(const Product &g, f32x16 (&acc)[TM / WM / 32][TN / WN / 32], const E *bias, E *C, int64_t row, int left, int64_t n0) {
+  constexpr int FM = TM / WM / 32, FN = TN / WN / 32;
   int wave = uniform(threadIdx.x / 64), wm = wave / WN, wn = wave % WN, l = lane();
-  __attribute__((address_space(3))) float *stage = (__attribute__((address_space(3))) float *)lds + wave * 32 * PITCH;
+  int64_t n1 = n0 + wn * FN * 32 + l / 32 * 8;
+  typename Vec<E>::v8 add[FN][2];
+  if (bias)
+#pragma unroll
+    for (int j = 0; j < FN; j++)
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        int64_t n = n1 + j * 32 + h * 16;
+        if (n < g.N) add[j][h] = load8<E>(bias + n, g.N - n);
+      }
 #pragma unroll
   for (int i = 0; i < FM; i++) {
+    int m = (wm * FM + i) * 32 + (l & 31);
 #pragma unroll
     for (int j = 0; j < FN; j++)
 #pragma unroll
-      for (int q = 0; q < 4; q++) {
-        f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        *(__attribute__((address_space(3))) f32x4 *)(stage + (l & 31) * PITCH + j * 32 + 8 * q + 4 * (l >> 5)) = v;
-      }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
+      for (int h = 0; h < 2; h++) {
+        float v[8];
 #pragma unroll
-    for (int p = 0; p < 32 / RPP; p++) {
-      int row = p * RPP + l / LPR, m = (wm * FM + i) * 32 + row;
-      int64_t n = n0 + wn * FN * 32 + l % LPR * 8;
-      float v[8];
-      for (int e = 0; e < 8; e += 4) *(f32x4 *)(v + e) = *(__attribute__((address_space(3))) f32x4 *)(stage + row * PITCH + l % LPR * 8 + e);
-      if (m < left && n < g.N) epilogue<E>(g, m0 + m, n, v);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
+        for (int e = 0; e < 4; e++) {
+          auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][8 * h + e]), __float_as_uint(acc[i][j][8 * h + 4 + e]), false, false);
+          v[e] = __uint_as_float(two[0]), v[4 + e] = __uint_as_float(two[1]);
+        }
+        int64_t n = n1 + j * 32 + h * 16, at = row + m;
+        if (m >= left || n >= g.N) continue;
+        typename Vec<E>::v8 out;
+        if (bias)
+#pragma unroll
+          for (int e = 0; e < 8; e++) v[e] += (float)add[j][h][e];
+        if (ACT != OOB_ACT_NONE && g.Z) { /* rounded to the type, as y is: half the memory between the passes; act' sees the rounding, act does not */
+#pragma unroll
+          for (int e = 0; e < 8; e++) out[e] = (E)v[e];
+          store8<E>((E *)g.Z + at * g.ldz + n, out, g.N - n);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) out[e] = (E)activate(v[e], ACT);
+        store8<E>(C + at * g.ldc + n, out, g.N - n);
+      }
   }
 }
 
-template <class E, int TM, int TN, int WM, int WN, bool AK, bool BK> constexpr int lds_bytes() {
-  constexpr int stages = 2 * (TM + TN) * KSTEP * 2, out = WM * WN * 32 * (TN / WN + 4) * 4;
-  return stages > out ? stages : out;
-}
+/* Where a workgroup's tile lies; expert -1: nowhere. */
+struct Where { int expert, left, k; int64_t row, n0; const char *pa, *pb; }; /* rows of C from `row` on; k: depth */
 
-/* Rows of y (BK: W as it is) or of dx (W by its columns). */
-template <class E, int TM, int TN, int WM, int WN, bool BK, bool GATHER>
-__global__ __launch_bounds__(WM *WN * 64, 2) void k_experts(Experts x) {
-  __shared__ __attribute__((aligned(1024))) char mem[lds_bytes<E, TM, TN, WM, WN, true, BK>()];
-  Product g = x.g;
-  int64_t tn = g.tiles_n;
-  Found f = find(x.d, [&](int64_t n) { return (n + TM - 1) / TM * tn; },
-                 [&](int total) { return (int)blockIdx.x < total ? (int)xcd_order(blockIdx.x, total) : total; });
-  if (f.expert < 0) return;
+/* Rows of y (BK: W as it is), of dx (W by its columns) or, DW, the matrices dw[e] = dz^T x over the rows of e.  A workgroup takes one tile after the other, every
+ * gridDim-th: the first loads of the next are asked for before the present one's epilogue. */
+template <class E, int TM, int TN, int WM, int WN, bool BK, bool GATHER, bool DW> __global__ __launch_bounds__(WM *WN * 64, 2) void k_experts(Experts x) {
+  constexpr int THREADS = WM * WN * 64;
+  constexpr bool AK = !DW;
+  using TA = std::conditional_t<GATHER, Gathered<E, TM, THREADS>, Strip<E, TM, THREADS, AK>>;
+  using TB = Strip<E, TN, THREADS, BK>;
+  __shared__ __attribute__((aligned(1024))) char even_[TA::BYTES + TB::BYTES], odd_[TA::BYTES + TB::BYTES];
+  lds_char *even = (lds_char *)even_, *odd = (lds_char *)odd_;
+  const Product &g = x.g;
+  const int64_t da = AK ? KSTEP * 2 : KSTEP * 2 * g.lda, db = BK ? KSTEP * 2 : KSTEP * 2 * g.ldb;
+
   /* within an expert bands of eight rows of tiles, as in the dense product */
-  constexpr int BAND = 8;
-  int tm = (int)(((int64_t)f.rows + TM - 1) / TM), tile = (int)f.part, band = tile / (BAND * (int)tn), in = tile - band * BAND * (int)tn;
-  int high = tm - band * BAND < BAND ? tm - band * BAND : BAND;
-  int64_t m0 = (int64_t)(band * BAND + in % high) * TM, n0 = (int64_t)(in / high) * TN, left = f.rows - m0, row = (int64_t)f.first + m0;
+  auto band = [&](int tile, int tm, int tn, int &m, int &n) {
+    int in = tile % (8 * tn), first = tile / (8 * tn) * 8, high = tm - first < 8 ? tm - first : 8;
+    m = first + in % high, n = in / high;
+  };
+  auto locate = [&](int id) -> Where {
+    Where w{};
+    int m, n;
+    if constexpr (DW) { /* every XCD gets an eighth of each expert's tiles, neighbours of one another: experts differ in rows */
+      int per = g.tiles_m * g.tiles_n, part = (per + 7) / 8, in_e = id % (8 * part), tile = in_e % 8 * part + in_e / 8;
+      w.expert = tile < per ? id / (8 * part) : -1;
+      if (w.expert < 0) return w;
+      band(tile, g.tiles_m, g.tiles_n, m, n);
+      int64_t first, rows = rows_of(x.d, w.expert, first), m0 = (int64_t)m * TM;
+      first = uniform((int)first), w.k = uniform((int)rows);
+      w.n0 = (int64_t)n * TN, w.left = (int)(g.M - m0 < TM ? g.M - m0 : TM), w.row = (int64_t)w.expert * g.M + m0;
+      w.pa = (const char *)g.A + (first * g.lda + m0) * 2, w.pb = (const char *)g.B + (first * g.ldb + w.n0) * 2;
+    } else {
+      int64_t tn = g.tiles_n;
+      Found f = find(x.d, [&](int64_t r) { return (r + TM - 1) / TM * tn; }, [&](int total) { return id < total ? (int)xcd_order(id, total) : total; });
+      w.expert = f.expert;
+      if (w.expert < 0) return w;
+      band(f.part, (int)(((int64_t)f.rows + TM - 1) / TM), (int)tn, m, n);
+      int64_t m0 = (int64_t)m * TM;
+      w.n0 = (int64_t)n * TN, w.left = f.rows - m0 < TM ? (int)(f.rows - m0) : TM, w.row = f.first + m0, w.k = (int)g.K;
+      w.pa = (const char *)g.A + (GATHER ? 0 : w.row * g.lda * 2);
+      w.pb = (const char *)g.B + (f.expert * x.expert_stride + (BK ? w.n0 * g.ldb : w.n0)) * 2;
+    }
+    return w;
+  };
+  auto next_of = [&](int &id) -> Where { /* the next tile from number `id` on that is one */
+    Where w{};
+    w.expert = -1;
+    for (; id < x.ids; id += gridDim.x) {
+      w = locate(id);
+      if (w.expert >= 0 || !DW) break;
+    }
+    id += gridDim.x;
+    return w;
+  };
 
-  Tile<E, TN, WM * WN * 64, BK> tb;
-  tb.init(g.ldb, g.N - n0);
-  const char *B = (const char *)g.B + f.expert * x.expert_stride * 2;
-  const char *pb = B + (BK ? n0 * g.ldb : n0) * 2;
-  int64_t db = BK ? KSTEP * 2 : KSTEP * 2 * g.ldb;
-  int steps = (int)((g.K + KSTEP - 1) / KSTEP);
-  f32x16 acc[TM / WM / 32][TN / WN / 32];
-  if (GATHER) {
-    Gathered<E, TM, WM * WN * 64> ta;
-    ta.init(g.lda, left, x.rows + row, x.per, x.T);
-    multiply<E, TM, TN, WM, WN, true, BK>(ta, tb, (const char *)g.A, pb, KSTEP * 2, db, g.K, steps, (lds_char *)mem, acc);
-  } else {
-    Tile<E, TM, WM * WN * 64, true> ta;
-    ta.init(g.lda, left);
-    multiply<E, TM, TN, WM, WN, true, BK>(ta, tb, (const char *)g.A + row * g.lda * 2, pb, KSTEP * 2, db, g.K, steps, (lds_char *)mem, acc);
+  TA ta;
+  TB tb;
+  int kleft, id = blockIdx.x;
+  const char *pa, *pb;
+  auto load = [&](lds_char *to) __attribute__((always_inline)) { /* past the last step: nothing is read, zeros land */
+    ta.load(pa, to, kleft);
+    tb.load(pb, to + TA::BYTES, kleft);
+    pa += da, pb += db, kleft -= KSTEP;
+  };
+  auto begin = [&](const Where &w) __attribute__((always_inline)) {
+    if constexpr (GATHER) ta.init(g.lda, w.left, x.rows + w.row, x.per, x.T);
+    else ta.init(g.lda, w.left);
+    tb.init(g.ldb, g.N - w.n0);
+    pa = w.pa, pb = w.pb, kleft = w.k;
+    load(even);
+    load(odd);
+  };
+  Where w = next_of(id);
+  if (w.expert < 0) return;
+  begin(w);
+  for (;;) {
+    Where then = next_of(id);
+    f32x16 acc[TM / WM / 32][TN / WN / 32];
+    multiply<E, TM, TN, WM, WN, AK, BK, TA, TB>(load, (w.k + KSTEP - 1) / KSTEP, even, odd, acc);
+    if (then.expert >= 0) begin(then);
+    const E *bias = g.bias ? (const E *)g.bias + (int64_t)w.expert * g.N : nullptr;
+    switch (g.act) {
+      case OOB_ACT_RELU: finish<E, OOB_ACT_RELU, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0); break;
+      case OOB_ACT_SILU: finish<E, OOB_ACT_SILU, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0); break;
+      case OOB_ACT_GELU: finish<E, OOB_ACT_GELU, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0); break;
+      case OOB_ACT_GELU_TANH: finish<E, OOB_ACT_GELU_TANH, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0); break;
+      default: finish<E, OOB_ACT_NONE, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0);
+    }
+    if (then.expert < 0) return;
+    w = then;
   }
-  if (g.bias) g.bias = (const E *)g.bias + f.expert * g.N;
-  finish<E, TM, TN, WM, WN>(g, acc, (lds_char *)mem, row, left, n0);
-}
-
-/* dw[e] = dz^T x over the rows of e: A is dz, B is x, both with rows of k. */
-template <class E, int TM, int TN, int WM, int WN> __global__ __launch_bounds__(WM *WN * 64, 2) void k_experts_dw(Experts x) {
-  __shared__ __attribute__((aligned(1024))) char mem[lds_bytes<E, TM, TN, WM, WN, false, false>()];
-  Product g = x.g;
-  int64_t per = (int64_t)g.tiles_m * g.tiles_n, id = xcd_order(blockIdx.x, gridDim.x);
-  int e = (int)(id / per), tile = (int)(id % per);
-  constexpr int BAND = 8;
-  int band = tile / (BAND * g.tiles_n), high = g.tiles_m - band * BAND < BAND ? g.tiles_m - band * BAND : BAND, in = tile - band * BAND * g.tiles_n;
-  int64_t m0 = (int64_t)(band * BAND + in % high) * TM, n0 = (int64_t)(in / high) * TN;
-  int64_t first, rows = rows_of(x.d, e, first);
-  first = uniform((int)first), rows = uniform((int)rows);
-  Tile<E, TM, WM * WN * 64, false> ta;
-  Tile<E, TN, WM * WN * 64, false> tb;
-  ta.init(g.lda, g.M - m0);
-  tb.init(g.ldb, g.N - n0);
-  f32x16 acc[TM / WM / 32][TN / WN / 32];
-  multiply<E, TM, TN, WM, WN, false, false>(ta, tb, (const char *)g.A + (first * g.lda + m0) * 2, (const char *)g.B + (first * g.ldb + n0) * 2,
-                                            KSTEP * 2 * g.lda, KSTEP * 2 * g.ldb, rows, (int)((rows + KSTEP - 1) / KSTEP), (lds_char *)mem, acc);
-  g.C = (E *)g.C + (int64_t)e * g.M * g.ldc;
-  finish<E, TM, TN, WM, WN>(g, acc, (lds_char *)mem, m0, g.M - m0, n0);
 }
 
 /* ---- rows of another pitch or order in the workspace: what the tiles' loads cannot take as it lies ------------------------------
@@ -363,22 +482,17 @@ int choose_dw(int64_t M, int64_t N, int E) {
   return 64;
 }
 
-template <class E, bool BK, bool GATHER> int products(Experts x, hipStream_t st) {
-  int tile = choose_tile(x.d.R, x.d.E, x.g.N);
-  x.g.tiles_n = (int)tiles(x.g.N, tile);
-  unsigned n = (unsigned)(row_tiles(x.d.R, x.d.E, tile) * x.g.tiles_n);
-  if (tile == 256) k_experts<E, 256, 256, 2, 4, BK, GATHER><<<n, 512, 0, st>>>(x);
-  else if (tile == 128) k_experts<E, 128, 128, 2, 2, BK, GATHER><<<n, 256, 0, st>>>(x);
-  else k_experts<E, 64, 64, 2, 2, BK, GATHER><<<n, 256, 0, st>>>(x);
-  return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
+template <class E, int TILE, int WN, bool BK, bool GATHER, bool DW> void launch(Experts x, hipStream_t st) {
+  x.g.tiles_m = (int)tiles(x.g.M, TILE), x.g.tiles_n = (int)tiles(x.g.N, TILE);
+  x.ids = (int)(DW ? x.d.E * up((int64_t)x.g.tiles_m * x.g.tiles_n, 8) : row_tiles(x.d.R, x.d.E, TILE) * x.g.tiles_n);
+  int most = TILE == 256 ? 256 : TILE == 128 ? 512 : 1024; /* that run at once: one, two, four a compute unit */
+  k_experts<E, TILE, TILE, 2, WN, BK, GATHER, DW><<<x.ids < most ? x.ids : most, 128 * WN, 0, st>>>(x);
 }
-template <class E> int products_dw(Experts x, hipStream_t st) {
-  int tile = choose_dw(x.g.M, x.g.N, x.d.E);
-  x.g.tiles_m = (int)tiles(x.g.M, tile), x.g.tiles_n = (int)tiles(x.g.N, tile);
-  unsigned n = (unsigned)((int64_t)x.d.E * x.g.tiles_m * x.g.tiles_n);
-  if (tile == 256) k_experts_dw<E, 256, 256, 2, 4><<<n, 512, 0, st>>>(x);
-  else if (tile == 128) k_experts_dw<E, 128, 128, 2, 2><<<n, 256, 0, st>>>(x);
-  else k_experts_dw<E, 64, 64, 2, 2><<<n, 256, 0, st>>>(x);
+template <class E, bool BK, bool GATHER, bool DW> int products(Experts x, hipStream_t st) {
+  int tile = DW ? choose_dw(x.g.M, x.g.N, x.d.E) : choose_tile(x.d.R, x.d.E, x.g.N);
+  if (tile == 256) launch<E, 256, 4, BK, GATHER, DW>(x, st);
+  else if (tile == 128) launch<E, 128, 2, BK, GATHER, DW>(x, st);
+  else launch<E, 64, 2, BK, GATHER, DW>(x, st);
   return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
 }
 
@@ -392,7 +506,7 @@ bool fits(int64_t blocks) { return blocks < (int64_t)1 << 31; }
 /* Workgroups of the smallest tiles and of the copies, 256 threads each. */
 bool launches_fit(const oob_expert_linear_t *p) {
   int64_t most = (p->N > p->K ? p->N : p->K) + 64;
-  return fits(row_tiles(p->R, p->E, 64) * tiles(most, 64)) && fits(p->E * tiles(p->N, 64) * tiles(p->K, 64)) &&
+  return fits(row_tiles(p->R, p->E, 64) * tiles(most, 64)) && fits(p->E * up(tiles(p->N, 64) * tiles(p->K, 64), 8)) &&
          fits((p->R + p->E * p->N) * ((up(p->K, 8)) / 8) / 256 + 1);
 }
 
@@ -412,7 +526,7 @@ template <class E> int forward(const oob_expert_linear_t *p, Arena w, hipStream_
   x.g.A = a.p, x.g.lda = a.ld, x.g.B = b.p, x.g.ldb = b.ld, x.expert_stride = b.part;
   x.g.N = p->N, x.g.K = p->K, x.g.bias = p->bias, x.g.C = p->y, x.g.ldc = p->y_stride, x.g.Z = p->z, x.g.ldz = p->z_stride, x.g.act = p->act;
   x.d = {p->offsets, p->E, p->R}, x.rows = p->rows, x.per = p->per, x.T = p->T;
-  return gather ? products<E, true, true>(x, st) : products<E, true, false>(x, st);
+  return gather ? products<E, true, true, false>(x, st) : products<E, true, false, false>(x, st);
 }
 
 /* dz, the runs' sums, then what the larger product takes */
@@ -463,7 +577,7 @@ template <class E> int backward(const oob_expert_linear_t *p, const oob_expert_l
     Experts x{};
     x.g.A = dz.p, x.g.lda = dz.ld, x.g.B = b.p, x.g.ldb = b.ld, x.expert_stride = b.part;
     x.g.N = p->K, x.g.K = p->N, x.g.C = g->dx, x.g.ldc = g->dx_stride, x.d = d;
-    rc = products<E, false, false>(x, st);
+    rc = products<E, false, false, false>(x, st);
   }
   if (rc == OOB_OK && g->dw) {
     Arena more = w;
@@ -472,7 +586,7 @@ template <class E> int backward(const oob_expert_linear_t *p, const oob_expert_l
     Experts x{};
     x.g.A = dz.p, x.g.lda = dz.ld, x.g.B = b.p, x.g.ldb = b.ld;
     x.g.M = p->N, x.g.N = p->K, x.g.C = g->dw, x.g.ldc = p->K, x.d = d;
-    rc = products_dw<E>(x, st);
+    rc = products<E, false, false, true>(x, st);
   }
   return rc;
 }
