@@ -1,25 +1,31 @@
 /* The norm over many tensors, and the tensors scaled so that it does not pass a bound. */
+#include <algorithm>
+#include <utility>
+#include <vector>
+
 #include "oob_expert.h"
 #include "oob_layer_device.h"
 
 namespace layer {
 namespace {
 
-/* Tensors of one launch: their addresses travel with the launch's arguments (4 KB), nothing is copied to the device. */
-constexpr int TENSORS = 112;
+/* Tensors of one launch: their addresses travel with the launch's arguments (4 KB), nothing is copied to the device.  Few tensors take a launch with fewer
+ * arguments, which is quicker to enqueue. */
+constexpr int TENSORS = 112, FEW = 24;
 constexpr int64_t CHUNK = 32768; /* values a workgroup takes at a time */
+constexpr int64_t MOST = 0x7f000000; /* chunks of a launch */
 constexpr int GROUPS = 2048;     /* workgroups of a launch at most, so that every workgroup of the second pass can add up their sums itself */
-struct Tensors {
-  const void *from[TENSORS];
-  void *to[TENSORS];
-  int64_t sizes[TENSORS];
-  int32_t until[TENSORS]; /* chunks of the tensors up to this one */
-  uint8_t types[TENSORS];
+template <int N> struct Tensors {
+  const void *from[N];
+  void *to[N];
+  int64_t sizes[N];
+  int32_t until[N]; /* chunks of the tensors up to this one */
+  uint8_t types[N];
   int n;
 };
-static_assert(sizeof(Tensors) <= 3800, "arguments of a launch");
+static_assert(sizeof(Tensors<TENSORS>) <= 3800, "arguments of a launch");
 
-__device__ inline int find(const Tensors &t, int chunk, int64_t &first) {
+template <int N> __device__ inline int find(const Tensors<N> &t, int chunk, int64_t &first) {
   int lo = 0, hi = t.n - 1;
   while (lo < hi) {
     int mid = (lo + hi) / 2;
@@ -58,7 +64,7 @@ template <class E> __device__ inline double squares(const E *from, int64_t size,
   return s;
 }
 
-__global__ __launch_bounds__(256) void k_squares(Tensors t, double *sums) {
+template <int N> __global__ __launch_bounds__(256) void k_squares(Tensors<N> t, double *sums) {
   double s = 0;
   for (int c = blockIdx.x; c < t.until[t.n - 1]; c += gridDim.x) {
     int64_t first;
@@ -100,7 +106,7 @@ template <class E> __device__ inline void scale(const E *from, E *to, int64_t si
 }
 
 /* Each workgroup adds up the first pass's sums itself, in the same order, in place of a launch between the two. */
-__global__ __launch_bounds__(256) void k_scale(Tensors t, const double *sums, int n, float max_norm, const float *given, float *norm) {
+template <int N> __global__ __launch_bounds__(256) void k_scale(Tensors<N> t, const double *sums, int n, float max_norm, const float *given, float *norm) {
   double s = given ? (double)*given : sqrt(add_up(sums, n));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)s;
   float factor = s > max_norm && s < INFINITY ? (float)(max_norm / s) : 1.f;
@@ -126,38 +132,66 @@ bool tensors_ok(int n, const void *const *from, void *const *to, const int64_t *
   return true;
 }
 
+bool overlap(int n, const void *const *to, const int64_t *sizes, const int *types) try {
+  std::vector<std::pair<uintptr_t, uintptr_t>> parts;
+  for (int i = 0; i < n; i++)
+    if (sizes[i]) parts.push_back({(uintptr_t)to[i], (uintptr_t)to[i] + (uintptr_t)sizes[i] * (types[i] == OOB_FP32 ? 4 : 2)});
+  std::sort(parts.begin(), parts.end());
+  for (size_t i = 1; i < parts.size(); i++)
+    if (parts[i].first < parts[i - 1].second) return true;
+  return false;
+} catch (...) { /* no host memory: refused, nothing passes the C entry */
+  return true;
+}
+
 /* The next launch's tensors from number `at` on: those with values, as many as fit. */
-bool next(int &at, int n, const void *const *from, void *const *to, const int64_t *sizes, const int *types, Tensors &t) {
+template <int N> bool next(int &at, int n, const void *const *from, void *const *to, const int64_t *sizes, const int *types, Tensors<N> &t) {
   int64_t chunks = 0;
-  for (t.n = 0; at < n && t.n < TENSORS; at++) {
-    if (sizes && sizes[at] > 0) {
+  for (t.n = 0; at < n && t.n < N; at++) {
+    if (sizes[at] > 0) {
       int64_t more = (sizes[at] + CHUNK - 1) / CHUNK;
-      if (chunks + more > 0x7fffffff) break;
+      if (chunks + more > MOST) break;
       chunks += more;
-      t.from[t.n] = from ? from[at] : nullptr, t.to[t.n] = to ? to[at] : nullptr;
-      t.sizes[t.n] = sizes[at], t.until[t.n] = (int32_t)chunks, t.types[t.n] = types ? (uint8_t)types[at] : 0;
+      t.from[t.n] = from[at], t.to[t.n] = to ? to[at] : nullptr;
+      t.sizes[t.n] = sizes[at], t.until[t.n] = (int32_t)chunks, t.types[t.n] = (uint8_t)types[at];
       t.n++;
     }
   }
   return t.n > 0;
 }
-int groups_of(const Tensors &t) { return t.until[t.n - 1] < GROUPS ? t.until[t.n - 1] : GROUPS; }
+int groups_of(int64_t chunks) { return chunks < GROUPS ? (int)chunks : GROUPS; }
 
-int sums_of(int n, const int64_t *sizes) {
-  Tensors t;
-  int at = 0, sums = 0;
-  while (next(at, n, nullptr, nullptr, sizes, nullptr, t)) sums += groups_of(t);
-  return sums;
+/* Sums of the first pass at most: every launch's workgroups, in launches of either kind. */
+int64_t sums_of(int n, const int64_t *sizes) {
+  int64_t chunks = 0, launches = n <= FEW ? 1 : (n + TENSORS - 1) / TENSORS;
+  for (int i = 0; i < n; i++) chunks += (sizes[i] + CHUNK - 1) / CHUNK;
+  launches += chunks / (MOST / 2); /* a launch that ends early holds more than half of what it may */
+  return chunks < launches * GROUPS ? chunks : launches * GROUPS;
 }
 
-int first_pass(int n, const void *const *from, const int64_t *sizes, const int *types, double *sums, hipStream_t st) {
-  Tensors t;
+template <int N> int first_pass(int n, const void *const *from, const int64_t *sizes, const int *types, double *sums, hipStream_t st) {
+  Tensors<N> t;
   int at = 0, done = 0;
   while (next(at, n, from, nullptr, sizes, types, t)) {
-    k_squares<<<groups_of(t), 256, 0, st>>>(t, sums + done);
-    done += groups_of(t);
+    int groups = groups_of(t.until[t.n - 1]);
+    k_squares<<<groups, 256, 0, st>>>(t, sums + done);
+    done += groups;
   }
   return done;
+}
+int first_pass(int n, const void *const *from, const int64_t *sizes, const int *types, double *sums, hipStream_t st) {
+  return n <= FEW ? first_pass<FEW>(n, from, sizes, types, sums, st) : first_pass<TENSORS>(n, from, sizes, types, sums, st);
+}
+
+template <int N> int second_pass(int n, const void *const *from, void *const *to, const int64_t *sizes, const int *types, const double *sums, int count,
+                                 float max_norm, const float *given, float *norm, hipStream_t st) {
+  Tensors<N> t;
+  int at = 0, launches = 0;
+  while (next(at, n, from, to, sizes, types, t)) {
+    k_scale<<<groups_of(t.until[t.n - 1]), 256, 0, st>>>(t, sums, count, max_norm, given, launches ? nullptr : norm);
+    launches++;
+  }
+  return launches;
 }
 
 }  // namespace
@@ -169,7 +203,11 @@ extern "C" size_t oob_clip_workspace_size(int n, const int64_t *sizes) {
   if (n < 0 || !sizes) return 0;
   for (int i = 0; i < n; i++)
     if (sizes[i] < 0 || sizes[i] >= (int64_t)1 << 40) return 0;
-  return (size_t)up((int64_t)sums_of(n, sizes) * 8, 256);
+  return (size_t)up(sums_of(n, sizes) * 8, 256);
+}
+
+extern "C" int oob_clip_overlap(int n, const void *const *to, const int64_t *sizes, const int *types) {
+  return n > 0 && to && sizes && types && overlap(n, to, sizes, types);
 }
 
 extern "C" int oob_clip_norm(int n, const void *const *from, const int64_t *sizes, const int *types, float *norm, void *workspace, size_t bytes,
@@ -186,15 +224,15 @@ extern "C" int oob_clip_norm(int n, const void *const *from, const int64_t *size
 extern "C" int oob_clip_scale(int n, const void *const *from, void *const *to, const int64_t *sizes, const int *types, float max_norm,
                               const float *given, float *norm, void *workspace, size_t bytes, void *stream) {
   if (!tensors_ok(n, from, to, sizes, types) || (n && !to) || !(max_norm >= 0) || !multiple(workspace, 256)) return OOB_EINVAL;
-  if (!multiple(given, 4) || !multiple(norm, 4) || (!given && !norm)) return OOB_EINVAL;
+  if (!multiple(given, 4) || !multiple(norm, 4) || (!given && !norm) || overlap(n, to, sizes, types)) return OOB_EINVAL;
   size_t need = n && !given ? oob_clip_workspace_size(n, sizes) : 0;
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
   hipStream_t st = (hipStream_t)stream;
-  int sums = given ? 0 : first_pass(n, from, sizes, types, (double *)workspace, st);
-  Tensors t;
-  int at = 0, launches = 0;
-  while (next(at, n, from, to, sizes, types, t))
-    k_scale<<<groups_of(t), 256, 0, st>>>(t, (const double *)workspace, sums, max_norm, given, given || launches++ ? nullptr : norm);
-  if (!given && !launches) k_norm<<<1, 256, 0, st>>>((const double *)workspace, 0, norm);
+  double *sums = (double *)workspace;
+  int count = given ? 0 : first_pass(n, from, sizes, types, sums, st);
+  if (given) norm = nullptr;
+  int launches = n <= FEW ? second_pass<FEW>(n, from, to, sizes, types, sums, count, max_norm, given, norm, st)
+                          : second_pass<TENSORS>(n, from, to, sizes, types, sums, count, max_norm, given, norm, st);
+  if (norm && !launches) k_norm<<<1, 256, 0, st>>>(sums, 0, norm);
   return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
 }

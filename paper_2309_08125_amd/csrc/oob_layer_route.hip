@@ -15,15 +15,37 @@ __device__ inline void put(void *p, int dtype, int64_t at, float v) {
   else ((fp16 *)p)[at] = (fp16)v;
 }
 
-/* Over runs of `lanes` lanes (a power of two). */
-template <class K> __device__ inline K max_over(K v, int lanes) {
-  for (int o = 1; o < lanes; o *= 2) {
-    K u = __shfl_xor(v, o);
-    v = u > v ? u : v;
+/* What a lane's partner holds at each level of a reduction over neighbouring lanes: within rows of 16 by DPP moves (swapped pairs, pairs of pairs, mirrored
+ * halves and rows: below each level all lanes of a part hold the same), across them by the swaps of rows and of halves. */
+template <class F> __device__ inline uint32_t over(uint32_t v, int lanes, F f) {
+  if (lanes > 1) v = f(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true));
+  if (lanes > 2) v = f(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true));
+  if (lanes > 4) v = f(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true));
+  if (lanes > 8) v = f(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xf, 0xf, true));
+  if (lanes > 16) {
+    auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = f(r[0], r[1]);
+  }
+  if (lanes > 32) {
+    auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = f(r[0], r[1]);
   }
   return v;
 }
-template <class K> __device__ inline K sum_over(K v, int lanes) {
+/* Over runs of `lanes` lanes (a power of two). */
+__device__ inline uint32_t max_over(uint32_t v, int lanes) { return over(v, lanes, [](uint32_t a, uint32_t b) { return a > b ? a : b; }); }
+__device__ inline float max_over(float v, int lanes) {
+  return __uint_as_float(over(__float_as_uint(v), lanes, [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+}
+__device__ inline float sum_over(float v, int lanes) {
+  return __uint_as_float(over(__float_as_uint(v), lanes, [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+__device__ inline uint64_t max_over(uint64_t v, int lanes) { /* the larger high half, then the larger low half of those that have it */
+  uint32_t hi = max_over((uint32_t)(v >> 32), lanes);
+  uint32_t lo = max_over((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u, lanes);
+  return (uint64_t)hi << 32 | lo;
+}
+__device__ inline double sum_over(double v, int lanes) {
   for (int o = 1; o < lanes; o *= 2) v += __shfl_xor(v, o);
   return v;
 }
@@ -49,92 +71,174 @@ __device__ inline uint64_t key_of(double v) {
 /* sigmoid(l) e^-m: with m the largest min(l, 0) of several, their ratios keep all digits however small they are. */
 __device__ inline float sigmoid_over(float l, float m) { return expf(fminf(l, 0.f) - m) / (1 + expf(-fabsf(l))); }
 
+__device__ inline float value_of(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); } /* of key_of(float), NaN aside */
+
 /* ---- routing -------------------------------------------------------------------------------------------------------------
  * A token takes a run of lanes, each V neighbouring experts of one group: a choice is a maximum over registers, then over the run; of
- * equals the first expert is that of the first lane that holds it, which a vote finds. */
+ * equals the first expert is that of the first lane that holds it, which a vote finds.
+ * Scores with a bias, and sums of groups, are compared as 64-bit programs do, to the last digit.  They are formed in 32 bits first: only where two that are
+ * compared lie closer than their errors allow is the token done again in 64 (16384 tokens, 256 experts in 8 groups: 54 us all in 64 bits). */
 struct Route {
   oob_route p;
   int lanes;    /* a token's: a power of two, at least k */
   int per;      /* experts of a group */
   int in_group; /* lanes of a group: a power of two */
+  int whole;    /* a lane's V experts all exist and lie at a multiple of their size */
 };
 
+template <int V> struct Token {
+  float x[V];       /* logits; -inf: closed or absent */
+  int there, group; /* so many of the V exist */
+  int e0;
+};
+
+/* Keys of scores in type F (double, float). */
+template <class F, int V, class K> __device__ inline F keys_of(const Route &r, const Token<V> &a, float top, K (&key)[V], F &best, F &next) {
+  F s[V], total = 0;
+  for (int i = 0; i < V; i++) {
+    if constexpr (sizeof(F) == 8) s[i] = a.x[i] == -INFINITY ? 0. : r.p.score == OOB_ROUTE_SOFTMAX ? exp((double)a.x[i] - (double)top) : 1 / (1 + exp(-(double)a.x[i]));
+    else {
+      float e = __builtin_amdgcn_exp2f((r.p.score == OOB_ROUTE_SOFTMAX ? a.x[i] - top : -a.x[i]) * 1.44269504f);
+      s[i] = a.x[i] == -INFINITY ? 0.f : r.p.score == OOB_ROUTE_SOFTMAX ? e : __builtin_amdgcn_rcpf(1 + e);
+    }
+    total += s[i];
+  }
+  F part = 1;
+  if (r.p.score == OOB_ROUTE_SOFTMAX) {
+    total = sum_over(total, r.lanes);
+    if constexpr (sizeof(F) == 4) part = 1 / total;
+  }
+  best = next = -INFINITY;
+  for (int i = 0; i < V; i++) {
+    F c = -INFINITY;
+    if (a.x[i] != -INFINITY) {
+      c = s[i];
+      if (r.p.score == OOB_ROUTE_SOFTMAX) c = sizeof(F) == 8 ? s[i] / total : s[i] * part;
+      if (r.p.bias) c += r.p.bias[a.e0 + i];
+    }
+    key[i] = i < a.there ? key_of(c) : 0;
+    if (c > best) next = best, best = c;
+    else if (c > next) next = c;
+  }
+  return total;
+}
+
+/* By how much a score and a bias of at most 4 formed in 32 bits may be off: the sum of up to 1024 exponentials 1.3e-6 of itself (16 in a row, then 6
+ * halvings), the exponentials' arguments 4e-7, three more roundings 2e-7, the bias's addition 3e-7.  Larger biases are left to 64 bits. */
+constexpr float OFF = 4e-6f, LARGE = 4.f;
+
+/* Closes the experts of the groups that are not kept; false: in 32 bits, two groups' sums lie too close to tell. */
+template <class F, int V, class K> __device__ inline bool groups(const Route &r, const Token<V> &a, K (&key)[V], F best, F next) {
+  const oob_route &p = r.p;
+  for (int o = 1; o < r.in_group; o *= 2) {
+    F b = __shfl_xor(best, o), n = __shfl_xor(next, o);
+    F low = b > best ? best : b; /* second of the four: the lower first or one of the seconds */
+    best = b > best ? b : best;
+    n = n > next ? n : next;
+    next = low > n ? low : n;
+  }
+  K of = a.group < p.groups ? key_of(p.group_best == 2 && r.per > 1 ? best + next : best) : 0;
+  bool kept = false, sure = true;
+  K most = 0;
+  for (int n = 0; n < p.keep_groups; n++) {
+    most = max_over(of, r.lanes);
+    int won = first_of(of == most, r.lanes) / r.in_group;
+    if (a.group == won) kept = true, of = 0;
+  }
+  if constexpr (sizeof(F) == 4) {
+    K beyond = max_over(of, r.lanes);
+    if (beyond) sure = value_of(most) - value_of(beyond) > 6 * OFF; /* two scores each, and their sum's rounding */
+  }
+  if (!kept)
+    for (int i = 0; i < V; i++) key[i] = 0;
+  return sure;
+}
+
+/* The k largest keys; lane j gets the number and the logit of choice j.  False: in 32 bits (CHECK), two in a row lie too close to tell. */
+template <bool CHECK, int V, class K> __device__ inline bool choose(const Route &r, const Token<V> &a, K (&key)[V], int &expert, float &mine) {
+  const int L = r.lanes, l = lane() & (L - 1), k = r.p.k;
+  bool sure = true;
+  K last = 0;
+  for (int j = 0; j < k + (CHECK ? 1 : 0); j++) {
+    K best = key[0];
+    for (int i = 1; i < V; i++) best = key[i] > best ? key[i] : best;
+    K most = max_over(best, L);
+    if constexpr (CHECK) {
+      if (j && most) sure = sure && value_of(last) - value_of(most) > 2 * OFF; /* NaN and infinities: not sure */
+      last = most;
+      if (j == k) break;
+    }
+    int won = first_of(best == most, L), at = 0; /* the maximum is never 0: k experts are there */
+    float value = a.x[0];
+    for (int i = V - 1; i > 0; i--)
+      if (key[i] == most) at = i, value = a.x[i];
+    if (key[0] == most) at = 0, value = a.x[0];
+    if (l == won)
+      for (int i = 0; i < V; i++)
+        if (i == at) key[i] = 0;
+    int from = (lane() & ~(L - 1)) + won, number = a.e0 + at;
+    if (L == 64) {
+      won = uniform(won);
+      value = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(value), won)), number = __builtin_amdgcn_readlane(number, won);
+    } else {
+      value = __shfl(value, from), number = __shfl(number, from);
+    }
+    if (l == j) mine = value, expert = number;
+  }
+  return sure;
+}
+
 template <int V, bool SCORES> __global__ __launch_bounds__(256) void k_route(Route r) {
-  using K = std::conditional_t<SCORES, uint64_t, uint32_t>;
   const oob_route &p = r.p;
   const int L = r.lanes, l = lane() & (L - 1);
   const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
   const bool live = t < p.T; /* runs of lanes as a whole: the others take part in the exchanges and write nothing */
-  const int group = l / r.in_group, in = l % r.in_group * V, e0 = group * r.per + in;
-  const int there = group < p.groups ? r.per - in : 0; /* of this lane's experts: so many exist */
-  float x[V], top = -INFINITY;
-  for (int i = 0; i < V; i++) {
-    x[i] = live && i < there ? logit(p.logits, p.dtype, t * p.logits_stride + e0 + i) : -INFINITY;
-    top = fmaxf(top, x[i]);
-  }
-  if (p.score == OOB_ROUTE_SOFTMAX) top = max_over(top, L);
-
-  K key[V];
-  double total = 0; /* of softmax */
-  if constexpr (SCORES) { /* in 64 bits: sums of a score and a bias that lie close are told apart as a 64-bit program does */
-    double s[V];
-    for (int i = 0; i < V; i++) {
-      s[i] = x[i] == -INFINITY ? 0. : p.score == OOB_ROUTE_SOFTMAX ? exp((double)x[i] - (double)top) : 1 / (1 + exp(-(double)x[i]));
-      total += s[i];
-    }
-    if (p.score == OOB_ROUTE_SOFTMAX) total = sum_over(total, L);
-    double best = -INFINITY, next = -INFINITY; /* of the group */
-    for (int i = 0; i < V; i++) {
-      double c = -INFINITY;
-      if (x[i] != -INFINITY) {
-        c = p.score == OOB_ROUTE_SOFTMAX ? s[i] / total : s[i];
-        if (p.bias) c += p.bias[e0 + i];
+  Token<V> a;
+  int in = l % r.in_group * V;
+  a.group = l / r.in_group, a.e0 = a.group * r.per + in;
+  a.there = a.group < p.groups ? r.per - in : 0;
+  int64_t at = t * p.logits_stride + a.e0;
+  if (V == 4 && r.whole) {
+    bool here = live && a.there > 0;
+    if (p.dtype == OOB_FP32) {
+      f32x4 v = here ? *(const f32x4 *)((const float *)p.logits + at) : f32x4{0, 0, 0, 0};
+      for (int i = 0; i < V; i++) a.x[i] = here ? v[i] : -INFINITY;
+    } else {
+      uint64_t v = here ? *(const uint64_t *)((const uint16_t *)p.logits + at) : 0;
+      for (int i = 0; i < V; i++) {
+        uint16_t h = (uint16_t)(v >> (16 * i));
+        a.x[i] = !here ? -INFINITY : p.dtype == OOB_BF16 ? (float)__builtin_bit_cast(bf16, h) : (float)__builtin_bit_cast(fp16, h);
       }
-      key[i] = i < there ? key_of(c) : 0;
-      if (c > best) next = best, best = c;
-      else if (c > next) next = c;
-    }
-    if (p.groups > 1) {
-      for (int o = 1; o < r.in_group; o *= 2) {
-        double b = __shfl_xor(best, o), n = __shfl_xor(next, o);
-        double low = b > best ? best : b; /* second of the four: the lower first or one of the seconds */
-        best = b > best ? b : best;
-        n = n > next ? n : next;
-        next = low > n ? low : n;
-      }
-      uint64_t of = group < p.groups ? key_of(p.group_best == 2 && r.per > 1 ? best + next : best) : 0;
-      bool kept = false;
-      for (int n = 0; n < p.keep_groups; n++) {
-        int won = first_of(of == max_over(of, L), L) / r.in_group;
-        if (group == won) kept = true, of = 0;
-      }
-      if (!kept)
-        for (int i = 0; i < V; i++) key[i] = 0;
     }
   } else {
-    for (int i = 0; i < V; i++) key[i] = i < there ? key_of(x[i]) : 0;
+    for (int i = 0; i < V; i++) a.x[i] = live && i < a.there ? logit(p.logits, p.dtype, at + i) : -INFINITY;
   }
+  float top = a.x[0];
+  for (int i = 1; i < V; i++) top = fmaxf(top, a.x[i]);
+  if (p.score == OOB_ROUTE_SOFTMAX) top = max_over(top, L);
 
-  float mine = -INFINITY; /* lane j gets the logit of choice j */
-  for (int j = 0; j < p.k; j++) {
-    K best = key[0];
-    for (int i = 1; i < V; i++) best = key[i] > best ? key[i] : best;
-    K most = max_over(best, L);
-    int won = first_of(best == most, L), at = 0; /* the maximum is never 0: k experts are there */
-    float value = 0;
-    if (l == won) {
-      for (int i = V - 1; i >= 0; i--)
-        if (key[i] == most) at = i, value = x[i];
-      for (int i = 0; i < V; i++)
-        if (i == at) key[i] = 0;
+  float mine = -INFINITY, all = 0;
+  int expert = 0;
+  if constexpr (SCORES) {
+    uint32_t key[V];
+    float best, next;
+    all = keys_of<float>(r, a, top, key, best, next);
+    bool sure = true;
+    if (p.bias)
+      for (int i = 0; i < V; i++) sure = sure && (i >= a.there || fabsf(p.bias[a.e0 + i]) <= LARGE);
+    if (p.groups > 1) sure = groups(r, a, key, best, next) && sure;
+    sure = choose<true>(r, a, key, expert, mine) && sure;
+    if (__ballot(live && !sure)) {
+      uint64_t wide[V];
+      double b, n;
+      keys_of<double>(r, a, top, wide, b, n);
+      if (p.groups > 1) groups(r, a, wide, b, n);
+      choose<false>(r, a, wide, expert, mine);
     }
-    int from = (lane() & ~(L - 1)) + won;
-    value = __shfl(value, from);
-    int number = __shfl(e0 + at, from);
-    if (l == j) {
-      mine = value;
-      if (live) p.experts[t * p.k + j] = number;
-    }
+  } else {
+    uint32_t key[V];
+    for (int i = 0; i < V; i++) key[i] = i < a.there ? key_of(a.x[i]) : 0;
+    choose<false>(r, a, key, expert, mine);
   }
 
   const bool has = l < p.k;
@@ -142,19 +246,21 @@ template <int V, bool SCORES> __global__ __launch_bounds__(256) void k_route(Rou
   if (p.renormalize) {
     float m = max_over(!has || mine != mine ? -INFINITY : p.score == OOB_ROUTE_SIGMOID ? fminf(mine, 0.f) : mine, L);
     float s = !has || mine == -INFINITY ? 0.f : p.score == OOB_ROUTE_SIGMOID ? sigmoid_over(mine, m) : expf(mine - m);
-    float all = sum_over(s, L);
-    w = all == 0 ? 0.f : s / all;
+    float sum = sum_over(s, L);
+    w = sum == 0 ? 0.f : s / sum;
   } else if (p.score == OOB_ROUTE_SIGMOID) {
     w = sigmoid_over(mine, 0.f);
   } else {
-    float all = (float)total;
     if (!SCORES) {
-      for (int i = 0; i < V; i++) all += x[i] == -INFINITY ? 0.f : expf(x[i] - top);
+      for (int i = 0; i < V; i++) all += a.x[i] == -INFINITY ? 0.f : expf(a.x[i] - top);
       all = sum_over(all, L);
     }
     w = mine == -INFINITY ? 0.f : expf(mine - top) / all;
   }
-  if (live && has) p.weights[t * p.k + l] = w * p.scale;
+  if (live && has) {
+    p.experts[t * p.k + l] = expert;
+    p.weights[t * p.k + l] = w * p.scale;
+  }
 }
 
 /* ---- its gradient: a token takes a run of lanes, lane j its choice j; the row is put together in LDS, where the choices add to it
@@ -164,7 +270,7 @@ struct RouteGrad {
   const float *dweights;
   void *dlogits;
   int64_t ld;
-  int lanes;
+  int lanes, whole; /* whole: rows of dlogits can be written four values at a time */
 };
 
 __global__ __launch_bounds__(256) void k_route_grad(RouteGrad g) {
@@ -217,8 +323,19 @@ __global__ __launch_bounds__(256) void k_route_grad(RouteGrad g) {
     if (l == j && has) row[e] += add;
     __builtin_amdgcn_wave_barrier();
   }
-  if (live)
+  if (!live) return;
+  if (g.whole && p.dtype == OOB_FP32) {
+    for (int i = 4 * l; i < p.E; i += 4 * L) *(f32x4 *)((float *)g.dlogits + t * g.ld + i) = f32x4{row[i], row[i + 1], row[i + 2], row[i + 3]};
+  } else if (g.whole) {
+    for (int i = 4 * l; i < p.E; i += 4 * L) {
+      uint64_t v = 0;
+      for (int e = 0; e < 4; e++)
+        v |= (uint64_t)(p.dtype == OOB_BF16 ? __builtin_bit_cast(uint16_t, (bf16)row[i + e]) : __builtin_bit_cast(uint16_t, (fp16)row[i + e])) << (16 * e);
+      *(uint64_t *)((uint16_t *)g.dlogits + t * g.ld + i) = v;
+    }
+  } else {
     for (int i = l; i < p.E; i += L) put(g.dlogits, p.dtype, t * g.ld + i, row[i]);
+  }
 }
 
 int ceil2(int n) {
@@ -249,16 +366,17 @@ template <int V> void route(const Route &r, hipStream_t st) {
 }
 
 /* ---- the chosen pairs in order of their experts ------------------------------------------------------------------------
- * A stable sort by counting.  A workgroup takes a run of pairs, 1024 at a time, a wave 64 of them; a pair's rank among the wave's of the same
- * expert comes from votes over the expert's bits, the counts of the waves lie in LDS.  Where there are more pairs than one workgroup takes, a first launch
- * leaves every run's counts, and each workgroup of the second adds up those of the runs before its own. */
+ * A stable sort by counting.  A workgroup takes a run of pairs, each of its 16 waves up to 8 times 64 neighbours: a pair's rank among the 64 of the same
+ * expert comes from votes over the expert's bits, among the wave's before them from the wave's own counts in LDS.  Where there are more pairs than one
+ * workgroup takes, a first launch leaves every run's counts, and each workgroup of the second adds up all runs' and those of the runs before its own. */
 struct Rows {
   const int32_t *experts;
-  int64_t n, per; /* pairs, pairs of a run (a multiple of 1024) */
+  int64_t n, per; /* pairs, pairs of a run */
   int first, E, runs, bits;
   int32_t *offsets, *rows, *place, *counts; /* counts [runs][E] */
 };
-constexpr int PAIRS = 1024, WAVES = PAIRS / 64;
+constexpr int WAVES = 16, THREADS = WAVES * 64, ROUNDS = 8;
+constexpr int64_t PAIRS = THREADS * ROUNDS; /* that a workgroup takes at a time */
 
 /* The lanes of the wave that hold the same number of `bits` bits. */
 __device__ inline uint64_t alike(int e, int bits) {
@@ -269,98 +387,137 @@ __device__ inline uint64_t alike(int e, int bits) {
   }
   return m;
 }
-__device__ inline int expert_of(const Rows &r, int64_t i) { /* E: left out */
-  if (i >= r.n) return r.E;
+__device__ inline int expert_of(const Rows &r, int64_t i, int64_t end) { /* E: left out */
+  if (i >= end) return r.E;
   int64_t e = (int64_t)r.experts[i] - r.first;
   return e >= 0 && e < r.E ? (int)e : r.E;
 }
 
-/* Counts of a run's experts to `count` in LDS [E + 1]. */
-__device__ inline void count_run(const Rows &r, int64_t from, int64_t to, int *count) {
-  for (int e = threadIdx.x; e <= r.E; e += PAIRS) count[e] = 0;
-  __syncthreads();
-  for (int64_t at = from; at < to; at += PAIRS) {
-    int e = expert_of(r, at + threadIdx.x);
-    uint64_t same = alike(e, r.bits);
-    if (__ffsll((unsigned long long)same) - 1 == lane()) atomicAdd(count + e, __popcll(same)); /* whole numbers: their order does not count */
+/* Counts per wave in LDS; a chunk has up to PAIRS pairs, a wave `rounds` times 64 of them in a row. */
+struct Counts { uint16_t of[WAVES][OOB_EXPERT_MAX + 2]; };
+
+__device__ inline void count(const Rows &r, int64_t from, int64_t end, int rounds, Counts &c, int (&e)[ROUNDS], int (&rank)[ROUNDS]) {
+  int wave = threadIdx.x / 64;
+  volatile uint16_t *mine = c.of[wave];
+  int64_t at = from + (int64_t)wave * rounds * 64 + lane();
+#pragma unroll
+  for (int i = 0; i < ROUNDS; i++) e[i] = i < rounds ? expert_of(r, at + i * 64, end) : r.E;
+  for (int x = lane(); x <= r.E; x += 64) mine[x] = 0;
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int i = 0; i < ROUNDS; i++) {
+    if (i >= rounds) break;
+    uint64_t same = alike(e[i], r.bits);
+    int before = mine[e[i]], in = __popcll(same & ((1ull << lane()) - 1));
+    rank[i] = before + in;
+    __builtin_amdgcn_wave_barrier();
+    if (in == 0) mine[e[i]] = (uint16_t)(before + __popcll(same));
+    __builtin_amdgcn_wave_barrier();
   }
   __syncthreads();
 }
-
-__global__ __launch_bounds__(PAIRS) void k_rows_count(Rows r) {
-  __shared__ int count[OOB_EXPERT_MAX + 1];
-  int64_t from = blockIdx.x * r.per, to = from + r.per < r.n ? from + r.per : r.n;
-  count_run(r, from, to, count);
-  for (int e = threadIdx.x; e < r.E; e += PAIRS) r.counts[(int64_t)blockIdx.x * r.E + e] = count[e];
-}
-
-__global__ __launch_bounds__(PAIRS) void k_rows(Rows r) {
-  __shared__ int base[OOB_EXPERT_MAX + 1];             /* the next row of each expert; before that, this run's counts */
-  __shared__ uint16_t of_wave[WAVES][OOB_EXPERT_MAX + 2]; /* counts of a wave, then what the waves before it have */
-  __shared__ int sums[WAVES];
-  int64_t from = blockIdx.x * r.per, to = from + r.per < r.n ? from + r.per : r.n;
-  int all = 0, before = 0; /* of this thread's expert: pairs, and those of earlier runs */
-  if (r.runs == 1) {
-    count_run(r, from, to, base);
-    if ((int)threadIdx.x < r.E) all = base[threadIdx.x];
-    __syncthreads();
-  } else if ((int)threadIdx.x < r.E) {
-    for (int i = 0; i < r.runs; i++) {
-      int c = r.counts[(int64_t)i * r.E + threadIdx.x];
-      if (i < (int)blockIdx.x) before += c;
-      all += c;
+/* The counts of this thread's expert over the waves; they become what the waves before have. */
+__device__ inline int waves_before(const Rows &r, Counts &c) {
+  int all = 0;
+  if ((int)threadIdx.x < r.E)
+#pragma unroll
+    for (int w = 0; w < WAVES; w++) {
+      int n = c.of[w][threadIdx.x];
+      c.of[w][threadIdx.x] = (uint16_t)all;
+      all += n;
     }
+  return all;
+}
+__device__ inline int rounds_of(int64_t pairs) { return pairs >= PAIRS ? ROUNDS : (int)((pairs + THREADS - 1) / THREADS); }
+
+__global__ __launch_bounds__(THREADS) void k_rows_count(Rows r) {
+  __shared__ Counts c;
+  int64_t from = blockIdx.x * r.per, end = from + r.per < r.n ? from + r.per : r.n;
+  int all = 0, e[ROUNDS], rank[ROUNDS];
+  for (; from < end; from += PAIRS) {
+    count(r, from, end, rounds_of(end - from), c, e, rank);
+    all += waves_before(r, c);
+    __syncthreads();
   }
-  int end = all; /* of the experts up to this thread's */
+  if ((int)threadIdx.x < r.E) r.counts[(int64_t)blockIdx.x * r.E + threadIdx.x] = all;
+}
+
+__global__ __launch_bounds__(THREADS) void k_rows(Rows r) {
+  __shared__ Counts c;
+  __shared__ int base[OOB_EXPERT_MAX + 1], total_of[OOB_EXPERT_MAX], sums[WAVES];
+  int64_t from = blockIdx.x * r.per, end = from + r.per < r.n ? from + r.per : r.n;
+  int e[ROUNDS], rank[ROUNDS], all = 0, before = 0, here = 0; /* of this thread's expert: pairs, those of earlier runs, those of this chunk */
+  if (r.runs == 1) {
+    count(r, from, end, rounds_of(end - from), c, e, rank);
+    all = here = waves_before(r, c);
+  } else {
+    /* all threads share the counts: the threads of an expert every so many runs; whole numbers, so that the order of their additions does not count */
+    int stride = 1;
+    while (stride < r.E) stride *= 2;
+    int x = threadIdx.x % stride, part = threadIdx.x / stride, parts = THREADS / stride;
+    if ((int)threadIdx.x < r.E) base[threadIdx.x] = total_of[threadIdx.x] = 0;
+    __syncthreads();
+    if (x < r.E) {
+#pragma unroll 8
+      for (int i = part; i < r.runs; i += parts) {
+        int n = r.counts[(int64_t)i * r.E + x];
+        if (i < (int)blockIdx.x) before += n;
+        all += n;
+      }
+      atomicAdd(base + x, before);
+      atomicAdd(total_of + x, all);
+    }
+    __syncthreads();
+    all = before = 0;
+    if ((int)threadIdx.x < r.E) before = base[threadIdx.x], all = total_of[threadIdx.x];
+  }
+  int upto = all; /* pairs of the experts up to this thread's */
   for (int o = 1; o < 64; o *= 2) {
-    int u = __shfl_up(end, o);
-    if (lane() >= o) end += u;
+    int u = __shfl_up(upto, o);
+    if (lane() >= o) upto += u;
   }
-  if (lane() == 63) sums[threadIdx.x / 64] = end;
+  if (lane() == 63) sums[threadIdx.x / 64] = upto;
   __syncthreads();
   int total = 0;
   for (int w = 0; w < WAVES; w++) {
-    if (w < (int)threadIdx.x / 64) end += sums[w];
+    if (w < (int)threadIdx.x / 64) upto += sums[w];
     total += sums[w];
   }
   if ((int)threadIdx.x < r.E) {
-    base[threadIdx.x] = end - all + before;
+    base[threadIdx.x] = upto - all + before;
     if (blockIdx.x == 0) {
-      r.offsets[threadIdx.x + 1] = end;
+      r.offsets[threadIdx.x + 1] = upto;
       if (threadIdx.x == 0) r.offsets[0] = 0;
     }
   }
-  __syncthreads();
-  for (int64_t at = from; at < to; at += PAIRS) {
-    int64_t i = at + threadIdx.x;
-    int e = expert_of(r, i), wave = threadIdx.x / 64;
-    uint64_t same = alike(e, r.bits);
-    int rank = __popcll(same & ((1ull << lane()) - 1));
-    for (int x = threadIdx.x; x < WAVES * (r.E + 1); x += PAIRS) of_wave[x / (r.E + 1)][x % (r.E + 1)] = 0;
-    __syncthreads();
-    if (rank == 0) of_wave[wave][e] = (uint16_t)__popcll(same);
-    __syncthreads();
-    int more = 0;
-    if ((int)threadIdx.x < r.E)
-      for (int w = 0; w < WAVES; w++) {
-        int c = of_wave[w][threadIdx.x];
-        of_wave[w][threadIdx.x] = (uint16_t)more;
-        more += c;
-      }
-    __syncthreads();
-    if (i < r.n) {
-      int row = e < r.E ? base[e] + of_wave[wave][e] + rank : -1;
-      r.place[i] = row;
-      if (row >= 0) r.rows[row] = (int32_t)i;
-      if (i >= total) r.rows[i] = -1; /* rows behind the last: no pair goes there */
+  for (bool counted = r.runs == 1; from < end; from += PAIRS, counted = false) {
+    int rounds = rounds_of(end - from), wave = threadIdx.x / 64;
+    if (!counted) {
+      count(r, from, end, rounds, c, e, rank);
+      here = waves_before(r, c);
     }
     __syncthreads();
-    if ((int)threadIdx.x < r.E) base[threadIdx.x] += more;
+#pragma unroll
+    for (int i = 0; i < ROUNDS; i++) {
+      int64_t at = from + ((int64_t)wave * rounds + i) * 64 + lane();
+      if (i < rounds && at < end) {
+        int row = e[i] < r.E ? base[e[i]] + c.of[wave][e[i]] + rank[i] : -1;
+        r.place[at] = row;
+        if (row >= 0) r.rows[row] = (int32_t)at;
+        if (at >= total) r.rows[at] = -1; /* rows behind the last: no pair goes there */
+      }
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < r.E) base[threadIdx.x] += here;
   }
 }
 
-/* Pairs of a run: one workgroup does the smallest numbers alone; beyond, 1024 each as long as there are no more than 256 runs. */
-int64_t run_of(int64_t n) { return n <= PAIRS * 2 ? up(n, PAIRS) : up((n + 255) / 256, PAIRS); }
+/* One workgroup does what it takes at a time alone; beyond, runs of 1024 pairs or more, 256 at most. */
+int64_t run_of(int64_t n) {
+  if (n <= PAIRS) return PAIRS;
+  int64_t run = up((n + 255) / 256, THREADS);
+  return run <= PAIRS ? run : up(run, PAIRS);
+}
 
 }  // namespace
 }  // namespace layer
@@ -370,13 +527,15 @@ using namespace layer;
 extern "C" int oob_expert_route(const oob_route *p, void *stream) {
   if (!route_ok(p, true)) return OOB_EINVAL;
   if (p->T == 0) return OOB_OK;
-  Route r{*p, 0, p->E / p->groups, 0};
+  Route r{*p, 0, p->E / p->groups, 0, 0};
   int groups = ceil2(p->groups), least = ceil2(p->k); /* lanes of a token: a power of two of them for each group */
   int in_group = ceil2((r.per + 3) / 4);              /* four experts a lane where there are enough lanes */
   while (groups * in_group > 64) in_group /= 2;
   while (groups * in_group < least) in_group *= 2;
   r.lanes = groups * in_group, r.in_group = in_group;
   int v = (r.per + in_group - 1) / in_group;
+  size_t four = p->dtype == OOB_FP32 ? 16 : 8;
+  r.whole = r.per % 4 == 0 && multiple(p->logits, four) && p->logits_stride % 4 == 0;
   hipStream_t st = (hipStream_t)stream;
   if (v <= 1) route<1>(r, st);
   else if (v <= 2) route<2>(r, st);
@@ -392,7 +551,7 @@ extern "C" int oob_expert_route_backward(const oob_route *p, const float *dweigh
   if (p->T == 0) return OOB_OK;
   size_t of = p->dtype == OOB_FP32 ? 4 : 2;
   if (!dweights || !dlogits || dlogits_stride < p->E || !multiple(dweights, 4) || !multiple(dlogits, of)) return OOB_EINVAL;
-  RouteGrad g{*p, dweights, dlogits, dlogits_stride, 0};
+  RouteGrad g{*p, dweights, dlogits, dlogits_stride, 0, p->E % 4 == 0 && dlogits_stride % 4 == 0 && multiple(dlogits, 4 * of)};
   int lanes = ceil2((p->E + 7) / 8), least = ceil2(p->k);
   g.lanes = lanes > 64 ? 64 : lanes < least ? least : lanes;
   unsigned n = (unsigned)((p->T * g.lanes + 255) / 256);
@@ -412,11 +571,11 @@ extern "C" int oob_expert_rows(const int32_t *experts, int64_t n, int first, int
   if (!multiple(experts, 4) || !multiple(offsets, 4) || !multiple(rows, 4) || !multiple(place, 4) || !multiple(workspace, 256)) return OOB_EINVAL;
   size_t need = oob_expert_rows_workspace_size(n, E);
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
-  Rows r{experts, n, n ? run_of(n) : PAIRS, first, E, 1, 0, offsets, rows, place, (int32_t *)workspace};
+  Rows r{experts, n, run_of(n), first, E, 1, 0, offsets, rows, place, (int32_t *)workspace};
   if (n) r.runs = (int)((n + r.per - 1) / r.per);
   while (1 << r.bits <= E) r.bits++; /* E itself stands for those left out */
   hipStream_t st = (hipStream_t)stream;
-  if (r.runs > 1) k_rows_count<<<r.runs, PAIRS, 0, st>>>(r);
-  k_rows<<<r.runs, PAIRS, 0, st>>>(r);
+  if (r.runs > 1) k_rows_count<<<r.runs, THREADS, 0, st>>>(r);
+  k_rows<<<r.runs, THREADS, 0, st>>>(r);
   return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
 }

@@ -13,7 +13,7 @@ from .layer import _act, _dtype, _rows, _stride
 SCORES = {"softmax": 0, "sigmoid": 1}
 EXPERT_SYMBOLS = ["oob_expert_route", "oob_expert_route_backward", "oob_expert_rows", "oob_expert_rows_workspace_size", "oob_expert_linear",
                   "oob_expert_linear_workspace_size", "oob_expert_linear_backward", "oob_expert_linear_backward_workspace_size", "oob_expert_sum",
-                  "oob_expert_sum_backward", "oob_clip_norm", "oob_clip_scale", "oob_clip_workspace_size"]
+                  "oob_expert_sum_backward", "oob_clip_norm", "oob_clip_overlap", "oob_clip_scale", "oob_clip_workspace_size"]
 MAX_EXPERTS, MAX_CHOICES = 1024, 64
 
 
@@ -38,6 +38,7 @@ class oob_expert_sum_t(C.Structure):
                [(n, C.c_void_p) for n in ("y", "place", "weights", "residual", "out")] + [(n + "_stride", C.c_int64) for n in ("y", "residual", "out")]
 
 
+_calls = {}
 _lib = torch = None
 
 
@@ -53,13 +54,13 @@ def _load():
                            ("oob_expert_rows", [p, n, i, i, p, p, p, p, C.c_size_t, p]),
                            ("oob_expert_linear", [linear, p, C.c_size_t, p]), ("oob_expert_linear_backward", [linear, grad, p, C.c_size_t, p]),
                            ("oob_expert_sum", [total, p]), ("oob_expert_sum_backward", [total, p, n, p, n, p, p]),
-                           ("oob_clip_norm", [i, p, p, p, p, p, C.c_size_t, p]),
+                           ("oob_clip_overlap", [i, p, p, p]), ("oob_clip_norm", [i, p, p, p, p, p, C.c_size_t, p]),
                            ("oob_clip_scale", [i, p, p, p, p, C.c_float, p, p, p, C.c_size_t, p])):
-            call = getattr(L, name)
+            call = _calls[name] = getattr(L, name)
             call.argtypes, call.restype = args, C.c_int
         for name, args in (("oob_expert_rows", [n, i]), ("oob_expert_linear", [linear]), ("oob_expert_linear_backward", [linear, grad]),
                            ("oob_clip", [i, p])):
-            size = getattr(L, name + "_workspace_size")
+            size = _calls[name + "_workspace_size"] = getattr(L, name + "_workspace_size")
             size.argtypes, size.restype = args, C.c_size_t
         _lib = L
     return _lib
@@ -69,20 +70,21 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _enqueue(name, device, *args, size=None, nbytes=0):
-    """Enqueues a call on the current stream of `device`, with a workspace where it takes one (size: its arguments)."""
-    at = device.index
-    if at is not None and at != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return _enqueue(name, torch.device("cuda"), *args, size=size)
-    more = ()
-    ws = None
-    if size is not None:
-        nbytes = getattr(_lib, size[0])(*size[1:])
+def _enqueue(name, at, *args, size=None):
+    """Enqueues a call on the current stream of GPU number `at`, with a workspace where it takes one (size: what that goes by)."""
+    if at != torch._C._cuda_getDevice():
+        with torch.cuda.device(at):
+            return _enqueue(name, at, *args, size=size)
+    stream = layer._stream(at)
+    if size is None:
+        rc = _calls[name](*args, stream)
+    else:
+        nbytes = _calls[size[0]](*size[1:])
         # the workspace is held until the call is enqueued; torch gives it to later work of this stream only
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-        more = (_ptr(ws), nbytes)
-    binding.check(getattr(_lib, name)(*args, *more, layer._stream(torch.cuda.current_device() if at is None else at)), name)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+        rc = _calls[name](*args, ws.data_ptr() if nbytes else None, nbytes, stream)
+    if rc:
+        binding.check(rc, name)
 
 
 def _numbers(t, shape, device, name):
@@ -132,10 +134,10 @@ def route(logits, k, score="softmax", bias=None, groups=1, keep_groups=None, gro
     args.groups, args.keep_groups, args.group_best = groups, keep_groups, group_best
     if bias is not None:
         args.bias = _floats(bias, (args.E,), logits.device, "bias")
-    experts = torch.empty((*logits.shape[:-1], k), dtype=torch.int32, device=logits.device)
-    weights = torch.empty((*logits.shape[:-1], k), dtype=torch.float32, device=logits.device)
+    shape = (*logits.shape[:-1], k)
+    experts, weights = logits.new_empty(shape, dtype=torch.int32), logits.new_empty(shape, dtype=torch.float32)
     args.experts, args.weights = experts.data_ptr(), weights.data_ptr()
-    _enqueue("oob_expert_route", logits.device, C.byref(args))
+    _enqueue("oob_expert_route", logits.get_device(), C.byref(args))
     return experts, weights
 
 
@@ -147,7 +149,7 @@ def route_backward(dweights, logits, experts, score="softmax", renormalize=True,
     args.experts = _numbers(experts, shape, logits.device, "experts")
     d = _floats(dweights, shape, logits.device, "dweights")
     out = logits.new_empty(logits.shape)
-    _enqueue("oob_expert_route_backward", logits.device, C.byref(args), d, out.data_ptr(), args.E)
+    _enqueue("oob_expert_route_backward", logits.get_device(), C.byref(args), d, out.data_ptr(), args.E)
     return out
 
 
@@ -163,21 +165,24 @@ def expert_rows(experts, E, first=0):
         raise ValueError("experts: contiguous int32 on the GPU are wanted")
     if not (1 <= E <= MAX_EXPERTS and -1 << 31 <= first < 1 << 31):
         raise ValueError(f"1 to {MAX_EXPERTS} experts are supported")
-    n = experts.numel()
-    offsets, rows, place = (torch.empty(s, dtype=torch.int32, device=experts.device) for s in (E + 1, n, experts.shape))
-    _enqueue_rows(experts, n, first, E, offsets, rows, place)
+    n, new = experts.numel(), experts.new_empty
+    offsets, rows, place = new(E + 1), new(n), new(experts.shape)
+    at = experts.get_device()
+    if at != torch._C._cuda_getDevice():
+        with torch.cuda.device(at):
+            _enqueue_rows(experts, n, first, E, offsets, rows, place, at)
+    else:
+        _enqueue_rows(experts, n, first, E, offsets, rows, place, at)
     return offsets, rows, place
 
 
-def _enqueue_rows(experts, n, first, E, offsets, rows, place):
-    at = experts.device.index
-    if at is not None and at != torch.cuda.current_device():
-        with torch.cuda.device(at):
-            return _enqueue_rows(experts, n, first, E, offsets, rows, place)
+def _enqueue_rows(experts, n, first, E, offsets, rows, place, at):
     nbytes = _lib.oob_expert_rows_workspace_size(n, E)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=experts.device) if nbytes else None
-    binding.check(_lib.oob_expert_rows(experts.data_ptr(), n, first, E, offsets.data_ptr(), rows.data_ptr(), place.data_ptr(), _ptr(ws), nbytes,
-                                       layer._stream(experts.get_device())), "oob_expert_rows")
+    ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+    rc = _lib.oob_expert_rows(experts.data_ptr(), n, first, E, offsets.data_ptr(), rows.data_ptr(), place.data_ptr(), ws.data_ptr() if nbytes else None,
+                              nbytes, layer._stream(at))
+    if rc:
+        binding.check(rc, "oob_expert_rows")
 
 
 def _linear_args(x, w, offsets, rows, act):
@@ -222,7 +227,7 @@ def expert_linear(x, w, offsets, bias=None, rows=None, act="none", keep=False, o
         args.bias = bias.data_ptr()
     args.y, args.y_stride, args.z, args.z_stride = y.data_ptr(), _stride(y), _ptr(z), args.N
     ref = C.byref(args)
-    _enqueue("oob_expert_linear", x.device, ref, size=("oob_expert_linear_workspace_size", ref))
+    _enqueue("oob_expert_linear", x.get_device(), ref, size=("oob_expert_linear_workspace_size", ref))
     return (y, z) if keep else y
 
 
@@ -263,7 +268,7 @@ def expert_linear_backward(dy, x, w, offsets, z=None, rows=None, act="none", nee
     db = x.new_empty((args.E, args.N)) if "b" in need else None
     grad = oob_expert_linear_grad(dy2.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db), _stride(dy2), args.K if dx is None else _stride(dx))
     refs = C.byref(args), C.byref(grad)
-    _enqueue("oob_expert_linear_backward", x.device, *refs, size=("oob_expert_linear_backward_workspace_size", *refs))
+    _enqueue("oob_expert_linear_backward", x.get_device(), *refs, size=("oob_expert_linear_backward_workspace_size", *refs))
     return dx, dw, db
 
 
@@ -294,7 +299,7 @@ def expert_sum(y, place, weights=None, residual=None):
         r = _rows(residual, args.C, y, "residual")
         args.residual, args.residual_stride = r.data_ptr(), _stride(r)
     args.out, args.out_stride = out.data_ptr(), args.C
-    _enqueue("oob_expert_sum", y.device, C.byref(args))
+    _enqueue("oob_expert_sum", y.get_device(), C.byref(args))
     return out
 
 
@@ -315,26 +320,23 @@ def expert_sum_backward(dout, y, place, weights=None, need=("y", "weights"), out
     if "y" in need:
         dy = y.new_empty((args.R, args.C)) if out is None else _out(out, args.R, args.C, y, "out")
     dweights = torch.empty(place.shape, dtype=torch.float32, device=y.device) if "weights" in need else None
-    _enqueue("oob_expert_sum_backward", y.device, C.byref(args), d.data_ptr(), _stride(d), _ptr(dy), args.C if dy is None else _stride(dy),
+    _enqueue("oob_expert_sum_backward", y.get_device(), C.byref(args), d.data_ptr(), _stride(d), _ptr(dy), args.C if dy is None else _stride(dy),
              _ptr(dweights))
     return dy, dweights
 
 
 def _tensors(tensors, name):
-    """Host arrays of the tensors' addresses, sizes and types."""
+    """Host arrays of the tensors' addresses, sizes and types, and their GPU."""
     n = len(tensors)
     if not n:
         raise ValueError(f"{name}: no tensors")
-    device, codes, sizes, types = tensors[0].device, layer._TYPES, [], []
-    _dtype(tensors[0], wide=True)  # fills the table of types
     at = tensors[0].get_device()
-    for t in tensors:
-        code = codes.get(t.dtype)
-        if code is None or at < 0 or t.get_device() != at or not t.is_contiguous():
-            raise ValueError(f"{name}: contiguous tensors of bfloat16, float16 or float32 on one GPU are wanted")
-        sizes.append(t.numel())
-        types.append(code)
-    return n, device, (C.c_void_p * n)(*[t.data_ptr() for t in tensors]), (C.c_int64 * n)(*sizes), (C.c_int * n)(*types)
+    _dtype(tensors[0], wide=True)  # fills the table of types
+    codes = layer._TYPES
+    types = [codes.get(t.dtype, -1) for t in tensors]
+    if at < 0 or min(types) < 0 or not all([t.is_contiguous() and t.get_device() == at for t in tensors]):
+        raise ValueError(f"{name}: contiguous tensors of bfloat16, float16 or float32 on one GPU are wanted")
+    return n, at, (C.c_void_p * n)(*[t.data_ptr() for t in tensors]), [t.numel() for t in tensors], types
 
 
 def gradient_norm(tensors):
@@ -342,9 +344,10 @@ def gradient_norm(tensors):
     device; squares are summed in 64 bits."""
     _load()
     tensors = list(tensors)
-    n, device, ptrs, sizes, types = _tensors(tensors, "tensors")
-    norm = torch.empty((), dtype=torch.float32, device=device)
-    _enqueue_clip("oob_clip_norm", device, n, sizes, (n, ptrs, sizes, types, norm.data_ptr()))
+    n, at, ptrs, sizes, types = _tensors(tensors, "tensors")
+    sizes, types = (C.c_int64 * n)(*sizes), (C.c_int * n)(*types)
+    norm = tensors[0].new_empty((), dtype=torch.float32)
+    _enqueue("oob_clip_norm", at, n, ptrs, sizes, types, norm.data_ptr(), size=("oob_clip_workspace_size", n, sizes))
     return norm
 
 
@@ -353,37 +356,29 @@ def clip_gradients(tensors, max_norm, norm=None, out=None):
     returns the norm.
 
     norm: a float32 scalar on the tensors' device to go by in place of gradient_norm(tensors), one that all ranks have added up, say.
-    out: as many tensors of the same shapes and types for the results; without it they are changed in place (no two may share memory)."""
+    out: as many tensors of the same sizes and types for the results; without it they are changed in place (no two may share memory)."""
     _load()
     tensors = list(tensors)
-    n, device, ptrs, sizes, types = _tensors(tensors, "tensors")
+    n, at, ptrs, sizes, types = _tensors(tensors, "tensors")
     max_norm = float(max_norm)
     if not (max_norm >= 0):
         raise ValueError("max_norm: at least 0")
     to = ptrs
     if out is not None:
-        out = list(out)
-        m, at, to, out_sizes, out_types = _tensors(out, "out")
-        if not (m == n and at == device and list(out_sizes) == list(sizes) and list(out_types) == list(types)):
+        m, of, to, out_sizes, out_types = _tensors(list(out), "out")
+        if not (m == n and of == at and out_sizes == sizes and out_types == types):
             raise ValueError("out: not like the tensors")
-    taken = sorted((a, s * (4 if t == 2 else 2)) for a, s, t in zip(to, sizes, types) if s)
-    if any(a + b > c for (a, b), (c, _) in zip(taken, taken[1:])):
+    sizes, types = (C.c_int64 * n)(*sizes), (C.c_int * n)(*types)
+    if _lib.oob_clip_overlap(n, to, sizes, types):
         raise ValueError("tensors that are written share memory")
     given = None
     if norm is not None:
-        given = _floats(norm, norm.shape, device, "norm")
+        given = _floats(norm, norm.shape, tensors[0].device, "norm")
         if norm.numel() != 1:
             raise ValueError("norm: one value is wanted")
+        size = ("oob_clip_workspace_size", 0, sizes)
     else:
-        norm = torch.empty((), dtype=torch.float32, device=device)
-    _enqueue_clip("oob_clip_scale", device, n, sizes, (n, ptrs, to, sizes, types, max_norm, given, None if given else norm.data_ptr()), given is None)
+        norm = tensors[0].new_empty((), dtype=torch.float32)
+        size = ("oob_clip_workspace_size", n, sizes)
+    _enqueue("oob_clip_scale", at, n, ptrs, to, sizes, types, max_norm, given, None if given else norm.data_ptr(), size=size)
     return norm
-
-
-def _enqueue_clip(name, device, n, sizes, args, sums=True):
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return _enqueue_clip(name, device, n, sizes, args, sums)
-    nbytes = _lib.oob_clip_workspace_size(n, sizes) if sums else 0
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    binding.check(getattr(_lib, name)(*args, _ptr(ws), nbytes, layer._stream(device.index)), name)
