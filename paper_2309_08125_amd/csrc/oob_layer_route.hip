@@ -34,6 +34,9 @@ template <class F> __device__ inline uint32_t over(uint32_t v, int lanes, F f) {
 }
 /* Over runs of `lanes` lanes (a power of two). */
 __device__ inline uint32_t max_over(uint32_t v, int lanes) { return over(v, lanes, [](uint32_t a, uint32_t b) { return a > b ? a : b; }); }
+__device__ inline int min_over(int v, int lanes) { /* of numbers that are not negative */
+  return (int)over((uint32_t)v, lanes, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
 __device__ inline float max_over(float v, int lanes) {
   return __uint_as_float(over(__float_as_uint(v), lanes, [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
 }
@@ -49,13 +52,6 @@ __device__ inline double sum_over(double v, int lanes) {
   for (int o = 1; o < lanes; o *= 2) v += __shfl_xor(v, o);
   return v;
 }
-/* The first lane of this lane's run for which `is` holds, counted in the run; -1: none. */
-__device__ inline int first_of(bool is, int lanes) {
-  uint64_t who = __ballot(is) >> (lane() & ~(lanes - 1));
-  if (lanes < 64) who &= (1ull << lanes) - 1;
-  return __ffsll((unsigned long long)who) - 1;
-}
-
 /* Numbers in the order of what they stand for: 0 is nothing (absent or taken), 1 a NaN, -inf and all else above. */
 __device__ inline uint32_t key_of(float v) {
   if (v != v) return 1;
@@ -74,8 +70,9 @@ __device__ inline float sigmoid_over(float l, float m) { return expf(fminf(l, 0.
 __device__ inline float value_of(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); } /* of key_of(float), NaN aside */
 
 /* ---- routing -------------------------------------------------------------------------------------------------------------
- * A token takes a run of lanes, each V neighbouring experts of one group: a choice is a maximum over registers, then over the run; of
- * equals the first expert is that of the first lane that holds it, which a vote finds.
+ * A token takes a run of lanes, each V neighbouring experts of one group: a choice is a maximum over registers, then over the run, and of those that hold it the
+ * smallest number.  What bounds it is instructions (16384 tokens, 256 experts in 8 groups, float32: 1070 a wave of two tokens, 25 us; a large copy would read
+ * the logits in 3.3): with four experts a lane reductions make most of them (46 us), with 16 too few waves hide each other's waits (28 us).
  * Scores with a bias, and sums of groups, are compared as 64-bit programs do, to the last digit.  They are formed in 32 bits first: only where two that are
  * compared lie closer than their errors allow is the token done again in 64 (16384 tokens, 256 experts in 8 groups: 54 us all in 64 bits). */
 struct Route {
@@ -83,17 +80,17 @@ struct Route {
   int lanes;    /* a token's: a power of two, at least k */
   int per;      /* experts of a group */
   int in_group; /* lanes of a group: a power of two */
-  int whole;    /* a lane's V experts all exist and lie at a multiple of their size */
+  int whole, whole_bias; /* a lane's logits, biases can be loaded four at a time */
 };
 
 template <int V> struct Token {
-  float x[V];       /* logits; -inf: closed or absent */
+  float x[V], bias[V]; /* logits, -inf: closed or absent; 0 without a bias */
   int there, group; /* so many of the V exist */
   int e0;
 };
 
 /* Keys of scores in type F (double, float). */
-template <class F, int V, class K> __device__ inline F keys_of(const Route &r, const Token<V> &a, float top, K (&key)[V], F &best, F &next) {
+template <class F, int V, class K> __device__ __forceinline__ F keys_of(const Route &r, const Token<V> &a, int L, float top, K (&key)[V], F &best, F &next) {
   F s[V], total = 0;
   for (int i = 0; i < V; i++) {
     if constexpr (sizeof(F) == 8) s[i] = a.x[i] == -INFINITY ? 0. : r.p.score == OOB_ROUTE_SOFTMAX ? exp((double)a.x[i] - (double)top) : 1 / (1 + exp(-(double)a.x[i]));
@@ -105,7 +102,7 @@ template <class F, int V, class K> __device__ inline F keys_of(const Route &r, c
   }
   F part = 1;
   if (r.p.score == OOB_ROUTE_SOFTMAX) {
-    total = sum_over(total, r.lanes);
+    total = sum_over(total, L);
     if constexpr (sizeof(F) == 4) part = 1 / total;
   }
   best = next = -INFINITY;
@@ -114,11 +111,12 @@ template <class F, int V, class K> __device__ inline F keys_of(const Route &r, c
     if (a.x[i] != -INFINITY) {
       c = s[i];
       if (r.p.score == OOB_ROUTE_SOFTMAX) c = sizeof(F) == 8 ? s[i] / total : s[i] * part;
-      if (r.p.bias) c += r.p.bias[a.e0 + i];
+      if (r.p.bias) c += a.bias[i];
     }
     key[i] = i < a.there ? key_of(c) : 0;
-    if (c > best) next = best, best = c;
-    else if (c > next) next = c;
+    F low = c > best ? best : c; /* a NaN is neither */
+    best = c > best ? c : best;
+    next = low > next ? low : next;
   }
   return total;
 }
@@ -128,7 +126,7 @@ template <class F, int V, class K> __device__ inline F keys_of(const Route &r, c
 constexpr float OFF = 4e-6f, LARGE = 4.f;
 
 /* Closes the experts of the groups that are not kept; false: in 32 bits, two groups' sums lie too close to tell. */
-template <class F, int V, class K> __device__ inline bool groups(const Route &r, const Token<V> &a, K (&key)[V], F best, F next) {
+template <class F, int V, class K> __device__ __forceinline__ bool groups(const Route &r, const Token<V> &a, int L, K (&key)[V], F best, F next) {
   const oob_route &p = r.p;
   for (int o = 1; o < r.in_group; o *= 2) {
     F b = __shfl_xor(best, o), n = __shfl_xor(next, o);
@@ -141,12 +139,12 @@ template <class F, int V, class K> __device__ inline bool groups(const Route &r,
   bool kept = false, sure = true;
   K most = 0;
   for (int n = 0; n < p.keep_groups; n++) {
-    most = max_over(of, r.lanes);
-    int won = first_of(of == most, r.lanes) / r.in_group;
+    most = max_over(of, L);
+    int won = min_over(of == most ? a.group : 1 << 30, L);
     if (a.group == won) kept = true, of = 0;
   }
   if constexpr (sizeof(F) == 4) {
-    K beyond = max_over(of, r.lanes);
+    K beyond = max_over(of, L);
     if (beyond) sure = value_of(most) - value_of(beyond) > 6 * OFF; /* two scores each, and their sum's rounding */
   }
   if (!kept)
@@ -154,43 +152,48 @@ template <class F, int V, class K> __device__ inline bool groups(const Route &r,
   return sure;
 }
 
-/* The k largest keys; lane j gets the number and the logit of choice j.  False: in 32 bits (CHECK), two in a row lie too close to tell. */
-template <bool CHECK, int V, class K> __device__ inline bool choose(const Route &r, const Token<V> &a, K (&key)[V], int &expert, float &mine) {
-  const int L = r.lanes, l = lane() & (L - 1), k = r.p.k;
+/* The k largest keys; lane j gets the number of choice j.  CHECK: keys of 32 bits whose lowest bits have given way to the number in the lane (no two of a lane
+ * are alike then, which saves a third of the instructions); false where two in a row lie too close to tell. */
+template <bool CHECK, int V, class K> __device__ __forceinline__ bool choose(const Route &r, const Token<V> &a, int L, K (&key)[V], int &expert) {
+  const int l = lane() & (L - 1), k = r.p.k;
   bool sure = true;
   K last = 0;
+  if constexpr (CHECK)
+#pragma unroll
+    for (int i = 0; i < V; i++) key[i] = key[i] ? (key[i] & ~(K)31) | (V - 1 - i) : 0;
   for (int j = 0; j < k + (CHECK ? 1 : 0); j++) {
     K best = key[0];
+#pragma unroll
     for (int i = 1; i < V; i++) best = key[i] > best ? key[i] : best;
-    K most = max_over(best, L);
+    K most = max_over(best, L); /* never 0: k experts are there */
+    int number;
     if constexpr (CHECK) {
-      if (j && most) sure = sure && value_of(last) - value_of(most) > 2 * OFF; /* NaN and infinities: not sure */
+      /* 32 units of the last place of a number, 4e-6 of it, each; NaN and infinities that follow one another: not sure */
+      if (j && most) sure = sure && value_of(last) - value_of(most) > 2 * OFF + 8e-6f * fabsf(value_of(last));
       last = most;
       if (j == k) break;
-    }
-    int won = first_of(best == most, L), at = 0; /* the maximum is never 0: k experts are there */
-    float value = a.x[0];
-    for (int i = V - 1; i > 0; i--)
-      if (key[i] == most) at = i, value = a.x[i];
-    if (key[0] == most) at = 0, value = a.x[0];
-    if (l == won)
-      for (int i = 0; i < V; i++)
-        if (i == at) key[i] = 0;
-    int from = (lane() & ~(L - 1)) + won, number = a.e0 + at;
-    if (L == 64) {
-      won = uniform(won);
-      value = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(value), won)), number = __builtin_amdgcn_readlane(number, won);
+      number = min_over(best == most ? a.e0 + V - 1 - (int)(most & 31) : 1 << 30, L);
+      if (number >= a.e0 && number < a.e0 + V)
+#pragma unroll
+        for (int i = 0; i < V; i++) key[i] = key[i] == most ? 0 : key[i];
     } else {
-      value = __shfl(value, from), number = __shfl(number, from);
+      int at = 1 << 30;
+#pragma unroll
+      for (int i = V - 1; i >= 0; i--) at = key[i] == most ? a.e0 + i : at;
+      number = min_over(at, L);
+      int in = number - a.e0;
+#pragma unroll
+      for (int i = 0; i < V; i++) key[i] = i == in ? 0 : key[i];
     }
-    if (l == j) mine = value, expert = number;
+    if (l == j) expert = number;
   }
   return sure;
 }
 
-template <int V, bool SCORES> __global__ __launch_bounds__(256) void k_route(Route r) {
+/* LANES: a token's, where they are known (the reductions then have no branches); 0: r.lanes. */
+template <int V, bool SCORES, int LANES> __global__ __launch_bounds__(256) void k_route(Route r) {
   const oob_route &p = r.p;
-  const int L = r.lanes, l = lane() & (L - 1);
+  const int L = LANES ? LANES : r.lanes, l = lane() & (L - 1);
   const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
   const bool live = t < p.T; /* runs of lanes as a whole: the others take part in the exchanges and write nothing */
   Token<V> a;
@@ -198,51 +201,67 @@ template <int V, bool SCORES> __global__ __launch_bounds__(256) void k_route(Rou
   a.group = l / r.in_group, a.e0 = a.group * r.per + in;
   a.there = a.group < p.groups ? r.per - in : 0;
   int64_t at = t * p.logits_stride + a.e0;
-  if (V == 4 && r.whole) {
-    bool here = live && a.there > 0;
-    if (p.dtype == OOB_FP32) {
-      f32x4 v = here ? *(const f32x4 *)((const float *)p.logits + at) : f32x4{0, 0, 0, 0};
-      for (int i = 0; i < V; i++) a.x[i] = here ? v[i] : -INFINITY;
-    } else {
-      uint64_t v = here ? *(const uint64_t *)((const uint16_t *)p.logits + at) : 0;
-      for (int i = 0; i < V; i++) {
-        uint16_t h = (uint16_t)(v >> (16 * i));
-        a.x[i] = !here ? -INFINITY : p.dtype == OOB_BF16 ? (float)__builtin_bit_cast(bf16, h) : (float)__builtin_bit_cast(fp16, h);
+  if (V % 4 == 0 && r.whole) {
+#pragma unroll
+    for (int q = 0; q < V; q += 4) {
+      bool here = live && q < a.there;
+      if (p.dtype == OOB_FP32) {
+        f32x4 v = here ? *(const f32x4 *)((const float *)p.logits + at + q) : f32x4{0, 0, 0, 0};
+        for (int i = 0; i < 4; i++) a.x[q + i] = here ? v[i] : -INFINITY;
+      } else {
+        uint64_t v = here ? *(const uint64_t *)((const uint16_t *)p.logits + at + q) : 0;
+        for (int i = 0; i < 4; i++) {
+          uint16_t h = (uint16_t)(v >> (16 * i));
+          a.x[q + i] = !here ? -INFINITY : p.dtype == OOB_BF16 ? (float)__builtin_bit_cast(bf16, h) : (float)__builtin_bit_cast(fp16, h);
+        }
       }
     }
   } else {
     for (int i = 0; i < V; i++) a.x[i] = live && i < a.there ? logit(p.logits, p.dtype, at + i) : -INFINITY;
   }
+  if constexpr (SCORES) { /* all loads before the first is waited for */
+    if (V % 4 == 0 && p.bias && r.whole_bias) {
+#pragma unroll
+      for (int q = 0; q < V; q += 4) {
+        f32x4 v = q < a.there ? *(const f32x4 *)(p.bias + a.e0 + q) : f32x4{0, 0, 0, 0};
+        for (int i = 0; i < 4; i++) a.bias[q + i] = v[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; i++) a.bias[i] = p.bias && i < a.there ? p.bias[a.e0 + i] : 0.f;
+    }
+  }
   float top = a.x[0];
   for (int i = 1; i < V; i++) top = fmaxf(top, a.x[i]);
   if (p.score == OOB_ROUTE_SOFTMAX) top = max_over(top, L);
 
-  float mine = -INFINITY, all = 0;
-  int expert = 0;
+  float all = 0;
+  int expert = 0; /* lane j's: choice j */
   if constexpr (SCORES) {
     uint32_t key[V];
     float best, next;
-    all = keys_of<float>(r, a, top, key, best, next);
+    all = keys_of<float>(r, a, L, top, key, best, next);
     bool sure = true;
     if (p.bias)
-      for (int i = 0; i < V; i++) sure = sure && (i >= a.there || fabsf(p.bias[a.e0 + i]) <= LARGE);
-    if (p.groups > 1) sure = groups(r, a, key, best, next) && sure;
-    sure = choose<true>(r, a, key, expert, mine) && sure;
+#pragma unroll
+      for (int i = 0; i < V; i++) sure &= fabsf(a.bias[i]) <= LARGE;
+    if (p.groups > 1) sure = groups(r, a, L, key, best, next) && sure;
+    sure = choose<true>(r, a, L, key, expert) && sure;
     if (__ballot(live && !sure)) {
       uint64_t wide[V];
       double b, n;
-      keys_of<double>(r, a, top, wide, b, n);
-      if (p.groups > 1) groups(r, a, wide, b, n);
-      choose<false>(r, a, wide, expert, mine);
+      keys_of<double>(r, a, L, top, wide, b, n);
+      if (p.groups > 1) groups(r, a, L, wide, b, n);
+      choose<false>(r, a, L, wide, expert);
     }
   } else {
     uint32_t key[V];
     for (int i = 0; i < V; i++) key[i] = i < a.there ? key_of(a.x[i]) : 0;
-    choose<false>(r, a, key, expert, mine);
+    choose<false>(r, a, L, key, expert);
   }
 
   const bool has = l < p.k;
-  float w;
+  float mine = live && has ? logit(p.logits, p.dtype, t * p.logits_stride + expert) : -INFINITY, w;
   if (p.renormalize) {
     float m = max_over(!has || mine != mine ? -INFINITY : p.score == OOB_ROUTE_SIGMOID ? fminf(mine, 0.f) : mine, L);
     float s = !has || mine == -INFINITY ? 0.f : p.score == OOB_ROUTE_SIGMOID ? sigmoid_over(mine, m) : expf(mine - m);
@@ -361,8 +380,14 @@ bool route_ok(const oob_route *p, bool forward) {
 
 template <int V> void route(const Route &r, hipStream_t st) {
   unsigned n = (unsigned)((r.p.T * r.lanes + 255) / 256);
-  if (r.p.bias || r.p.groups > 1) k_route<V, true><<<n, 256, 0, st>>>(r);
-  else k_route<V, false><<<n, 256, 0, st>>>(r);
+  bool scores = r.p.bias || r.p.groups > 1;
+  if (V == 8 && r.lanes == 32) {
+    if (scores) k_route<V, true, 32><<<n, 256, 0, st>>>(r);
+    else k_route<V, false, 32><<<n, 256, 0, st>>>(r);
+  } else {
+    if (scores) k_route<V, true, 0><<<n, 256, 0, st>>>(r);
+    else k_route<V, false, 0><<<n, 256, 0, st>>>(r);
+  }
 }
 
 /* ---- the chosen pairs in order of their experts ------------------------------------------------------------------------
@@ -527,15 +552,18 @@ using namespace layer;
 extern "C" int oob_expert_route(const oob_route *p, void *stream) {
   if (!route_ok(p, true)) return OOB_EINVAL;
   if (p->T == 0) return OOB_OK;
-  Route r{*p, 0, p->E / p->groups, 0, 0};
+  Route r{*p, 0, p->E / p->groups, 0, 0, 0};
   int groups = ceil2(p->groups), least = ceil2(p->k); /* lanes of a token: a power of two of them for each group */
-  int in_group = ceil2((r.per + 3) / 4);              /* four experts a lane where there are enough lanes */
+  /* eight experts a lane where the waves fill the GPU all the same, four otherwise (16 tokens: 2.6 us) */
+  int in_group = ceil2((r.per + 7) / 8);
+  if (p->T * groups * in_group < 64 * 2048) in_group = ceil2((r.per + 3) / 4);
   while (groups * in_group > 64) in_group /= 2;
   while (groups * in_group < least) in_group *= 2;
   r.lanes = groups * in_group, r.in_group = in_group;
   int v = (r.per + in_group - 1) / in_group;
   size_t four = p->dtype == OOB_FP32 ? 16 : 8;
   r.whole = r.per % 4 == 0 && multiple(p->logits, four) && p->logits_stride % 4 == 0;
+  r.whole_bias = r.per % 4 == 0 && multiple(p->bias, 16);
   hipStream_t st = (hipStream_t)stream;
   if (v <= 1) route<1>(r, st);
   else if (v <= 2) route<2>(r, st);
