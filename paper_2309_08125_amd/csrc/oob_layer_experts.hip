@@ -118,11 +118,21 @@ template <class E, int ROWS, int THREADS> struct Gathered {
   }
 };
 
-/* The sums of one tile over `steps` steps of k, the first two of which are on their way to LDS; load(buffer) asks for the next.  Two buffers, two arrays: the compiler then
- * knows that a read of one does not wait for the loads to the other.  A step's last products run behind the barrier that frees its buffer: while they
- * do, the first fragments of the next step are read and the loads of the one after are asked for.  At the end nobody reads the buffers any more. */
-template <class E, int TM, int TN, int WM, int WN, bool AK, bool BK, class TA, class TB, class L>
-__device__ __forceinline__ void multiply(L &load, int steps, lds_char *even, lds_char *odd, f32x16 (&acc)[TM / WM / 32][TN / WN / 32]) {
+/* Waits until no more than `most` of the wave's loads and none of its reads of LDS are on the way, then for the workgroup. */
+template <int most> __device__ inline void wait_but() {
+  static_assert(most < 64, "six bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (most & 15) | (most >> 4) << 14); /* vmcnt(most) lgkmcnt(0), expcnt as it is */
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+/* The sums of one tile over `steps` steps of k, the first BUFFERS of which are on their way to LDS; load(buffer) asks for the next.  Each buffer is an array of its own: the
+ * compiler then knows that a read of one does not wait for the loads to the others.  A step's last products run behind the barrier that frees its
+ * buffer: while they do, the first fragments of the next step are read and the loads of a later one are asked for.  At the end nobody reads the buffers any more.
+ * Small tiles have four buffers: their steps are shorter than the way from memory. */
+template <class E, int TM, int TN, int WM, int WN, bool AK, bool BK, int BUFFERS, class TA, class TB, class L>
+__device__ __forceinline__ void multiply(L &load, int steps, lds_char *const (&buffers)[BUFFERS], f32x16 (&acc)[TM / WM / 32][TN / WN / 32]) {
   constexpr int FM = TM / WM / 32, FN = TN / WN / 32, READS = FM * (AK ? 1 : 2) + FN * (BK ? 1 : 2), LOADS = TA::LOADS + TB::LOADS;
   int wave = uniform(threadIdx.x / 64), wm = wave / WN, wn = wave % WN;
   Fragment<E, TM, FM, AK> fa;
@@ -168,7 +178,7 @@ __device__ __forceinline__ void multiply(L &load, int steps, lds_char *even, lds
     order();
   };
   auto back = [&](lds_char *now, lds_char *next) __attribute__((always_inline)) { /* product 3, read 0 of the next step */
-    wait_barrier(); /* the next step's loads have landed, and nobody reads this buffer any more */
+    wait_but<(BUFFERS - 2) * LOADS>(); /* the next step's loads have landed, and nobody reads this buffer any more */
     fetch(next, 0, a0, b0);
     load(now);
     products(a1, b1);
@@ -180,19 +190,23 @@ __device__ __forceinline__ void multiply(L &load, int steps, lds_char *even, lds
     }
   };
   wait_barrier();
-  fetch(even, 0, a0, b0);
-  front(even);
-  /* the loop begins where all loads are waited for: the compiler does so at its head whatever is on the way */
-  for (int t = 2; t < steps; t += 2) {
-    back(even, odd);
-    front(odd);
-    back(odd, even);
-    front(even);
+  fetch(buffers[0], 0, a0, b0);
+  front(buffers[0]);
+  /* the loop begins where loads are waited for: the compiler waits for all of them at its head whatever is on the way */
+  int left = steps - 1;
+  for (; left >= BUFFERS; left -= BUFFERS) {
+#pragma unroll
+    for (int i = 0; i < BUFFERS; i++) {
+      back(buffers[i], buffers[(i + 1) % BUFFERS]);
+      front(buffers[(i + 1) % BUFFERS]);
+    }
   }
-  if (steps % 2 == 0) {
-    back(even, odd);
-    front(odd);
-  }
+#pragma unroll
+  for (int i = 0; i < BUFFERS - 1; i++)
+    if (left > i) {
+      back(buffers[i], buffers[i + 1]);
+      front(buffers[i + 1]);
+    }
   products(a1, b1);
   wait_barrier(); /* the loads past the last step have landed: the next tile's may be asked for */
 }
@@ -255,8 +269,10 @@ template <class E, int TM, int TN, int WM, int WN, bool BK, bool GATHER, bool DW
   constexpr bool AK = !DW;
   using TA = std::conditional_t<GATHER, Gathered<E, TM, THREADS>, Strip<E, TM, THREADS, AK>>;
   using TB = Strip<E, TN, THREADS, BK>;
-  __shared__ __attribute__((aligned(1024))) char even_[TA::BYTES + TB::BYTES], odd_[TA::BYTES + TB::BYTES];
-  lds_char *even = (lds_char *)even_, *odd = (lds_char *)odd_;
+  constexpr int BUFFERS = TM == 64 ? 4 : 2, SIZE = TA::BYTES + TB::BYTES;
+  __shared__ __attribute__((aligned(1024))) char first_[SIZE], second_[SIZE], third_[BUFFERS > 2 ? SIZE : 1024], fourth_[BUFFERS > 2 ? SIZE : 1024];
+  lds_char *const all[4] = {(lds_char *)first_, (lds_char *)second_, (lds_char *)third_, (lds_char *)fourth_};
+  lds_char *const(&buffers)[BUFFERS] = reinterpret_cast<lds_char *const(&)[BUFFERS]>(all);
   const Product &g = x.g;
   const int64_t da = AK ? KSTEP * 2 : KSTEP * 2 * g.lda, db = BK ? KSTEP * 2 : KSTEP * 2 * g.ldb;
 
@@ -315,8 +331,8 @@ template <class E, int TM, int TN, int WM, int WN, bool BK, bool GATHER, bool DW
     else ta.init(g.lda, w.left);
     tb.init(g.ldb, g.N - w.n0);
     pa = w.pa, pb = w.pb, kleft = w.k;
-    load(even);
-    load(odd);
+#pragma unroll
+    for (int i = 0; i < BUFFERS; i++) load(buffers[i]);
   };
   Where w = next_of(id);
   if (w.expert < 0) return;
@@ -324,7 +340,7 @@ template <class E, int TM, int TN, int WM, int WN, bool BK, bool GATHER, bool DW
   for (;;) {
     Where then = next_of(id);
     f32x16 acc[TM / WM / 32][TN / WN / 32];
-    multiply<E, TM, TN, WM, WN, AK, BK, TA, TB>(load, (w.k + KSTEP - 1) / KSTEP, even, odd, acc);
+    multiply<E, TM, TN, WM, WN, AK, BK, BUFFERS, TA, TB>(load, (w.k + KSTEP - 1) / KSTEP, buffers, acc);
     if (then.expert >= 0) begin(then);
     const E *bias = g.bias ? (const E *)g.bias + (int64_t)w.expert * g.N : nullptr;
     switch (g.act) {
@@ -485,7 +501,7 @@ int choose_dw(int64_t M, int64_t N, int E) {
 template <class E, int TILE, int WN, bool BK, bool GATHER, bool DW> void launch(Experts x, hipStream_t st) {
   x.g.tiles_m = (int)tiles(x.g.M, TILE), x.g.tiles_n = (int)tiles(x.g.N, TILE);
   x.ids = (int)(DW ? x.d.E * up((int64_t)x.g.tiles_m * x.g.tiles_n, 8) : row_tiles(x.d.R, x.d.E, TILE) * x.g.tiles_n);
-  int most = TILE == 256 ? 256 : TILE == 128 ? 512 : 1024; /* that run at once: one, two, four a compute unit */
+  int most = TILE == 256 ? 256 : 512; /* that run at once: one, two a compute unit */
   k_experts<E, TILE, TILE, 2, WN, BK, GATHER, DW><<<x.ids < most ? x.ids : most, 128 * WN, 0, st>>>(x);
 }
 template <class E, bool BK, bool GATHER, bool DW> int products(Experts x, hipStream_t st) {
