@@ -259,12 +259,50 @@ __device__ __forceinline__ void finish(const Product &g, f32x16 (&acc)[TM / WM /
   }
 }
 
+/* The same eight columns of a row, as sums that are not complete: TM x TN floats. */
+template <int TM, int TN, int WM, int WN>
+__device__ __forceinline__ void leave(f32x16 (&acc)[TM / WM / 32][TN / WN / 32], float *to, int left) {
+  constexpr int FM = TM / WM / 32, FN = TN / WN / 32;
+  int wave = uniform(threadIdx.x / 64), wm = wave / WN, wn = wave % WN, l = lane();
+#pragma unroll
+  for (int i = 0; i < FM; i++) {
+    int m = (wm * FM + i) * 32 + (l & 31);
+#pragma unroll
+    for (int j = 0; j < FN; j++)
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        f32x4 lo, hi;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][8 * h + e]), __float_as_uint(acc[i][j][8 * h + 4 + e]), false, false);
+          lo[e] = __uint_as_float(two[0]), hi[e] = __uint_as_float(two[1]);
+        }
+        if (m >= left) continue;
+        f32x4 *at = (f32x4 *)(to + (int64_t)m * TN + wn * FN * 32 + j * 32 + h * 16 + l / 32 * 8);
+        at[0] = lo, at[1] = hi;
+      }
+  }
+}
+
 /* Where a workgroup's tile lies; expert -1: nowhere. */
-struct Where { int expert, left, k; int64_t row, n0; const char *pa, *pb; }; /* rows of C from `row` on; k: depth */
+struct Where { int expert, left, k, part; int64_t row, n0; const char *pa, *pb; }; /* rows of C from `row` on; k: depth; part: where its sums are left */
 
 /* Rows of y (BK: W as it is), of dx (W by its columns) or, DW, the matrices dw[e] = dz^T x over the rows of e.  A workgroup takes one tile after the other, every
- * gridDim-th: the first loads of the next are asked for before the present one's epilogue. */
-template <class E, int TM, int TN, int WM, int WN, bool BK, bool GATHER, bool DW> __global__ __launch_bounds__(WM *WN * 64, 2) void k_experts(Experts x) {
+ * gridDim-th: the first loads of the next are asked for before the present one's epilogue.
+ * Large tiles that are left over from whole rounds of the GPU, where they would keep few compute units busy for a round, are left to a second launch (REST), in which k
+ * is divided among several workgroups that leave their sums, and a third that joins them.  8192 rows, 8 experts, 4096 x 8192, dx: 576 tiles,
+ * 508 us; 597 without (the quarters of the 64 tiles left over, done as tiles of 128: 566). */
+constexpr int UNITS = 256;
+struct Rest { int whole, tiles, splits; }; /* of all large tiles the first `whole` are done one a workgroup */
+__device__ inline Rest rest_of(int total, int steps) {
+  int rest = total > UNITS ? total % UNITS : 0, splits = rest ? UNITS / rest : 1;
+  if (splits > 8) splits = 8;
+  if (splits > steps / 16) splits = steps / 16; /* a part of 16 steps takes as long as its sums' way to memory and back */
+  return splits < 2 ? Rest{total, 0, 1} : Rest{total - rest, rest, splits};
+}
+
+template <class E, int TM, int TN, int WM, int WN, bool BK, bool GATHER, bool DW, bool REST>
+__global__ __launch_bounds__(WM *WN * 64, 2) void k_experts(Experts x) {
   constexpr int THREADS = WM * WN * 64;
   constexpr bool AK = !DW;
   using TA = std::conditional_t<GATHER, Gathered<E, TM, THREADS>, Strip<E, TM, THREADS, AK>>;
@@ -295,14 +333,25 @@ template <class E, int TM, int TN, int WM, int WN, bool BK, bool GATHER, bool DW
       w.pa = (const char *)g.A + (first * g.lda + m0) * 2, w.pb = (const char *)g.B + (first * g.ldb + w.n0) * 2;
     } else {
       int64_t tn = g.tiles_n;
-      Found f = find(x.d, [&](int64_t r) { return (r + TM - 1) / TM * tn; }, [&](int total) { return id < total ? (int)xcd_order(id, total) : total; });
+      int steps = (int)((g.K + KSTEP - 1) / KSTEP), first = 0, last = steps;
+      Found f = find(x.d, [&](int64_t r) { return (r + TM - 1) / TM * tn; }, [&](int total) {
+        Rest r = TM == 256 ? rest_of(total, steps) : Rest{total, 0, 1};
+        if (!REST) return id < r.whole ? (int)xcd_order(id, r.whole) : total;
+        if (id >= r.tiles * r.splits) return total;
+        w.part = (int)xcd_order(id, r.tiles * r.splits);
+        int split = w.part / r.tiles;
+        first = steps * split / r.splits, last = steps * (split + 1) / r.splits;
+        return r.whole + w.part % r.tiles;
+      });
       w.expert = f.expert;
       if (w.expert < 0) return w;
       band(f.part, (int)(((int64_t)f.rows + TM - 1) / TM), (int)tn, m, n);
       int64_t m0 = (int64_t)m * TM;
-      w.n0 = (int64_t)n * TN, w.left = f.rows - m0 < TM ? (int)(f.rows - m0) : TM, w.row = f.first + m0, w.k = (int)g.K;
-      w.pa = (const char *)g.A + (GATHER ? 0 : w.row * g.lda * 2);
-      w.pb = (const char *)g.B + (f.expert * x.expert_stride + (BK ? w.n0 * g.ldb : w.n0)) * 2;
+      w.n0 = (int64_t)n * TN;
+      w.left = f.rows - m0 < TM ? (int)(f.rows - m0) : TM, w.row = f.first + m0;
+      w.k = (last == steps ? (int)g.K : last * KSTEP) - first * KSTEP;
+      w.pa = (const char *)g.A + (GATHER ? 0 : w.row * g.lda * 2) + first * da;
+      w.pb = (const char *)g.B + (f.expert * x.expert_stride + (BK ? w.n0 * g.ldb : w.n0)) * 2 + first * db;
     }
     return w;
   };
@@ -343,7 +392,8 @@ template <class E, int TM, int TN, int WM, int WN, bool BK, bool GATHER, bool DW
     multiply<E, TM, TN, WM, WN, AK, BK, BUFFERS, TA, TB>(load, (w.k + KSTEP - 1) / KSTEP, buffers, acc);
     if (then.expert >= 0) begin(then);
     const E *bias = g.bias ? (const E *)g.bias + (int64_t)w.expert * g.N : nullptr;
-    switch (g.act) {
+    if constexpr (REST) leave<TM, TN, WM, WN>(acc, g.partial + (int64_t)w.part * TM * TN, w.left);
+    else switch (g.act) {
       case OOB_ACT_RELU: finish<E, OOB_ACT_RELU, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0); break;
       case OOB_ACT_SILU: finish<E, OOB_ACT_SILU, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0); break;
       case OOB_ACT_GELU: finish<E, OOB_ACT_GELU, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0); break;
@@ -353,6 +403,33 @@ template <class E, int TM, int TN, int WM, int WN, bool BK, bool GATHER, bool DW
     if (then.expert < 0) return;
     w = then;
   }
+}
+
+/* Joins what REST left: 32 workgroups a tile, eight values a thread. */
+template <class E> __global__ __launch_bounds__(256) void k_experts_join(Experts x) {
+  constexpr int TILE = 256;
+  const Product &g = x.g;
+  int64_t tn = g.tiles_n;
+  int tile = blockIdx.x / 32, at = (int)(blockIdx.x % 32 * 256 + threadIdx.x) * 8, steps = (int)((g.K + KSTEP - 1) / KSTEP);
+  Rest r{};
+  Found f = find(x.d, [&](int64_t n) { return (n + TILE - 1) / TILE * tn; }, [&](int total) {
+    r = rest_of(total, steps);
+    return tile < r.tiles ? r.whole + tile : total;
+  });
+  if (f.expert < 0) return;
+  int tm = (int)(((int64_t)f.rows + TILE - 1) / TILE), in = f.part % (8 * (int)tn), band = f.part / (8 * (int)tn) * 8, high = tm - band < 8 ? tm - band : 8;
+  int64_t m = (int64_t)(band + in % high) * TILE + at / TILE, n = (int64_t)(in / high) * TILE + at % TILE;
+  if (m >= f.rows || n >= g.N) return;
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int s = 0; s < r.splits; s++) {
+    const f32x4 *p = (const f32x4 *)(g.partial + ((int64_t)s * r.tiles + tile) * TILE * TILE + at);
+    f32x4 lo = p[0], hi = p[1];
+    for (int e = 0; e < 4; e++) v[e] += lo[e], v[4 + e] += hi[e];
+  }
+  Product one = g;
+  if (g.bias) one.bias = (const E *)g.bias + (int64_t)f.expert * g.N;
+  if (g.act == OOB_ACT_NONE) one.Z = nullptr;
+  epilogue<E>(one, f.first + m, n, v);
 }
 
 /* ---- rows of another pitch or order in the workspace: what the tiles' loads cannot take as it lies ------------------------------
@@ -498,11 +575,22 @@ int choose_dw(int64_t M, int64_t N, int E) {
   return 64;
 }
 
+/* Sums of tiles whose k is divided: room for as many parts as compute units where any division of the rows has more large tiles than these. */
+size_t rest_bytes(int64_t R, int E, int64_t N, int64_t K) {
+  return choose_tile(R, E, N) == 256 && row_tiles(R, E, 256) * tiles(N, 256) > UNITS && tiles(K, KSTEP) >= 32 ? (size_t)UNITS * 256 * 256 * 4 : 0;
+}
+
 template <class E, int TILE, int WN, bool BK, bool GATHER, bool DW> void launch(Experts x, hipStream_t st) {
   x.g.tiles_m = (int)tiles(x.g.M, TILE), x.g.tiles_n = (int)tiles(x.g.N, TILE);
   x.ids = (int)(DW ? x.d.E * up((int64_t)x.g.tiles_m * x.g.tiles_n, 8) : row_tiles(x.d.R, x.d.E, TILE) * x.g.tiles_n);
   int most = TILE == 256 ? 256 : 512; /* that run at once: one, two a compute unit */
-  k_experts<E, TILE, TILE, 2, WN, BK, GATHER, DW><<<x.ids < most ? x.ids : most, 128 * WN, 0, st>>>(x);
+  k_experts<E, TILE, TILE, 2, WN, BK, GATHER, DW, false><<<x.ids < most ? x.ids : most, 128 * WN, 0, st>>>(x);
+  if constexpr (TILE == 256 && !DW)
+    if (x.g.partial) {
+      x.ids = UNITS;
+      k_experts<E, TILE, TILE, 2, WN, BK, GATHER, false, true><<<UNITS, 128 * WN, 0, st>>>(x);
+      k_experts_join<E><<<UNITS / 2 * 32, 256, 0, st>>>(x);
+    }
 }
 template <class E, bool BK, bool GATHER, bool DW> int products(Experts x, hipStream_t st) {
   int tile = DW ? choose_dw(x.g.M, x.g.N, x.d.E) : choose_tile(x.d.R, x.d.E, x.g.N);
@@ -530,6 +618,7 @@ size_t forward_bytes(const oob_expert_linear_t *p) {
   Arena w{nullptr, 0, 0};
   pack_w(p, w, nullptr);
   if (!x_loadable(p)) pack_x(p, w, nullptr);
+  w.take(rest_bytes(p->R, p->E, p->N, p->K));
   return w.used;
 }
 
@@ -538,6 +627,8 @@ template <class E> int forward(const oob_expert_linear_t *p, Arena w, hipStream_
   Operand b = pack_w(p, w, st), a{p->x, p->x_stride, 0};
   bool gather = p->rows && x_loadable(p);
   if (!x_loadable(p)) a = pack_x(p, w, st);
+  size_t rest = rest_bytes(p->R, p->E, p->N, p->K);
+  x.g.partial = rest ? (float *)w.take(rest) : nullptr;
   if (!w.ok()) return OOB_ECAPACITY;
   x.g.A = a.p, x.g.lda = a.ld, x.g.B = b.p, x.g.ldb = b.ld, x.expert_stride = b.part;
   x.g.N = p->N, x.g.K = p->K, x.g.bias = p->bias, x.g.C = p->y, x.g.ldc = p->y_stride, x.g.Z = p->z, x.g.ldz = p->z_stride, x.g.act = p->act;
@@ -559,7 +650,7 @@ size_t backward_bytes(const oob_expert_linear_t *p, const oob_expert_linear_grad
   Arena w{nullptr, 0, 0}, dx{nullptr, 0, 0}, dw{nullptr, 0, 0};
   if (makes_dz(p, g)) w.take((size_t)p->R * up(p->N, 8) * 2);
   if (g->db) w.take(sums_bytes(p));
-  if (g->dx) pack_w(p, dx, nullptr);
+  if (g->dx) pack_w(p, dx, nullptr), dx.take(rest_bytes(p->R, p->E, p->K, p->N));
   if (g->dw) pack_x(p, dw, nullptr);
   return w.used + (dx.used > dw.used ? dx.used : dw.used);
 }
@@ -589,8 +680,10 @@ template <class E> int backward(const oob_expert_linear_t *p, const oob_expert_l
   if (rc == OOB_OK && g->dx && p->R) {
     Arena more = w; /* what one product takes is free again for the next on the stream */
     Operand b = pack_w(p, more, st);
-    if (!more.ok()) return OOB_ECAPACITY;
+    size_t rest = rest_bytes(p->R, p->E, p->K, p->N);
     Experts x{};
+    x.g.partial = rest ? (float *)more.take(rest) : nullptr;
+    if (!more.ok()) return OOB_ECAPACITY;
     x.g.A = dz.p, x.g.lda = dz.ld, x.g.B = b.p, x.g.ldb = b.ld, x.expert_stride = b.part;
     x.g.N = p->K, x.g.K = p->N, x.g.C = g->dx, x.g.ldc = g->dx_stride, x.d = d;
     rc = products<E, false, false, false>(x, st);

@@ -297,6 +297,14 @@ def test_linear_large_tiles(P, T, k, E, N, K):
     linear_case(P, T, k, E, K, N, "none", torch.bfloat16, gather=False)
 
 
+@pytest.mark.parametrize("skew", [0.0, 0.3, 1.0])
+def test_linear_tiles_left_over(P, skew):
+    """More large tiles than compute units: those of the last round have their depth divided among workgroups."""
+    linear_case(P, 1024, 2, 4, 8184, 2056, "silu", torch.bfloat16, skew=skew, need=("w",))
+    linear_case(P, 1024, 2, 4, 8184, 2056, "none", torch.float16, gather=False, bias=False, skew=skew, need=("b",))
+    linear_case(P, 1024, 2, 4, 2056, 8184, "relu", torch.bfloat16, skew=skew, need=("x",))
+
+
 def test_linear_shares_and_skewed_divisions(P):
     linear_case(P, 120, 3, 4, 72, 64, "silu", torch.bfloat16, of=16)            # most rows are elsewhere
     linear_case(P, 120, 3, 4, 72, 64, "silu", torch.bfloat16, of=16, gather=False)
