@@ -127,7 +127,7 @@ template <int most> __device__ inline void wait_but() {
   asm volatile("" ::: "memory");
 }
 
-/* The sums of one tile over `steps` steps of k, the first BUFFERS of which are on their way to LDS; load(buffer) asks for the next.  Each buffer is an array of its own: the
+/* The sums of one tile over `steps` steps of k, the first BUFFERS of which lie in LDS; load(buffer) asks for the next.  Each buffer is an array of its own: the
  * compiler then knows that a read of one does not wait for the loads to the others.  A step's last products run behind the barrier that frees its
  * buffer: while they do, the first fragments of the next step are read and the loads of a later one are asked for.  At the end nobody reads the buffers any more.
  * Small tiles have four buffers: their steps are shorter than the way from memory. */
@@ -189,7 +189,6 @@ __device__ __forceinline__ void multiply(L &load, int steps, lds_char *const (&b
       __builtin_amdgcn_sched_group_barrier(0x10, (LOADS + FM * FN - 1) / (FM * FN), 0);
     }
   };
-  wait_barrier();
   fetch(buffers[0], 0, a0, b0);
   front(buffers[0]);
   /* the loop begins where loads are waited for: the compiler waits for all of them at its head whatever is on the way */
@@ -213,8 +212,9 @@ __device__ __forceinline__ void multiply(L &load, int steps, lds_char *const (&b
 
 /* A tile's sums through the epilogue, from the registers that the products leave them in: a lane has a row and, of 16 neighbouring columns, two times four.
  * An exchange between the halves of the wave makes them eight in a row, 16 bytes of C a store.  Nothing goes through LDS, so that the next tile's
- * first loads are on their way meanwhile. */
-template <class E, int ACT, int TM, int TN, int WM, int WN>
+ * first loads are on their way meanwhile.  FULL: all rows and columns are there, so that every wave makes STORES stores at least, which the wait behind counts on. */
+template <int TM, int TN, int WM, int WN> constexpr int STORES = TM / WM / 32 * (TN / WN / 32) * 2;
+template <class E, int ACT, bool FULL, int TM, int TN, int WM, int WN>
 __device__ __forceinline__ void finish(const Product &g, f32x16 (&acc)[TM / WM / 32][TN / WN / 32], const E *bias, E *C, int64_t row, int left, int64_t n0) {
   constexpr int FM = TM / WM / 32, FN = TN / WN / 32;
   int wave = uniform(threadIdx.x / 64), wm = wave / WN, wn = wave % WN, l = lane();
@@ -226,7 +226,7 @@ __device__ __forceinline__ void finish(const Product &g, f32x16 (&acc)[TM / WM /
 #pragma unroll
       for (int h = 0; h < 2; h++) {
         int64_t n = n1 + j * 32 + h * 16;
-        if (n < g.N) add[j][h] = load8<E>(bias + n, g.N - n);
+        if (FULL || n < g.N) add[j][h] = load8<E>(bias + n, FULL ? 8 : g.N - n);
       }
 #pragma unroll
   for (int i = 0; i < FM; i++) {
@@ -242,7 +242,7 @@ __device__ __forceinline__ void finish(const Product &g, f32x16 (&acc)[TM / WM /
           v[e] = __uint_as_float(two[0]), v[4 + e] = __uint_as_float(two[1]);
         }
         int64_t n = n1 + j * 32 + h * 16, at = row + m;
-        if (m >= left || n >= g.N) continue;
+        if (!FULL && (m >= left || n >= g.N)) continue;
         typename Vec<E>::v8 out;
         if (bias)
 #pragma unroll
@@ -250,11 +250,11 @@ __device__ __forceinline__ void finish(const Product &g, f32x16 (&acc)[TM / WM /
         if (ACT != OOB_ACT_NONE && g.Z) { /* rounded to the type, as y is: half the memory between the passes; act' sees the rounding, act does not */
 #pragma unroll
           for (int e = 0; e < 8; e++) out[e] = (E)v[e];
-          store8<E>((E *)g.Z + at * g.ldz + n, out, g.N - n);
+          store8<E>((E *)g.Z + at * g.ldz + n, out, FULL ? 8 : g.N - n);
         }
 #pragma unroll
         for (int e = 0; e < 8; e++) out[e] = (E)activate(v[e], ACT);
-        store8<E>(C + at * g.ldc + n, out, g.N - n);
+        store8<E>(C + at * g.ldc + n, out, FULL ? 8 : g.N - n);
       }
   }
 }
@@ -386,19 +386,36 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_experts(Experts x) {
   Where w = next_of(id);
   if (w.expert < 0) return;
   begin(w);
+  wait_barrier();
   for (;;) {
     Where then = next_of(id);
     f32x16 acc[TM / WM / 32][TN / WN / 32];
     multiply<E, TM, TN, WM, WN, AK, BK, BUFFERS, TA, TB>(load, (w.k + KSTEP - 1) / KSTEP, buffers, acc);
     if (then.expert >= 0) begin(then);
     const E *bias = g.bias ? (const E *)g.bias + (int64_t)w.expert * g.N : nullptr;
-    if constexpr (REST) leave<TM, TN, WM, WN>(acc, g.partial + (int64_t)w.part * TM * TN, w.left);
-    else switch (g.act) {
-      case OOB_ACT_RELU: finish<E, OOB_ACT_RELU, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0); break;
-      case OOB_ACT_SILU: finish<E, OOB_ACT_SILU, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0); break;
-      case OOB_ACT_GELU: finish<E, OOB_ACT_GELU, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0); break;
-      case OOB_ACT_GELU_TANH: finish<E, OOB_ACT_GELU_TANH, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0); break;
-      default: finish<E, OOB_ACT_NONE, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0);
+    if constexpr (REST) {
+      leave<TM, TN, WM, WN>(acc, g.partial + (int64_t)w.part * TM * TN, w.left);
+      wait_barrier();
+    } else if (w.left == TM && w.n0 + TN <= g.N) {
+#define OOB_FINISH(ACT, FULL) finish<E, ACT, FULL, TM, TN, WM, WN>(g, acc, bias, (E *)g.C, w.row, w.left, w.n0)
+      switch (g.act) {
+        case OOB_ACT_RELU: OOB_FINISH(OOB_ACT_RELU, true); break;
+        case OOB_ACT_SILU: OOB_FINISH(OOB_ACT_SILU, true); break;
+        case OOB_ACT_GELU: OOB_FINISH(OOB_ACT_GELU, true); break;
+        case OOB_ACT_GELU_TANH: OOB_FINISH(OOB_ACT_GELU_TANH, true); break;
+        default: OOB_FINISH(OOB_ACT_NONE, true);
+      }
+      wait_but<STORES<TM, TN, WM, WN>>(); /* the next tile's loads, which are older than the stores, have landed; the stores have not */
+    } else {
+      switch (g.act) {
+        case OOB_ACT_RELU: OOB_FINISH(OOB_ACT_RELU, false); break;
+        case OOB_ACT_SILU: OOB_FINISH(OOB_ACT_SILU, false); break;
+        case OOB_ACT_GELU: OOB_FINISH(OOB_ACT_GELU, false); break;
+        case OOB_ACT_GELU_TANH: OOB_FINISH(OOB_ACT_GELU_TANH, false); break;
+        default: OOB_FINISH(OOB_ACT_NONE, false);
+      }
+      wait_barrier();
+#undef OOB_FINISH
     }
     if (then.expert < 0) return;
     w = then;
@@ -565,7 +582,7 @@ int64_t row_tiles(int64_t R, int E, int tile) { return R / tile + (R < E ? R : E
 /* By the rows that an expert has on average. */
 int choose_tile(int64_t R, int E, int64_t N) {
   int64_t mean = R / E;
-  if (mean >= 192 && tiles(R, 256) * tiles(N, 256) >= 192) return 256;
+  if (mean >= 192 && tiles(R, 256) * tiles(N, 256) >= 112) return 256; /* 4096 x 2048 x 2048, 8 experts: 49 us, the middle one 56; of 64 tiles 77 and 55 */
   if (mean >= 96 && tiles(R, 128) * tiles(N, 128) >= 192) return 128;
   return 64;
 }
