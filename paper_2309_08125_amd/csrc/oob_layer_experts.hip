@@ -459,8 +459,13 @@ struct Packed {
   int per, E;
 };
 
-__global__ __launch_bounds__(256) void k_pack_rows(Packed p) {
-  int64_t per = p.ld_to / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x, r = id / per, c = id % per * 8;
+/* Two matrices in one launch, w and x: the first takes workgroups below `first`. */
+struct Packs { Packed p[2]; int64_t first; };
+
+__global__ __launch_bounds__(256) void k_pack_rows(Packs packs) {
+  const bool second = (int64_t)blockIdx.x >= packs.first;
+  const Packed &p = packs.p[second];
+  int64_t per = p.ld_to / 8, id = ((int64_t)blockIdx.x - (second ? packs.first : 0)) * 256 + threadIdx.x, r = id / per, c = id % per * 8;
   if (p.offsets) {
     int end = 0;
     for (int e = lane(); e <= p.E; e += 64) end = max(end, p.offsets[e]);
@@ -553,24 +558,27 @@ bool x_loadable(const oob_expert_linear_t *p) {
   return loadable(p->x, p->x_stride, p->K) && (!p->rows || p->T * p->x_stride < (int64_t)1 << 30);
 }
 
-void pack(const Packed &k, hipStream_t st) {
-  int64_t n = k.n * (k.ld_to / 8);
-  if (n) k_pack_rows<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(k);
+int64_t groups_of(const Packed &k) { return (k.n * (k.ld_to / 8) + 255) / 256; }
+void pack(const Packed &a, const Packed &b, hipStream_t st) {
+  int64_t first = groups_of(a), n = first + groups_of(b);
+  if (n) k_pack_rows<<<(unsigned)n, 256, 0, st>>>(Packs{{a, b}, first});
 }
-Operand pack_w(const oob_expert_linear_t *p, Arena &w, hipStream_t st) {
+/* As the products take them, in the workspace where they have to be copied: `how` says so then (n is 0 otherwise). */
+Operand plan_w(const oob_expert_linear_t *p, Arena &w, Packed &how) {
+  how = Packed{};
   if (w_loadable(p)) return {p->w, p->w_stride, p->expert_stride};
   int64_t ld = up(p->K, 8);
   void *to = w.take((size_t)p->E * p->N * ld * 2);
-  if (w.ok() && w.base) pack({(const uint16_t *)p->w, (uint16_t *)to, p->E * p->N, p->N, p->expert_stride, p->K, p->w_stride, ld, 0, nullptr, nullptr, 1, 0}, st);
+  how = {(const uint16_t *)p->w, (uint16_t *)to, p->E * p->N, p->N, p->expert_stride, p->K, p->w_stride, ld, 0, nullptr, nullptr, 1, 0};
   return {to, ld, p->N * ld};
 }
 /* Rows of x in order of their experts. */
-Operand pack_x(const oob_expert_linear_t *p, Arena &w, hipStream_t st) {
+Operand plan_x(const oob_expert_linear_t *p, Arena &w, Packed &how) {
+  how = Packed{};
   if (!p->rows && loadable(p->x, p->x_stride, p->K)) return {p->x, p->x_stride, 0};
   int64_t ld = up(p->K, 8);
   void *to = w.take((size_t)p->R * ld * 2);
-  if (w.ok() && w.base)
-    pack({(const uint16_t *)p->x, (uint16_t *)to, p->R, p->R, 0, p->K, p->x_stride, ld, p->T, p->rows, p->offsets, p->per, p->E}, st);
+  how = {(const uint16_t *)p->x, (uint16_t *)to, p->R, p->R, 0, p->K, p->x_stride, ld, p->T, p->rows, p->offsets, p->per, p->E};
   return {to, ld, 0};
 }
 
@@ -631,29 +639,28 @@ bool launches_fit(const oob_expert_linear_t *p) {
          fits((p->R + p->E * p->N) * ((up(p->K, 8)) / 8) / 256 + 1);
 }
 
-size_t forward_bytes(const oob_expert_linear_t *p) {
-  Arena w{nullptr, 0, 0};
-  pack_w(p, w, nullptr);
-  if (!x_loadable(p)) pack_x(p, w, nullptr);
-  w.take(rest_bytes(p->R, p->E, p->N, p->K));
-  return w.used;
+struct Forward { Operand a, b; Packed x, w; float *rest; };
+Forward plan(const oob_expert_linear_t *p, Arena &w) {
+  Forward f{{p->x, p->x_stride, 0}, {}, {}, {}, nullptr};
+  f.b = plan_w(p, w, f.w);
+  if (!x_loadable(p)) f.a = plan_x(p, w, f.x);
+  size_t rest = rest_bytes(p->R, p->E, p->N, p->K);
+  if (rest) f.rest = (float *)w.take(rest);
+  return f;
 }
 
 template <class E> int forward(const oob_expert_linear_t *p, Arena w, hipStream_t st) {
-  Experts x{};
-  Operand b = pack_w(p, w, st), a{p->x, p->x_stride, 0};
-  bool gather = p->rows && x_loadable(p);
-  if (!x_loadable(p)) a = pack_x(p, w, st);
-  size_t rest = rest_bytes(p->R, p->E, p->N, p->K);
-  x.g.partial = rest ? (float *)w.take(rest) : nullptr;
+  Forward f = plan(p, w);
   if (!w.ok()) return OOB_ECAPACITY;
-  x.g.A = a.p, x.g.lda = a.ld, x.g.B = b.p, x.g.ldb = b.ld, x.expert_stride = b.part;
+  pack(f.w, f.x, st);
+  Experts x{};
+  x.g.A = f.a.p, x.g.lda = f.a.ld, x.g.B = f.b.p, x.g.ldb = f.b.ld, x.expert_stride = f.b.part, x.g.partial = f.rest;
   x.g.N = p->N, x.g.K = p->K, x.g.bias = p->bias, x.g.C = p->y, x.g.ldc = p->y_stride, x.g.Z = p->z, x.g.ldz = p->z_stride, x.g.act = p->act;
   x.d = {p->offsets, p->E, p->R}, x.rows = p->rows, x.per = p->per, x.T = p->T;
-  return gather ? products<E, true, true, false>(x, st) : products<E, true, false, false>(x, st);
+  return p->rows && x_loadable(p) ? products<E, true, true, false>(x, st) : products<E, true, false, false>(x, st);
 }
 
-/* dz, the runs' sums, then what the larger product takes */
+/* dz, the runs' sums, copies of w and x, sums of tiles whose depth is divided */
 bool makes_dz(const oob_expert_linear_t *p, const oob_expert_linear_grad *g) {
   return (g->dx || g->dw) && (p->act != OOB_ACT_NONE || !loadable(g->dy, g->dy_stride, p->N));
 }
@@ -663,21 +670,27 @@ int run_rows(const oob_expert_linear_t *p) { /* about 1024 workgroups, 16 rows a
 }
 size_t sums_bytes(const oob_expert_linear_t *p) { return (size_t)row_tiles(p->R, p->E, run_rows(p)) * p->N * 4; }
 
-size_t backward_bytes(const oob_expert_linear_t *p, const oob_expert_linear_grad *g) {
-  Arena w{nullptr, 0, 0}, dx{nullptr, 0, 0}, dw{nullptr, 0, 0};
-  if (makes_dz(p, g)) w.take((size_t)p->R * up(p->N, 8) * 2);
-  if (g->db) w.take(sums_bytes(p));
-  if (g->dx) pack_w(p, dx, nullptr), dx.take(rest_bytes(p->R, p->E, p->K, p->N));
-  if (g->dw) pack_x(p, dw, nullptr);
-  return w.used + (dx.used > dw.used ? dx.used : dw.used);
+struct Backward { Operand dz, w, x; Packed how_w, how_x; float *sums, *rest; };
+Backward plan(const oob_expert_linear_t *p, const oob_expert_linear_grad *g, Arena &w) {
+  Backward b{{g->dy, g->dy_stride, 0}, {}, {}, {}, {}, nullptr, nullptr};
+  if (makes_dz(p, g)) b.dz = {w.take((size_t)p->R * up(p->N, 8) * 2), up(p->N, 8), 0};
+  if (g->db) b.sums = (float *)w.take(sums_bytes(p));
+  if (g->dx) {
+    b.w = plan_w(p, w, b.how_w);
+    size_t rest = rest_bytes(p->R, p->E, p->K, p->N);
+    if (rest) b.rest = (float *)w.take(rest);
+  }
+  if (g->dw) b.x = plan_x(p, w, b.how_x);
+  return b;
 }
 
 template <class E> int backward(const oob_expert_linear_t *p, const oob_expert_linear_grad *g, Arena w, hipStream_t st) {
-  Operand dz{g->dy, g->dy_stride, 0};
   bool makes = makes_dz(p, g);
-  if (makes) dz = {w.take((size_t)p->R * up(p->N, 8) * 2), up(p->N, 8), 0};
-  float *sums = g->db ? (float *)w.take(sums_bytes(p)) : nullptr;
+  Backward b = plan(p, g, w);
   if (!w.ok()) return OOB_ECAPACITY;
+  if (p->R) pack(b.how_w, b.how_x, st);
+  Operand dz = b.dz;
+  float *sums = b.sums;
   Division d{p->offsets, p->E, p->R};
   if (makes || g->db) {
     ActGrad a{};
@@ -694,27 +707,30 @@ template <class E> int backward(const oob_expert_linear_t *p, const oob_expert_l
     if (g->db) k_experts_db<E><<<dim3((unsigned)tiles(p->N, 64), p->E), 256, 0, st>>>(a, (E *)g->db);
   }
   int rc = hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
+  Experts x{};
+  x.g.A = dz.p, x.g.lda = dz.ld, x.d = d;
   if (rc == OOB_OK && g->dx && p->R) {
-    Arena more = w; /* what one product takes is free again for the next on the stream */
-    Operand b = pack_w(p, more, st);
-    size_t rest = rest_bytes(p->R, p->E, p->K, p->N);
-    Experts x{};
-    x.g.partial = rest ? (float *)more.take(rest) : nullptr;
-    if (!more.ok()) return OOB_ECAPACITY;
-    x.g.A = dz.p, x.g.lda = dz.ld, x.g.B = b.p, x.g.ldb = b.ld, x.expert_stride = b.part;
-    x.g.N = p->K, x.g.K = p->N, x.g.C = g->dx, x.g.ldc = g->dx_stride, x.d = d;
+    x.g.B = b.w.p, x.g.ldb = b.w.ld, x.expert_stride = b.w.part, x.g.partial = b.rest;
+    x.g.N = p->K, x.g.K = p->N, x.g.C = g->dx, x.g.ldc = g->dx_stride;
     rc = products<E, false, false, false>(x, st);
   }
   if (rc == OOB_OK && g->dw) {
-    Arena more = w;
-    Operand b = pack_x(p, more, st);
-    if (!more.ok()) return OOB_ECAPACITY;
-    Experts x{};
-    x.g.A = dz.p, x.g.lda = dz.ld, x.g.B = b.p, x.g.ldb = b.ld;
-    x.g.M = p->N, x.g.N = p->K, x.g.C = g->dw, x.g.ldc = p->K, x.d = d;
+    x.g.B = b.x.p, x.g.ldb = b.x.ld, x.expert_stride = 0, x.g.partial = nullptr;
+    x.g.M = p->N, x.g.N = p->K, x.g.K = 0, x.g.C = g->dw, x.g.ldc = p->K;
     rc = products<E, false, false, true>(x, st);
   }
   return rc;
+}
+
+size_t forward_bytes(const oob_expert_linear_t *p) {
+  Arena w{nullptr, 0, 0};
+  plan(p, w);
+  return w.used;
+}
+size_t backward_bytes(const oob_expert_linear_t *p, const oob_expert_linear_grad *g) {
+  Arena w{nullptr, 0, 0};
+  plan(p, g, w);
+  return w.used;
 }
 
 bool even(const void *p) { return multiple(p, 2); }

@@ -87,16 +87,16 @@ def _enqueue(name, at, *args, size=None):
         binding.check(rc, name)
 
 
-def _numbers(t, shape, device, name):
-    """A contiguous int32 tensor."""
-    if not (t.dtype == torch.int32 and t.device == device and tuple(t.shape) == tuple(shape) and t.is_contiguous()):
-        raise ValueError(f"{name}: a contiguous int32 {list(shape)} on {device} is wanted")
+def _numbers(t, shape, like, name):
+    """A contiguous int32 tensor on the device of `like`."""
+    if not (t.dtype is torch.int32 and t.get_device() == like.get_device() and t.shape == shape and t.is_contiguous()):
+        raise ValueError(f"{name}: a contiguous int32 {list(shape)} on {like.device} is wanted")
     return t.data_ptr()
 
 
-def _floats(t, shape, device, name):
-    if not (t.dtype == torch.float32 and t.device == device and tuple(t.shape) == tuple(shape) and t.is_contiguous()):
-        raise ValueError(f"{name}: contiguous float32 {list(shape)} on {device} is wanted")
+def _floats(t, shape, like, name):
+    if not (t.dtype is torch.float32 and t.get_device() == like.get_device() and t.shape == shape and t.is_contiguous()):
+        raise ValueError(f"{name}: contiguous float32 {list(shape)} on {like.device} is wanted")
     return t.data_ptr()
 
 
@@ -133,9 +133,10 @@ def route(logits, k, score="softmax", bias=None, groups=1, keep_groups=None, gro
         raise ValueError(f"{keep_groups} groups of {args.E // groups} experts do not hold {k}")
     args.groups, args.keep_groups, args.group_best = groups, keep_groups, group_best
     if bias is not None:
-        args.bias = _floats(bias, (args.E,), logits.device, "bias")
+        args.bias = _floats(bias, (args.E,), logits, "bias")
     shape = (*logits.shape[:-1], k)
-    experts, weights = logits.new_empty(shape, dtype=torch.int32), logits.new_empty(shape, dtype=torch.float32)
+    new = logits.new_empty
+    experts, weights = new(shape, dtype=torch.int32), new(shape, dtype=torch.float32)
     args.experts, args.weights = experts.data_ptr(), weights.data_ptr()
     _enqueue("oob_expert_route", logits.get_device(), C.byref(args))
     return experts, weights
@@ -146,8 +147,8 @@ def route_backward(dweights, logits, experts, score="softmax", renormalize=True,
     _load()
     args = _route_args(logits, experts.shape[-1], score, renormalize, scale)
     shape = (*logits.shape[:-1], args.k)
-    args.experts = _numbers(experts, shape, logits.device, "experts")
-    d = _floats(dweights, shape, logits.device, "dweights")
+    args.experts = _numbers(experts, shape, logits, "experts")
+    d = _floats(dweights, shape, logits, "dweights")
     out = logits.new_empty(logits.shape)
     _enqueue("oob_expert_route_backward", logits.get_device(), C.byref(args), d, out.data_ptr(), args.E)
     return out
@@ -201,8 +202,8 @@ def _linear_args(x, w, offsets, rows, act):
         if not (R == 0 if T == 0 else R % T == 0 and R > 0):
             raise ValueError(f"rows: {R} pairs do not divide among {T} tokens")
         per = R // T if T else 1
-        rows = _numbers(rows, rows.shape, x.device, "rows")
-    args = oob_expert_linear_t(dtype, _act(act), E, per, R, T, N, K, _numbers(offsets, (E + 1,), x.device, "offsets"), rows, x2.data_ptr(),
+        rows = _numbers(rows, rows.shape, x, "rows")
+    args = oob_expert_linear_t(dtype, _act(act), E, per, R, T, N, K, _numbers(offsets, (E + 1,), x, "offsets"), rows, x2.data_ptr(),
                                w.data_ptr(), None, None, None)
     args.x_stride = _stride(x2)
     args.w_stride = w.stride(1) if N > 1 else K
@@ -222,7 +223,7 @@ def expert_linear(x, w, offsets, bias=None, rows=None, act="none", keep=False, o
     y = x.new_empty((args.R, args.N)) if out is None else _out(out, args.R, args.N, x, "out")
     z = x.new_empty((args.R, args.N)) if keep and args.act else None
     if bias is not None:
-        if not (bias.dtype is x.dtype and bias.device == x.device and tuple(bias.shape) == (args.E, args.N) and bias.is_contiguous()):
+        if not (bias.dtype is x.dtype and bias.get_device() == x.get_device() and bias.shape == (args.E, args.N) and bias.is_contiguous()):
             raise ValueError(f"bias: a contiguous [{args.E}, {args.N}] of {x.dtype} on {x.device} is wanted")
         args.bias = bias.data_ptr()
     args.y, args.y_stride, args.z, args.z_stride = y.data_ptr(), _stride(y), _ptr(z), args.N
@@ -280,8 +281,8 @@ def _sum_args(y, place, weights):
         raise ValueError(f"1 to {MAX_CHOICES} choices are supported")
     dtype = _dtype(y, wide=True)
     y = _rows(y, y.shape[1], y, "y")
-    return oob_expert_sum_t(dtype, k, place.numel() // k, y.shape[0], y.shape[1], y.data_ptr(), _numbers(place, place.shape, y.device, "place"),
-                            None if weights is None else _floats(weights, place.shape, y.device, "weights"), None, None, _stride(y), 0, 0)
+    return oob_expert_sum_t(dtype, k, place.numel() // k, y.shape[0], y.shape[1], y.data_ptr(), _numbers(place, place.shape, y, "place"),
+                            None if weights is None else _floats(weights, place.shape, y, "weights"), None, None, _stride(y), 0, 0)
 
 
 def expert_sum(y, place, weights=None, residual=None):
@@ -313,13 +314,13 @@ def expert_sum_backward(dout, y, place, weights=None, need=("y", "weights"), out
         raise ValueError("need: out of y, weights")
     if not (out is None or "y" in need):
         raise ValueError("out: dy is not among what is needed")
-    if not (tuple(dout.shape) == (*place.shape[:-1], args.C)):
+    if not (dout.shape == (*place.shape[:-1], args.C)):
         raise ValueError("dout: the result's shape is wanted")
     d = _rows(dout, args.C, y, "dout")
     dy = None
     if "y" in need:
         dy = y.new_empty((args.R, args.C)) if out is None else _out(out, args.R, args.C, y, "out")
-    dweights = torch.empty(place.shape, dtype=torch.float32, device=y.device) if "weights" in need else None
+    dweights = y.new_empty(place.shape, dtype=torch.float32) if "weights" in need else None
     _enqueue("oob_expert_sum_backward", y.get_device(), C.byref(args), d.data_ptr(), _stride(d), _ptr(dy), args.C if dy is None else _stride(dy),
              _ptr(dweights))
     return dy, dweights
@@ -373,7 +374,7 @@ def clip_gradients(tensors, max_norm, norm=None, out=None):
         raise ValueError("tensors that are written share memory")
     given = None
     if norm is not None:
-        given = _floats(norm, norm.shape, tensors[0].device, "norm")
+        given = _floats(norm, norm.shape, tensors[0], "norm")
         if norm.numel() != 1:
             raise ValueError("norm: one value is wanted")
         size = ("oob_clip_workspace_size", 0, sizes)
