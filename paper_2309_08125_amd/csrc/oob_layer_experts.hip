@@ -105,7 +105,7 @@ template <class E, int ROWS, int THREADS> struct Gathered {
     for (int i = 0; i < LOADS; i++) {
       int p = (i * THREADS + threadIdx.x) * 16, r = p / 128, c = (p / 16 % 8) ^ (r / 2 % 8);
       k = c * 8; /* the same for all */
-      int64_t t = r < left ? rows[r] : -1;
+      int t = r < left ? rows[r] : -1;
       t = t < 0 ? -1 : t / per;
       off[i] = t >= 0 && t < T ? (uint32_t)(t * ld * 2 + c * 16) : OOB_LAYER_OUT;
     }

@@ -627,6 +627,48 @@ def test_streams_and_repeated_runs_give_the_same_bits(P):
         assert all(torch.equal(a, b) for a, b in zip(r, want))
 
 
+# ---- more than 32 bits of elements or bytes --------------------------------------------------------------------
+def test_far_rows_of_logits_sums_and_tensors(P):
+    E = 1024
+    l = torch.zeros(2_100_000, E, dtype=torch.bfloat16, device="cuda")  # noqa: E741  2.1e9 values
+    l[-40:] = rand(40, E)
+    experts, w = P.route(l, 4)
+    last = P.route(l[-40:].clone(), 4)
+    assert torch.equal(experts[-40:], last[0]) and torch.equal(w[-40:], last[1]) and experts[0].tolist() == [0, 1, 2, 3]
+    d = P.route_backward(torch.ones_like(w), l, experts)
+    assert torch.equal(d[-40:], P.route_backward(torch.ones_like(last[1]), l[-40:].clone(), last[0]))
+    del d
+    y = l.view(-1, 4096)  # 525 000 rows
+    place = torch.tensor([[y.shape[0] - 1, 0], [y.shape[0] - 7, -1], [3, y.shape[0] - 2]], dtype=torch.int32, device="cuda")
+    weights = rand(3, 2, t=torch.float32)
+    rows = y[place.clamp(min=0).long()].double() * weights.double()[:, :, None] * (place >= 0)[:, :, None]
+    within(P.expert_sum(y, place, weights), rows.sum(1), U[y.dtype] * rows.sum(1).abs() + 1e-6 * rows.abs().sum(1) + 1e-30, "sum")
+    dy, _ = P.expert_sum_backward(rand(3, 4096), y, place, weights, out=torch.zeros_like(y))
+    assert dy[-1].any() and dy[-7].any() and dy[-2].any() and not dy[-6:-2].any() and not dy[4:-7].any()
+    del dy
+    l.fill_(1.0)
+    assert abs(P.gradient_norm([l]).item() - l.numel() ** 0.5) <= 1
+    P.clip_gradients([l], 0.5 * l.numel() ** 0.5)
+    assert float(l[0, 0]) == float(l[-1, -1]) == 0.5 and bool((l == 0.5).all())
+
+
+def test_linear_tokens_that_32_bit_offsets_do_not_reach(P):
+    T, E, N, K = 1 << 18, 2, 16, 64
+    wide = torch.zeros(T, 4104, dtype=torch.bfloat16, device="cuda")  # rows 8208 bytes apart: 2.15 GB
+    x = wide[:, :K]
+    x.copy_(rand(T, K))
+    offsets, rows, _ = P.expert_rows(torch.randint(0, E, (T, 1), dtype=torch.int32, device="cuda"), E)
+    w, dy = rand(E, N, K), rand(T, N)
+    y, want = P.expert_linear(x, w, offsets, rows=rows), P.expert_linear(x.contiguous(), w, offsets, rows=rows)
+    assert torch.equal(y, want)
+    got, want = (P.expert_linear_backward(dy, a, w, offsets, rows=rows) for a in (x, x.contiguous()))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    big = torch.zeros(40, N, 4 << 20, dtype=torch.bfloat16, device="cuda")[:, :, :K]       # rows 8 MB apart: copied; experts 128 MB: 5 GB in all
+    big.copy_(rand(40, N, K))
+    offsets, rows, _ = P.expert_rows(torch.randint(0, 40, (300, 1), dtype=torch.int32, device="cuda"), 40)
+    assert torch.equal(P.expert_linear(x[:300], big, offsets, rows=rows), P.expert_linear(x[:300], big.contiguous(), offsets, rows=rows))
+
+
 # ---- refusals ----------------------------------------------------------------------------------------------
 def test_refusals(P):
     l = rand(4, 8)  # noqa: E741
