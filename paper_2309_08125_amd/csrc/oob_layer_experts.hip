@@ -289,6 +289,9 @@ struct Where { int expert, left, k, part; int64_t row, n0; const char *pa, *pb; 
 
 /* Rows of y (BK: W as it is), of dx (W by its columns) or, DW, the matrices dw[e] = dz^T x over the rows of e.  A workgroup takes one tile after the other, every
  * gridDim-th: the first loads of the next are asked for before the present one's epilogue.
+ * 8192 rows, 8 experts, 4096 x 8192, bfloat16 (550 GFLOP each): y 620 us, dx 510, dw 555; a library's eight products of 1024 rows, without bias, activation and z, 497, 622 and 618.  Matrix
+ * cores are busy 60 % of the time that a unit has a tile, at 1.8 GHz; without the loads y takes 510 us, without the epilogue 535.  Few rows: 16 tokens, 8 experts of 2048 x 2048: 13.2 us,
+ * 5.1 TB/s of matrices (two buffers: 19.2).
  * Large tiles that are left over from whole rounds of the GPU, where they would keep few compute units busy for a round, are left to a second launch (REST), in which k
  * is divided among several workgroups that leave their sums, and a third that joins them.  8192 rows, 8 experts, 4096 x 8192, dx: 576 tiles,
  * 508 us; 597 without (the quarters of the 64 tiles left over, done as tiles of 128: 566). */

@@ -5,7 +5,8 @@
 namespace layer {
 namespace {
 
-/* A token takes `width` threads of a workgroup (a power of two), eight columns each at a time. */
+/* A token takes `width` threads of a workgroup (a power of two), eight columns each at a time, eight choices' rows on their way together.  Memory bounds it: 4096
+ * tokens, 8 choices, 4096 columns, bfloat16: 78 us (335 MB, 4.3 TB/s), the gradients 122 us (570 MB, 4.7 TB/s). */
 struct Sum {
   oob_expert_sum_t p;
   int width;
