@@ -91,15 +91,15 @@ template <class E> __global__ __launch_bounds__(256) void k_sum_grad(Sum g) {
 #pragma unroll
     for (int j = 0; j < TOGETHER; j++)
       for (int o = 1; o < run; o *= 2) dot[j] += __shfl_xor(dot[j], o);
-    if (g.width > 64) { /* one token a workgroup: its waves' sums in their order */
+    if (g.width > 64) { /* the sums of a token's waves, in their order */
       __syncthreads();
       if (lane() == 0)
         for (int j = 0; j < TOGETHER; j++) part[threadIdx.x / 64][j] = dot[j];
       __syncthreads();
       if (at == 0)
         for (int j = 0; j < TOGETHER; j++) {
-          dot[j] = part[0][j];
-          for (int wave = 1; wave < g.width / 64; wave++) dot[j] += part[wave][j];
+          dot[j] = part[threadIdx.x / 64][j];
+          for (int wave = 1; wave < g.width / 64; wave++) dot[j] += part[threadIdx.x / 64 + wave][j];
         }
     }
     if (live && at == 0)

@@ -434,6 +434,12 @@ def test_sum(P, T, k, C, of, t):
             assert only[1] is None and torch.equal(only[0][place[at].long()], d[:, None].expand(T, k, C)[at])
 
 
+@pytest.mark.parametrize("t", ALL)
+@pytest.mark.parametrize("C", [9, 17, 33, 72, 136, 264, 300, 513, 700, 1024, 1025])
+def test_sum_of_every_number_of_tokens_a_workgroup(P, C, t):
+    test_sum(P, 37, 3, C, 9, t)
+
+
 def test_sum_places_out_of_range(P):
     y, w, d = rand(6, 40), rand(3, 2, t=torch.float32), rand(3, 40)
     place = torch.tensor([[0, -1], [6, 2147483647], [-2147483648, 5]], dtype=torch.int32, device="cuda")
