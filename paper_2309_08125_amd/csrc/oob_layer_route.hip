@@ -54,9 +54,10 @@ __device__ inline double sum_over(double v, int lanes) {
   for (int o = 1; o < lanes; o *= 2) v += __shfl_xor(v, o);
   return v;
 }
-/* Numbers in the order of what they stand for: 0 is nothing (absent or taken), 1 a NaN, -inf and all else above. */
+/* Numbers in the order of what they stand for: 0 is nothing (absent or taken), NaN above it, -inf and all else above that.  The five lowest bits of those of
+ * 32 can give way to another number, and a NaN's is not 0 then either. */
 __device__ inline uint32_t key_of(float v) {
-  if (v != v) return 1;
+  if (v != v) return 32;
   uint32_t b = __float_as_uint(v + 0.f); /* -0 is 0 */
   return b >> 31 ? ~b : b | 0x80000000u;
 }

@@ -151,6 +151,28 @@ def test_route_nan_and_infinity(P):
     assert (experts[:, 0] == 7).all() and (experts[:, -1] == 5).all()
 
 
+@pytest.mark.parametrize("T,E", [(1, 4), (3, 8), (40, 16), (3000, 12), (2, 24), (3000, 24)])
+def test_route_every_expert_where_one_is_nan(P, T, E):
+    """NaN comes last, and every expert is chosen once: with scores that are compared in 32 bits first, and with logits."""
+    for bias in (torch.linspace(-1, 1, E, device="cuda"), None):
+        for groups in (1, 4):
+            for at in (0, 3, E // 2, E - 1):
+                l = rand(T, E, t=torch.float32)  # noqa: E741
+                l[:, at] = math.nan
+                experts, _ = P.route(l, E, "sigmoid", bias=bias, groups=groups)
+                want = X.choose(l.double().cpu(), E, "sigmoid", None if bias is None else bias.double().cpu(), groups, groups, 2)
+                assert (experts[:, -1] == at).all() and torch.equal(experts.cpu().long(), want), (groups, at)
+
+
+@pytest.mark.parametrize("T", [5, 5000])
+@pytest.mark.parametrize("at", [0, 3, 6, 7, 15])
+def test_route_all_of_a_group_where_one_is_nan(P, T, at):
+    l = rand(T, 64, t=torch.float32)  # noqa: E741
+    l[:, at::16] = math.nan
+    experts, _ = P.route(l, 16, "sigmoid", groups=4, keep_groups=1)
+    assert torch.equal(experts.cpu().long(), X.choose(l.double().cpu(), 16, "sigmoid", None, 4, 1, 2)) and (experts[:, -1] % 16 == at).all()
+
+
 def test_route_strides_shapes_and_gradient_of_several_axes(P):
     l = rand(3, 4, 20, t=torch.float16)  # noqa: E741
     experts, w = P.route(l, 3)
