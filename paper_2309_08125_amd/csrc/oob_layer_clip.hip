@@ -133,14 +133,23 @@ bool tensors_ok(int n, const void *const *from, void *const *to, const int64_t *
   return true;
 }
 
-bool overlap(int n, const void *const *to, const int64_t *sizes, const int *types) try {
-  std::vector<std::pair<uintptr_t, uintptr_t>> parts;
+/* Memory that is written and written or read by others. */
+bool overlap(int n, const void *const *from, const void *const *to, const int64_t *sizes, const int *types, const void *given) try {
+  using Part = std::pair<uintptr_t, uintptr_t>;
+  std::vector<Part> parts;
+  auto part = [&](const void *p, int i) { return Part{(uintptr_t)p, (uintptr_t)p + (uintptr_t)sizes[i] * (types[i] == OOB_FP32 ? 4 : 2)}; };
   for (int i = 0; i < n; i++)
-    if (sizes[i]) parts.push_back({(uintptr_t)to[i], (uintptr_t)to[i] + (uintptr_t)sizes[i] * (types[i] == OOB_FP32 ? 4 : 2)});
+    if (sizes[i]) parts.push_back(part(to[i], i));
   std::sort(parts.begin(), parts.end());
   for (size_t i = 1; i < parts.size(); i++)
     if (parts[i].first < parts[i - 1].second) return true;
-  return false;
+  auto written = [&](Part p) { /* the parts do not overlap: only the last that begins before p's end can reach into it */
+    auto after = std::lower_bound(parts.begin(), parts.end(), Part{p.second, 0});
+    return after != parts.begin() && std::prev(after)->second > p.first;
+  };
+  for (int i = 0; i < n; i++)
+    if (sizes[i] && from[i] != to[i] && written(part(from[i], i))) return true;
+  return given && written({(uintptr_t)given, (uintptr_t)given + 4});
 } catch (...) { /* no host memory: refused, nothing passes the C entry */
   return true;
 }
@@ -207,8 +216,8 @@ extern "C" size_t oob_clip_workspace_size(int n, const int64_t *sizes) {
   return (size_t)up(sums_of(n, sizes) * 8, 256);
 }
 
-extern "C" int oob_clip_overlap(int n, const void *const *to, const int64_t *sizes, const int *types) {
-  return n > 0 && to && sizes && types && overlap(n, to, sizes, types);
+extern "C" int oob_clip_overlap(int n, const void *const *from, const void *const *to, const int64_t *sizes, const int *types, const float *given) {
+  return n > 0 && from && to && sizes && types && overlap(n, from, to, sizes, types, given);
 }
 
 extern "C" int oob_clip_norm(int n, const void *const *from, const int64_t *sizes, const int *types, float *norm, void *workspace, size_t bytes,
@@ -225,7 +234,7 @@ extern "C" int oob_clip_norm(int n, const void *const *from, const int64_t *size
 extern "C" int oob_clip_scale(int n, const void *const *from, void *const *to, const int64_t *sizes, const int *types, float max_norm,
                               const float *given, float *norm, void *workspace, size_t bytes, void *stream) {
   if (!tensors_ok(n, from, to, sizes, types) || (n && !to) || !(max_norm >= 0) || !multiple(workspace, 256)) return OOB_EINVAL;
-  if (!multiple(given, 4) || !multiple(norm, 4) || (!given && !norm) || overlap(n, to, sizes, types)) return OOB_EINVAL;
+  if (!multiple(given, 4) || !multiple(norm, 4) || (!given && !norm) || overlap(n, from, to, sizes, types, given)) return OOB_EINVAL;
   size_t need = n && !given ? oob_clip_workspace_size(n, sizes) : 0;
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
   hipStream_t st = (hipStream_t)stream;

@@ -54,7 +54,7 @@ def _load():
                            ("oob_expert_rows", [p, n, i, i, p, p, p, p, C.c_size_t, p]),
                            ("oob_expert_linear", [linear, p, C.c_size_t, p]), ("oob_expert_linear_backward", [linear, grad, p, C.c_size_t, p]),
                            ("oob_expert_sum", [total, p]), ("oob_expert_sum_backward", [total, p, n, p, n, p, p]),
-                           ("oob_clip_overlap", [i, p, p, p]), ("oob_clip_norm", [i, p, p, p, p, p, C.c_size_t, p]),
+                           ("oob_clip_overlap", [i, p, p, p, p, p]), ("oob_clip_norm", [i, p, p, p, p, p, C.c_size_t, p]),
                            ("oob_clip_scale", [i, p, p, p, p, C.c_float, p, p, p, C.c_size_t, p])):
             call = _calls[name] = getattr(L, name)
             call.argtypes, call.restype = args, C.c_int
@@ -357,7 +357,8 @@ def clip_gradients(tensors, max_norm, norm=None, out=None):
     returns the norm.
 
     norm: a float32 scalar on the tensors' device to go by in place of gradient_norm(tensors), one that all ranks have added up, say.
-    out: as many tensors of the same sizes and types for the results; without it they are changed in place (no two may share memory)."""
+    out: as many tensors of the same sizes and types for the results; without it they are changed in place.  What is written may share no memory
+    with anything else that is written or read."""
     _load()
     tensors = list(tensors)
     n, at, ptrs, sizes, types = _tensors(tensors, "tensors")
@@ -370,13 +371,14 @@ def clip_gradients(tensors, max_norm, norm=None, out=None):
         if not (m == n and of == at and out_sizes == sizes and out_types == types):
             raise ValueError("out: not like the tensors")
     sizes, types = (C.c_int64 * n)(*sizes), (C.c_int * n)(*types)
-    if _lib.oob_clip_overlap(n, to, sizes, types):
-        raise ValueError("tensors that are written share memory")
     given = None
     if norm is not None:
         given = _floats(norm, norm.shape, tensors[0], "norm")
         if norm.numel() != 1:
             raise ValueError("norm: one value is wanted")
+    if _lib.oob_clip_overlap(n, ptrs, to, sizes, types, given):
+        raise ValueError("tensors that are written share memory with one another or with what is read")
+    if given:
         size = ("oob_clip_workspace_size", 0, sizes)
     else:
         norm = tensors[0].new_empty((), dtype=torch.float32)

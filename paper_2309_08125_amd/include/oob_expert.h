@@ -123,11 +123,12 @@ int oob_expert_sum_backward(const oob_expert_sum_t *p, const void *dout, int64_t
 size_t oob_clip_workspace_size(int n, const int64_t *sizes);
 int oob_clip_norm(int n, const void *const *from, const int64_t *sizes, const int *types, float *norm, void *workspace, size_t bytes,
                   void *stream);
-/* 1 where two of the tensors share memory (host arrays; nothing is enqueued), 0 otherwise. */
-int oob_clip_overlap(int n, const void *const *to, const int64_t *sizes, const int *types);
+/* 1 where a tensor of `to` shares memory with another of them, with one of `from` that it does not lie on, or with the value `given` (may be NULL), 0
+ * otherwise (host arrays; nothing is enqueued). */
+int oob_clip_overlap(int n, const void *const *from, const void *const *to, const int64_t *sizes, const int *types, const float *given);
 /* to[i] = from[i] factor, factor = max_norm / norm where norm > max_norm and finite, 1 otherwise.  to[i] may be from[i]: with a factor of
  * 1 nothing is written then.  given (float [1], on the device) is the norm if it is not NULL, one that several GPUs have added up, say; otherwise it is
- * that of oob_clip_norm, which is written to `norm`.  Tensors of `to` that share memory: OOB_EINVAL. */
+ * that of oob_clip_norm, which is written to `norm`.  Where oob_clip_overlap is 1: OOB_EINVAL. */
 int oob_clip_scale(int n, const void *const *from, void *const *to, const int64_t *sizes, const int *types, float max_norm,
                    const float *given, float *norm, void *workspace, size_t bytes, void *stream);
 

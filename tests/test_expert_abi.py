@@ -137,5 +137,15 @@ def test_clip_refuses():
     assert {scale(to=None), scale(m=-1.0), scale(m=float("nan")), scale(out=0), scale(out=FAKE + 2), scale(given=FAKE + 2, out=0)} == {P.OOB_EINVAL}
     assert scale(b=need - 1) == P.OOB_ECAPACITY
     same = (C.c_void_p * 3)(FAKE, FAKE + 4096, FAKE + 4096 + 198)  # two that share two bytes
-    assert lib().oob_clip_overlap(3, same, sizes, types) == 1 and scale(to=same) == P.OOB_EINVAL
-    assert lib().oob_clip_overlap(3, ptr, sizes, types) == 0 and lib().oob_clip_overlap(3, (C.c_void_p * 3)(FAKE, FAKE + 200, FAKE + 400), sizes, types) == 0
+    overlap = lambda to, given=None: lib().oob_clip_overlap(3, ptr, to, sizes, types, given)  # noqa: E731
+    at = lambda *a: (C.c_void_p * 3)(*a)  # noqa: E731
+    assert overlap(same) == 1 and scale(to=same) == P.OOB_EINVAL
+    far = FAKE + (1 << 20)
+    assert overlap(ptr) == overlap(at(far, far + 200, far + 400)) == 0
+    # what is written lies on another's input, or beside its own by one value; or on the given norm
+    for to in (at(FAKE + 4096, FAKE, FAKE + 8192), at(FAKE + 2, far, far + 200), at(FAKE - 198, far, far + 200), at(far, far + 200, FAKE + 4096 + 198)):
+        assert overlap(to) == 1 and scale(to=to) == P.OOB_EINVAL
+    assert overlap(at(FAKE + 200, far, FAKE + 4096 - 200)) == 0
+    for given, shares in ((FAKE - 4, 0), (FAKE, 1), (FAKE + 196, 1), (FAKE + 200, 0), (FAKE + 8192 + 196, 1), (FAKE + 8192 + 200, 0)):
+        assert overlap(ptr, given) == shares
+        assert not shares or scale(given=given, out=0) == P.OOB_EINVAL

@@ -722,7 +722,8 @@ def test_refusals(P):
                  lambda: P.expert_sum_backward(rand(4, 24), y, place, wt, need=("weights",), out=y),
                  lambda: P.gradient_norm([]), lambda: P.gradient_norm([l.double()]), lambda: P.gradient_norm([l.cpu()]), lambda: P.gradient_norm([l, rand(4, 4).t()]),
                  lambda: P.clip_gradients([l], -1.0), lambda: P.clip_gradients([l], math.nan), lambda: P.clip_gradients([l], 1.0, norm=torch.ones(2, device="cuda")),
-                 lambda: P.clip_gradients([l], 1.0, norm=torch.ones(())), lambda: P.clip_gradients([l, l], 1.0), lambda: P.clip_gradients([l[:3], l[2:]], 1.0),
+                 lambda: P.clip_gradients([l], 1.0, norm=torch.ones(())), lambda: P.clip_gradients([l, l], 1.0), lambda: P.clip_gradients([l[:2], l[2:]], 1.0, out=[l[2:], l[:2]]),
+                 lambda: P.clip_gradients([wt], 1.0, norm=wt[0, 0]), lambda: P.clip_gradients([l[:3], l[2:]], 1.0),
                  lambda: P.clip_gradients([l], 1.0, out=[]), lambda: P.clip_gradients([l], 1.0, out=[l[:3]]), lambda: P.clip_gradients([l], 1.0, out=[l.half()])):
         with pytest.raises(ValueError):
             call()
