@@ -215,12 +215,12 @@ def expert_linear(x, w, offsets, bias=None, rows=None, act="none", keep=False, o
     """Row r of expert e, offsets[e] <= r < offsets[e + 1]: y[r] = act(x[token] w[e]^T + bias[e]).
 
     x [T, K] with rows [R] of expert_rows: row r is that of token rows[r] // (R // T); or x [R, K], in order already (rows None).  w [E, N,
-    K], bias [E, N]; bfloat16 or float16, rows of any stride.  y [R, N], or `out`; rows that are no expert's stay as they are (in a
+    K], bias [E, N]; bfloat16 or float16, rows of any stride.  y [R, N], or `out`, which shares no memory with x, w and bias; rows that are no expert's stay as they are (in a
     new y: whatever memory held).  keep=True: (y, z) with z = x w^T + bias, which the backward pass wants where there is an
     activation (z is None without one).  No autograd graph is built: gradients are expert_linear_backward's."""
     _load()
     args = _linear_args(x, w, offsets, rows, act)
-    y = x.new_empty((args.R, args.N)) if out is None else _out(out, args.R, args.N, x, "out")
+    y = x.new_empty((args.R, args.N)) if out is None else _out(out, args.R, args.N, x, "out", x, w, bias)
     z = x.new_empty((args.R, args.N)) if keep and args.act else None
     if bias is not None:
         if not (bias.dtype is x.dtype and bias.get_device() == x.get_device() and bias.shape == (args.E, args.N) and bias.is_contiguous()):
@@ -232,20 +232,39 @@ def expert_linear(x, w, offsets, bias=None, rows=None, act="none", keep=False, o
     return (y, z) if keep else y
 
 
-def _out(t, R, cols, like, name):
-    """A matrix to write to; no two of its rows may share memory."""
+def _part(t):
+    """Where a tensor lies: first byte, end, and of rows (all but its last axis) their pitch and length in bytes."""
+    size, at, n = t.element_size(), t.data_ptr(), t.shape
+    span = sum((c - 1) * s for c, s in zip(n, t.stride())) + 1 if t.numel() else 0
+    return at, at + span * size, t.stride(0) * size if t.dim() == 2 and n[0] > 1 else 0, n[-1] * size
+
+
+def _apart(a, b):
+    """Whether two tensors share no memory; columns of one matrix of rows do not."""
+    a0, a1, pitch, wide = _part(a)
+    b0, b1, other, long = _part(b)
+    if a1 <= b0 or b1 <= a0:
+        return True
+    gap = (b0 - a0) % pitch if pitch and pitch == other else 0
+    return gap >= wide and gap + long <= pitch
+
+
+def _out(t, R, cols, like, name, *read):
+    """A matrix to write to; no two of its rows may share memory, and it may share none with what is read."""
     if not (t.dim() == 2 and t.shape[0] == R):
         raise ValueError(f"{name}: [{R}, {cols}] is wanted")
     t = _rows(t, cols, like, name)
     if not (R <= 1 or t.stride(0) >= cols):
         raise ValueError(f"{name}: its rows overlap")
+    if not all([v is None or _apart(t, v) for v in read]):
+        raise ValueError(f"{name}: it shares memory with what the call reads")
     return t
 
 
 def expert_linear_backward(dy, x, w, offsets, z=None, rows=None, act="none", need=("x", "w", "b"), out=None):
     """(dx, dw, db) of expert_linear: dz = dy act'(z), dx[r] = dz[r] w[e] (a row each: expert_sum(dx, place) adds those of a token),
     dw[e] = sum of dz[r]^T x[token], db[e] = sum of dz[r], 0 for an expert without rows; None for what `need` does not name.  out: where
-    dx goes; rows that are no expert's stay as they are."""
+    dx goes, no memory that the call reads; rows that are no expert's stay as they are."""
     _load()
     args = _linear_args(x, w, offsets, rows, act)
     if not (args.act == 0 or z is not None):
@@ -264,7 +283,7 @@ def expert_linear_backward(dy, x, w, offsets, z=None, rows=None, act="none", nee
         args.z, args.z_stride = z2.data_ptr(), _stride(z2)
     dx = None
     if "x" in need:
-        dx = x.new_empty((args.R, args.K)) if out is None else _out(out, args.R, args.K, x, "out")
+        dx = x.new_empty((args.R, args.K)) if out is None else _out(out, args.R, args.K, x, "out", dy2, x, w, z)
     dw = x.new_empty((args.E, args.N, args.K)) if "w" in need else None
     db = x.new_empty((args.E, args.N)) if "b" in need else None
     grad = oob_expert_linear_grad(dy2.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db), _stride(dy2), args.K if dx is None else _stride(dx))
@@ -306,7 +325,7 @@ def expert_sum(y, place, weights=None, residual=None):
 
 def expert_sum_backward(dout, y, place, weights=None, need=("y", "weights"), out=None):
     """(dy, dweights) of expert_sum: dy[place[t, j]] = weights[t, j] dout[t], dweights[t, j] = dout[t] . y[place[t, j]] (0 where the
-    place is out of range); None for what `need` does not name.  out: where dy goes; rows that are nobody's stay as they are.  No two
+    place is out of range); None for what `need` does not name.  out: where dy goes, apart from y and dout; rows that are nobody's stay as they are.  No two
     places may be the same (expert_rows makes such).  The residual's gradient is dout."""
     _load()
     args = _sum_args(y, place, weights)
@@ -319,7 +338,7 @@ def expert_sum_backward(dout, y, place, weights=None, need=("y", "weights"), out
     d = _rows(dout, args.C, y, "dout")
     dy = None
     if "y" in need:
-        dy = y.new_empty((args.R, args.C)) if out is None else _out(out, args.R, args.C, y, "out")
+        dy = y.new_empty((args.R, args.C)) if out is None else _out(out, args.R, args.C, y, "out", y, d)
     dweights = y.new_empty(place.shape, dtype=torch.float32) if "weights" in need else None
     _enqueue("oob_expert_sum_backward", y.get_device(), C.byref(args), d.data_ptr(), _stride(d), _ptr(dy), args.C if dy is None else _stride(dy),
              _ptr(dweights))

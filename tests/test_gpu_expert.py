@@ -346,6 +346,17 @@ def test_linear_strides_and_parts(P):
         linear_case(P, 90, 2, 3, 48, 40, "none", torch.bfloat16, need=need)
 
 
+def test_results_beside_what_is_read(P):
+    """Results in columns of the matrix whose other columns are read."""
+    offsets, rows, place = division(40, 1, 3)
+    wide, w = rand(40, 16 + 24), rand(3, 24, 16)
+    x, want = wide[:, :16], wide.clone()
+    y = P.expert_linear(x.clone(), w, offsets)
+    assert torch.equal(P.expert_linear(x, w, offsets, out=wide[:, 16:]), y) and torch.equal(wide[:, :16], want[:, :16])
+    dx = P.expert_linear_backward(y, x.clone(), w, offsets)[0]
+    assert torch.equal(P.expert_linear_backward(wide[:, 16:], x.clone(), w, offsets, out=x)[0], dx) and torch.equal(wide[:, 16:], y)
+
+
 def test_linear_without_tokens(P):
     w, offsets = rand(3, 16, 24), torch.zeros(4, dtype=torch.int32, device="cuda")
     none = torch.zeros(0, dtype=torch.int32, device="cuda")
@@ -702,7 +713,7 @@ def test_refusals(P):
     l = rand(4, 8)  # noqa: E741
     i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")  # noqa: E731
     x, w, offsets, rows = rand(4, 16), rand(3, 24, 16), i32(4), i32(8)
-    y, place, wt = rand(8, 24), i32(4, 2), torch.ones(4, 2, device="cuda")
+    y, place, wt, both = rand(8, 24), i32(4, 2), torch.ones(4, 2, device="cuda"), rand(4, 40)
     for call in (lambda: P.route(l, 0), lambda: P.route(l, 9), lambda: P.route(l, 2, "relu"), lambda: P.route(l, 2, groups=3), lambda: P.route(l, 3, groups=4, keep_groups=1),
                  lambda: P.route(l, 2, groups=4, keep_groups=5), lambda: P.route(l, 2, groups=2, group_best=3), lambda: P.route(l.cpu(), 2), lambda: P.route(l.double(), 2),
                  lambda: P.route(l, 2, bias=rand(8)), lambda: P.route(l, 2, bias=torch.zeros(7, device="cuda")), lambda: P.route(l, 2, scale=math.inf), lambda: P.route(l.t(), 2),
@@ -713,7 +724,9 @@ def test_refusals(P):
                  lambda: P.expert_linear(x, w.half(), offsets), lambda: P.expert_linear(x.float(), w.float(), offsets), lambda: P.expert_linear(x, w, offsets, rows=i32(7)),
                  lambda: P.expert_linear(x, w, offsets, rows=i32(0)), lambda: P.expert_linear(x, w, offsets, bias=rand(24)), lambda: P.expert_linear(x, w, offsets, act="tanh"),
                  lambda: P.expert_linear(x, w, offsets, out=rand(5, 24)), lambda: P.expert_linear(x, w, offsets, out=rand(1, 24).expand(4, 24)),
-                 lambda: P.expert_linear(x, w.transpose(1, 2), offsets), lambda: P.expert_linear(x, rand(1025, 1, 16), i32(1026)),
+                 lambda: P.expert_linear(x, w.transpose(1, 2), offsets), lambda: P.expert_linear(y, w.new_empty(3, 24, 24), offsets, out=y),
+                 lambda: P.expert_linear(both[:, :16], w, offsets, out=both[:, 8:32]), lambda: P.expert_linear(x, w, offsets, out=w.view(-1)[16:112].view(4, 24)),
+                 lambda: P.expert_linear_backward(y, y, w.new_empty(3, 24, 24), offsets, out=y), lambda: P.expert_sum_backward(rand(4, 24), y, place, wt, out=y), lambda: P.expert_linear(x, rand(1025, 1, 16), i32(1026)),
                  lambda: P.expert_linear_backward(rand(4, 24), x, w, offsets, act="gelu"), lambda: P.expert_linear_backward(rand(5, 24), x, w, offsets),
                  lambda: P.expert_linear_backward(rand(4, 24), x, w, offsets, need=("z",)), lambda: P.expert_linear_backward(rand(4, 24), x, w, offsets, need=("w",), out=rand(4, 16)),
                  lambda: P.expert_sum(y, place.long()), lambda: P.expert_sum(y, place, wt[:3]), lambda: P.expert_sum(y, place, wt.half()),
