@@ -634,12 +634,13 @@ bool sizes_ok(const oob_expert_linear_t *p) {
          p->per >= 1 && p->R >= 0 && p->T >= 0 && p->N >= 1 && p->K >= 1 && p->R < most && p->T < most && p->N < (1 << 21) && p->K < (1 << 21) &&
          (p->rows ? p->T * p->per == p->R : p->per == 1);
 }
-bool fits(int64_t blocks) { return blocks < (int64_t)1 << 31; }
-/* Workgroups of the smallest tiles and of the copies, 256 threads each. */
-bool launches_fit(const oob_expert_linear_t *p) {
+bool fits(int64_t tiles) { return tiles < (int64_t)1 << 31; }
+/* Numbers of the smallest tiles, which are 32-bit; threads of the copies, 2^32 at most. */
+bool launches_fit(const oob_expert_linear_t *p, bool forward) {
   int64_t most = (p->N > p->K ? p->N : p->K) + 64;
+  bool x_lies = forward ? x_loadable(p) : !p->rows && loadable(p->x, p->x_stride, p->K);
   return fits(row_tiles(p->R, p->E, 64) * tiles(most, 64)) && fits(p->E * up(tiles(p->N, 64) * tiles(p->K, 64), 8)) &&
-         fits((p->R + p->E * p->N) * ((up(p->K, 8)) / 8) / 256 + 1);
+         ((w_loadable(p) ? 0 : p->E * p->N) + (x_lies ? 0 : p->R)) * (up(p->K, 8) / 8) < ((int64_t)1 << 32) - 512;
 }
 
 struct Forward { Operand a, b; Packed x, w; float *rest; };
@@ -667,9 +668,10 @@ template <class E> int forward(const oob_expert_linear_t *p, Arena w, hipStream_
 bool makes_dz(const oob_expert_linear_t *p, const oob_expert_linear_grad *g) {
   return (g->dx || g->dw) && (p->act != OOB_ACT_NONE || !loadable(g->dy, g->dy_stride, p->N));
 }
-int run_rows(const oob_expert_linear_t *p) { /* about 1024 workgroups, 16 rows at least */
-  int64_t r = up(p->R * tiles(p->N, 512) / 1024, 16);
-  return (int)(r < 16 ? 16 : r > 4096 ? 4096 : r);
+int run_rows(const oob_expert_linear_t *p) { /* about 1024 workgroups, 16 rows at least; 65535 runs at most */
+  int64_t r = up(p->R * tiles(p->N, 512) / 1024, 16), least = up(p->R / 32768, 16);
+  r = r < 16 ? 16 : r > 4096 ? 4096 : r;
+  return (int)(r < least ? least : r);
 }
 size_t sums_bytes(const oob_expert_linear_t *p) { return (size_t)row_tiles(p->R, p->E, run_rows(p)) * p->N * 4; }
 
@@ -746,7 +748,7 @@ using namespace layer;
 extern "C" size_t oob_expert_linear_workspace_size(const oob_expert_linear_t *p) { return sizes_ok(p) && p->R ? forward_bytes(p) : 0; }
 
 extern "C" int oob_expert_linear(const oob_expert_linear_t *p, void *workspace, size_t bytes, void *stream) {
-  if (!sizes_ok(p) || !launches_fit(p)) return OOB_EINVAL;
+  if (!sizes_ok(p) || !launches_fit(p, true)) return OOB_EINVAL;
   if (p->R == 0) return OOB_OK;
   if (!p->offsets || !p->x || !p->w || !p->y || p->x_stride < p->K || p->w_stride < p->K || p->y_stride < p->N || p->expert_stride < 0) return OOB_EINVAL;
   if (p->z && p->z_stride < p->N) return OOB_EINVAL;
@@ -763,8 +765,7 @@ extern "C" size_t oob_expert_linear_backward_workspace_size(const oob_expert_lin
 }
 
 extern "C" int oob_expert_linear_backward(const oob_expert_linear_t *p, const oob_expert_linear_grad *g, void *workspace, size_t bytes, void *stream) {
-  if (!sizes_ok(p) || !g || !launches_fit(p) || !fits(p->R * (p->N / 8 + 1) / 256) || !p->offsets) return OOB_EINVAL;
-  if (row_tiles(p->R, p->E, run_rows(p)) > 65535 || p->E > 65535) return OOB_EINVAL;
+  if (!sizes_ok(p) || !g || !launches_fit(p, false) || !p->offsets) return OOB_EINVAL;
   if (p->R && (!g->dy || g->dy_stride < p->N || (p->act != OOB_ACT_NONE && (!p->z || p->z_stride < p->N)))) return OOB_EINVAL;
   if (p->R && g->dx && (!p->w || p->w_stride < p->K || p->expert_stride < 0 || g->dx_stride < p->K)) return OOB_EINVAL;
   if (p->R && g->dw && (!p->x || p->x_stride < p->K)) return OOB_EINVAL;

@@ -360,6 +360,17 @@ __global__ __launch_bounds__(256) void k_route_grad(RouteGrad g) {
   }
 }
 
+/* Tokens of a launch, which has less than 2^32 threads. */
+int64_t tokens_of(int lanes) { return ((int64_t)1 << 31) / lanes; }
+/* The same operands from token t on, n of them. */
+oob_route part_of(const oob_route &p, int64_t t, int64_t n) {
+  oob_route q = p;
+  q.T = p.T - t < n ? p.T - t : n;
+  q.logits = (const char *)p.logits + t * p.logits_stride * (p.dtype == OOB_FP32 ? 4 : 2), q.experts += t * p.k;
+  if (p.weights) q.weights += t * p.k;
+  return q;
+}
+
 int ceil2(int n) {
   int p = 1;
   while (p < n) p *= 2;
@@ -570,12 +581,15 @@ extern "C" int oob_expert_route(const oob_route *p, void *stream) {
   r.whole = r.per % 4 == 0 && multiple(p->logits, four) && p->logits_stride % 4 == 0;
   r.whole_bias = r.per % 4 == 0 && multiple(p->bias, 16);
   hipStream_t st = (hipStream_t)stream;
-  if (v <= 1) route<1>(r, st);
-  else if (v <= 2) route<2>(r, st);
-  else if (v <= 4) route<4>(r, st);
-  else if (v <= 8) route<8>(r, st);
-  else if (v <= 16) route<16>(r, st);
-  else route<32>(r, st);
+  for (int64_t t = 0, n = tokens_of(r.lanes); t < p->T; t += n) {
+    r.p = part_of(*p, t, n);
+    if (v <= 1) route<1>(r, st);
+    else if (v <= 2) route<2>(r, st);
+    else if (v <= 4) route<4>(r, st);
+    else if (v <= 8) route<8>(r, st);
+    else if (v <= 16) route<16>(r, st);
+    else route<32>(r, st);
+  }
   return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
 }
 
@@ -587,8 +601,10 @@ extern "C" int oob_expert_route_backward(const oob_route *p, const float *dweigh
   RouteGrad g{*p, dweights, dlogits, dlogits_stride, 0, p->E % 4 == 0 && dlogits_stride % 4 == 0 && multiple(dlogits, 4 * of)};
   int lanes = ceil2((p->E + 7) / 8), least = ceil2(p->k);
   g.lanes = lanes > 64 ? 64 : lanes < least ? least : lanes;
-  unsigned n = (unsigned)((p->T * g.lanes + 255) / 256);
-  k_route_grad<<<n, 256, 256 / g.lanes * p->E * 4, (hipStream_t)stream>>>(g);
+  for (int64_t t = 0, n = tokens_of(g.lanes); t < p->T; t += n) {
+    g.p = part_of(*p, t, n), g.dweights = dweights + t * p->k, g.dlogits = (char *)dlogits + t * dlogits_stride * of;
+    k_route_grad<<<(unsigned)((g.p.T * g.lanes + 255) / 256), 256, 256 / g.lanes * p->E * 4, (hipStream_t)stream>>>(g);
+  }
   return hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
 }
 

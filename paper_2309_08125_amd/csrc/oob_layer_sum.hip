@@ -129,14 +129,32 @@ int width_of(int64_t C) {
   return w;
 }
 
-template <class E> void sum(const Sum &g, hipStream_t st) {
-  int64_t per = 256 / g.width;
-  dim3 grid((unsigned)((g.p.T + per - 1) / per), (unsigned)((g.p.C + g.width * 8 - 1) / (g.width * 8)));
-  k_sum<E><<<grid, 256, 0, st>>>(g);
+/* The same operands from token t on, as many as a launch takes: it has less than 2^32 threads. */
+template <class E> Sum part_of(const Sum &g, int64_t t, int64_t n) {
+  Sum q = g;
+  oob_expert_sum_t &p = q.p;
+  p.T = g.p.T - t < n ? g.p.T - t : n, p.place += t * p.k;
+  if (p.weights) p.weights += t * p.k;
+  if (p.residual) p.residual = (const E *)p.residual + t * p.residual_stride;
+  if (p.out) p.out = (E *)p.out + t * p.out_stride;
+  if (q.dout) q.dout = (const E *)q.dout + t * q.ld_dout;
+  if (q.dweights) q.dweights += t * p.k;
+  return q;
 }
-template <class E> void sum_grad(const Sum &g, hipStream_t st) {
-  int64_t per = 256 / g.width;
-  k_sum_grad<E><<<(unsigned)((g.p.T + per - 1) / per), 256, 0, st>>>(g);
+template <class E> void sum(const Sum &all, hipStream_t st) {
+  int64_t per = 256 / all.width, n = per << 23;
+  for (int64_t t = 0; t < all.p.T; t += n) {
+    Sum g = part_of<E>(all, t, n);
+    dim3 grid((unsigned)((g.p.T + per - 1) / per), (unsigned)((g.p.C + g.width * 8 - 1) / (g.width * 8)));
+    k_sum<E><<<grid, 256, 0, st>>>(g);
+  }
+}
+template <class E> void sum_grad(const Sum &all, hipStream_t st) {
+  int64_t per = 256 / all.width, n = per << 23;
+  for (int64_t t = 0; t < all.p.T; t += n) {
+    Sum g = part_of<E>(all, t, n);
+    k_sum_grad<E><<<(unsigned)((g.p.T + per - 1) / per), 256, 0, st>>>(g);
+  }
 }
 
 }  // namespace

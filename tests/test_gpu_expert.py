@@ -691,6 +691,33 @@ def test_far_rows_of_logits_sums_and_tensors(P):
     assert float(l[0, 0]) == float(l[-1, -1]) == 0.5 and bool((l == 0.5).all())
 
 
+def test_tokens_of_more_than_one_launch(P):
+    T = (1 << 28) + 5  # eight lanes each
+    l = torch.zeros(T, 8, dtype=torch.bfloat16, device="cuda")  # noqa: E741
+    l[-40:] = rand(40, 8)
+    last = l[-40:].clone()
+    experts, w = P.route(l, 8)
+    want = P.route(last, 8)
+    assert torch.equal(experts[-40:], want[0]) and torch.equal(w[-40:], want[1])
+    assert experts[:: 1 << 20][:-1].tolist() == [list(range(8))] * 256 and bool((w[:: 1 << 20][:-1] == 0.125).all())
+    dw = torch.zeros_like(w)
+    dw[-40:] = rand(40, 8, t=torch.float32)
+    d = P.route_backward(dw, l, experts)
+    assert torch.equal(d[-40:], P.route_backward(dw[-40:].clone(), last, want[0])) and not d[:-40].any()
+    del l, experts, w, dw, d
+    T = (1 << 23) + 9  # a workgroup each
+    y, weights = rand(4, 1032), torch.ones(T, 1, device="cuda")
+    place = torch.zeros(T, 1, dtype=torch.int32, device="cuda")
+    place[-40:, 0] = torch.arange(40, device="cuda", dtype=torch.int32) % 4
+    weights[-40:] = rand(40, 1, t=torch.float32)
+    res = y[:1].expand(T, 1032).contiguous()
+    out = P.expert_sum(y, place, weights, residual=res)
+    assert torch.equal(out[-40:], P.expert_sum(y, place[-40:].clone(), weights[-40:].clone(), residual=res[-40:].clone())) and torch.equal(out[:: 1 << 15][:-1], (2 * res)[:: 1 << 15][:-1])
+    dweights = P.expert_sum_backward(out, y, place, weights, need=("weights",))[1]
+    want = P.expert_sum_backward(out[-40:].clone(), y, place[-40:].clone(), weights[-40:].clone(), need=("weights",))[1]
+    assert torch.equal(dweights[-40:], want) and bool((dweights[:-40] == dweights[0]).all())
+
+
 def test_linear_tokens_that_32_bit_offsets_do_not_reach(P):
     T, E, N, K = 1 << 18, 2, 16, 64
     wide = torch.zeros(T, 4104, dtype=torch.bfloat16, device="cuda")  # rows 8208 bytes apart: 2.15 GB
