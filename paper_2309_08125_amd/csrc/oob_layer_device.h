@@ -145,5 +145,18 @@ struct Arena {
 
 static inline bool multiple(const void *p, size_t of) { return (uintptr_t)p % of == 0; }
 
+/* Rows in memory, columns and pitch in bytes. */
+struct Lies { const void *p; int64_t rows, cols, ld; };
+/* Whether two share bytes; columns of one matrix do not. */
+static inline bool share(const Lies &a, const Lies &b) {
+  if (!a.rows || !b.rows) return false;
+  uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
+  if (a0 + (a.rows - 1) * a.ld + a.cols <= b0 || b0 + (b.rows - 1) * b.ld + b.cols <= a0) return false;
+  if (a.ld != b.ld || a.rows == 1 || b.rows == 1) return true;
+  int64_t gap = (int64_t)(b0 - a0) % a.ld;
+  if (gap < 0) gap += a.ld;
+  return gap < a.cols || gap + b.cols > a.ld;
+}
+
 }  // namespace layer
 #endif

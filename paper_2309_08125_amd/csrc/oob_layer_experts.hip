@@ -643,6 +643,11 @@ bool launches_fit(const oob_expert_linear_t *p, bool forward) {
          ((w_loadable(p) ? 0 : p->E * p->N) + (x_lies ? 0 : p->R)) * (up(p->K, 8) / 8) < ((int64_t)1 << 32) - 512;
 }
 
+/* Where matrices lie; an expert's after the other: one long row. */
+Lies lies(const void *p, int64_t rows, int64_t cols, int64_t ld) { return {p, rows, cols * 2, ld * 2}; }
+Lies lies_w(const oob_expert_linear_t *p) { return lies(p->w, p->w ? 1 : 0, (p->E - 1) * p->expert_stride + (p->N - 1) * p->w_stride + p->K, 0); }
+Lies lies_x(const oob_expert_linear_t *p) { return lies(p->x, p->x ? p->T : 0, p->K, p->x_stride); }
+
 struct Forward { Operand a, b; Packed x, w; float *rest; };
 Forward plan(const oob_expert_linear_t *p, Arena &w) {
   Forward f{{p->x, p->x_stride, 0}, {}, {}, {}, nullptr};
@@ -756,6 +761,8 @@ extern "C" int oob_expert_linear(const oob_expert_linear_t *p, void *workspace, 
   if (!multiple(workspace, 256)) return OOB_EINVAL;
   size_t need = forward_bytes(p);
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
+  for (Lies y : {lies(p->y, p->R, p->N, p->y_stride), lies(p->z, p->z ? p->R : 0, p->N, p->z_stride)})
+    if (share(y, lies_x(p)) || share(y, lies_w(p)) || share(y, lies(p->bias, p->bias ? 1 : 0, p->E * p->N, 0))) return OOB_EINVAL;
   Arena w{(char *)workspace, bytes, 0};
   return p->dtype == OOB_BF16 ? forward<bf16>(p, w, (hipStream_t)stream) : forward<fp16>(p, w, (hipStream_t)stream);
 }
@@ -773,6 +780,10 @@ extern "C" int oob_expert_linear_backward(const oob_expert_linear_t *p, const oo
   if (!multiple(p->offsets, 4) || !multiple(p->rows, 4) || !multiple(workspace, 256)) return OOB_EINVAL;
   size_t need = backward_bytes(p, g);
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
+  Lies dx = lies(g->dx, g->dx ? p->R : 0, p->K, g->dx_stride);
+  if (share(dx, lies(g->dy, p->R, p->N, g->dy_stride)) || share(dx, lies(p->z, p->z && p->act != OOB_ACT_NONE ? p->R : 0, p->N, p->z_stride)) || share(dx, lies_w(p)) ||
+      (g->dw && share(dx, lies_x(p))))
+    return OOB_EINVAL;
   Arena w{(char *)workspace, bytes, 0};
   return p->dtype == OOB_BF16 ? backward<bf16>(p, g, w, (hipStream_t)stream) : backward<fp16>(p, g, w, (hipStream_t)stream);
 }

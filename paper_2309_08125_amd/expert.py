@@ -70,11 +70,12 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _enqueue(name, at, *args, size=None):
-    """Enqueues a call on the current stream of GPU number `at`, with a workspace where it takes one (size: what that goes by)."""
+def _enqueue(name, at, *args, size=None, out=None, read=()):
+    """Enqueues a call on the current stream of GPU number `at`, with a workspace where it takes one (size: what that goes by); out: the
+    caller's tensor that the call writes to and refuses where it shares memory with those that it reads."""
     if at != torch._C._cuda_getDevice():
         with torch.cuda.device(at):
-            return _enqueue(name, at, *args, size=size)
+            return _enqueue(name, at, *args, size=size, out=out, read=read)
     stream = layer._stream(at)
     if size is None:
         rc = _calls[name](*args, stream)
@@ -84,7 +85,26 @@ def _enqueue(name, at, *args, size=None):
         ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
         rc = _calls[name](*args, ws.data_ptr() if nbytes else None, nbytes, stream)
     if rc:
+        if out is not None and not all([t is None or _apart(out, t) for t in read]):
+            raise ValueError("out: it shares memory with what the call reads")
         binding.check(rc, name)
+
+
+def _part(t):
+    """Where a tensor lies: first byte, end, and of rows (all but its last axis) their pitch and length in bytes."""
+    size, at, n = t.element_size(), t.data_ptr(), t.shape
+    span = sum((c - 1) * s for c, s in zip(n, t.stride())) + 1 if t.numel() else 0
+    return at, at + span * size, t.stride(0) * size if t.dim() == 2 and n[0] > 1 else 0, n[-1] * size
+
+
+def _apart(a, b):
+    """Whether two tensors share no memory; columns of one matrix of rows do not."""
+    a0, a1, pitch, wide = _part(a)
+    b0, b1, other, long = _part(b)
+    if a1 <= b0 or b1 <= a0:
+        return True
+    gap = (b0 - a0) % pitch if pitch and pitch == other else 0
+    return gap >= wide and gap + long <= pitch
 
 
 def _numbers(t, shape, like, name):
@@ -220,7 +240,7 @@ def expert_linear(x, w, offsets, bias=None, rows=None, act="none", keep=False, o
     activation (z is None without one).  No autograd graph is built: gradients are expert_linear_backward's."""
     _load()
     args = _linear_args(x, w, offsets, rows, act)
-    y = x.new_empty((args.R, args.N)) if out is None else _out(out, args.R, args.N, x, "out", x, w, bias)
+    y = x.new_empty((args.R, args.N)) if out is None else _out(out, args.R, args.N, x, "out")
     z = x.new_empty((args.R, args.N)) if keep and args.act else None
     if bias is not None:
         if not (bias.dtype is x.dtype and bias.get_device() == x.get_device() and bias.shape == (args.E, args.N) and bias.is_contiguous()):
@@ -228,36 +248,17 @@ def expert_linear(x, w, offsets, bias=None, rows=None, act="none", keep=False, o
         args.bias = bias.data_ptr()
     args.y, args.y_stride, args.z, args.z_stride = y.data_ptr(), _stride(y), _ptr(z), args.N
     ref = C.byref(args)
-    _enqueue("oob_expert_linear", x.get_device(), ref, size=("oob_expert_linear_workspace_size", ref))
+    _enqueue("oob_expert_linear", x.get_device(), ref, size=("oob_expert_linear_workspace_size", ref), out=out, read=(x, w, bias))
     return (y, z) if keep else y
 
 
-def _part(t):
-    """Where a tensor lies: first byte, end, and of rows (all but its last axis) their pitch and length in bytes."""
-    size, at, n = t.element_size(), t.data_ptr(), t.shape
-    span = sum((c - 1) * s for c, s in zip(n, t.stride())) + 1 if t.numel() else 0
-    return at, at + span * size, t.stride(0) * size if t.dim() == 2 and n[0] > 1 else 0, n[-1] * size
-
-
-def _apart(a, b):
-    """Whether two tensors share no memory; columns of one matrix of rows do not."""
-    a0, a1, pitch, wide = _part(a)
-    b0, b1, other, long = _part(b)
-    if a1 <= b0 or b1 <= a0:
-        return True
-    gap = (b0 - a0) % pitch if pitch and pitch == other else 0
-    return gap >= wide and gap + long <= pitch
-
-
-def _out(t, R, cols, like, name, *read):
-    """A matrix to write to; no two of its rows may share memory, and it may share none with what is read."""
+def _out(t, R, cols, like, name):
+    """A matrix to write to; no two of its rows may share memory."""
     if not (t.dim() == 2 and t.shape[0] == R):
         raise ValueError(f"{name}: [{R}, {cols}] is wanted")
     t = _rows(t, cols, like, name)
     if not (R <= 1 or t.stride(0) >= cols):
         raise ValueError(f"{name}: its rows overlap")
-    if not all([v is None or _apart(t, v) for v in read]):
-        raise ValueError(f"{name}: it shares memory with what the call reads")
     return t
 
 
@@ -283,12 +284,13 @@ def expert_linear_backward(dy, x, w, offsets, z=None, rows=None, act="none", nee
         args.z, args.z_stride = z2.data_ptr(), _stride(z2)
     dx = None
     if "x" in need:
-        dx = x.new_empty((args.R, args.K)) if out is None else _out(out, args.R, args.K, x, "out", dy2, x, w, z)
+        dx = x.new_empty((args.R, args.K)) if out is None else _out(out, args.R, args.K, x, "out")
     dw = x.new_empty((args.E, args.N, args.K)) if "w" in need else None
     db = x.new_empty((args.E, args.N)) if "b" in need else None
     grad = oob_expert_linear_grad(dy2.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db), _stride(dy2), args.K if dx is None else _stride(dx))
     refs = C.byref(args), C.byref(grad)
-    _enqueue("oob_expert_linear_backward", x.get_device(), *refs, size=("oob_expert_linear_backward_workspace_size", *refs))
+    _enqueue("oob_expert_linear_backward", x.get_device(), *refs, size=("oob_expert_linear_backward_workspace_size", *refs), out=out,
+             read=(dy2, x, w, z))
     return dx, dw, db
 
 
@@ -338,10 +340,10 @@ def expert_sum_backward(dout, y, place, weights=None, need=("y", "weights"), out
     d = _rows(dout, args.C, y, "dout")
     dy = None
     if "y" in need:
-        dy = y.new_empty((args.R, args.C)) if out is None else _out(out, args.R, args.C, y, "out", y, d)
+        dy = y.new_empty((args.R, args.C)) if out is None else _out(out, args.R, args.C, y, "out")
     dweights = y.new_empty(place.shape, dtype=torch.float32) if "weights" in need else None
     _enqueue("oob_expert_sum_backward", y.get_device(), C.byref(args), d.data_ptr(), _stride(d), _ptr(dy), args.C if dy is None else _stride(dy),
-             _ptr(dweights))
+             _ptr(dweights), out=out, read=(y, d))
     return dy, dweights
 
 

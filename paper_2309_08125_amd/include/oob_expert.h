@@ -71,7 +71,7 @@ int oob_expert_rows(const int32_t *experts, int64_t n, int first, int E, int32_t
  * Row r of expert e, offsets[e] <= r < offsets[e + 1]:  z[r] = x[token(r)] w[e]^T + bias[e];  y[r] = act(z[r]).
  * token(r) = rows[r] / per where rows is given (x [T][K], R = T per), r itself otherwise (x [R][K]).  Rows of y and z that
  * are no expert's stay as they are.  Offsets out of 0 .. R are taken as the nearest of these, a run that ends before it begins as empty; a row
- * whose token is out of 0 .. T-1 is one of zeros.  Rows that offsets give to two experts are undefined (nothing outside the arrays is touched). */
+ * whose token is out of 0 .. T-1 is one of zeros.  y and z share no memory with what is read (OOB_EINVAL).  Rows that offsets give to two experts are undefined (nothing outside the arrays is touched). */
 typedef struct oob_expert_linear_t {
   int dtype, act;          /* OOB_BF16 or OOB_FP16; OOB_ACT_* */
   int E, per;              /* experts, at most OOB_EXPERT_MAX; pairs of a token (rows NULL: 1) */
@@ -87,7 +87,7 @@ int oob_expert_linear(const oob_expert_linear_t *p, void *workspace, size_t byte
 
 /* dz = dy act'(z);  dx[r] = dz[r] w[e] (a row of x's gradient each: oob_expert_sum without weights adds those of a token);
  * dw[e] = sum of dz[r]^T x[token(r)], db[e] = sum of dz[r] over the rows of e, 0 where it has none.  dx, dw, db: each may be NULL.
- * Reads p's sizes, offsets, rows, x, w and z. */
+ * Reads p's sizes, offsets, rows, x, w and z; dx shares no memory with what is read (OOB_EINVAL). */
 typedef struct oob_expert_linear_grad {
   const void *dy;          /* [R][N] */
   void *dx, *dw, *db;      /* [R][K], [E][N][K] contiguous, [E][N] */
@@ -113,7 +113,8 @@ typedef struct oob_expert_sum_t {
 int oob_expert_sum(const oob_expert_sum_t *p, void *stream);
 
 /* dy[place[t][j]] = weights[t][j] dout[t];  dweights[t][j] = dout[t] . y[place[t][j]], 0 where the place is out of 0 .. R-1.  Rows of
- * dy that are nobody's stay as they are; no two places may be the same.  dy, dweights: one may be NULL.  The residual's gradient is dout. */
+ * dy that are nobody's stay as they are; no two places may be the same.  dy, dweights: one may be NULL; dy shares no
+ * memory with what is read (OOB_EINVAL).  The residual's gradient is dout. */
 int oob_expert_sum_backward(const oob_expert_sum_t *p, const void *dout, int64_t dout_stride, void *dy, int64_t dy_stride, float *dweights,
                             void *stream);
 

@@ -149,3 +149,17 @@ def test_clip_refuses():
     for given, shares in ((FAKE - 4, 0), (FAKE, 1), (FAKE + 196, 1), (FAKE + 200, 0), (FAKE + 8192 + 196, 1), (FAKE + 8192 + 200, 0)):
         assert overlap(ptr, given) == shares
         assert not shares or scale(given=given, out=0) == P.OOB_EINVAL
+
+
+def test_results_on_what_is_read_are_refused():
+    """Of the calls that are refused nothing is enqueued; those that would be let through are not made here."""
+    at = lambda i: FAKE + i * (1 << 16)  # noqa: E731
+    apart = dict(LINEAR, x=at(0), w=at(1), bias=at(2), y=at(3), z=at(4), z_stride=LINEAR["y_stride"])
+    run = lambda **kw: lib().oob_expert_linear(C.byref(make(X.oob_expert_linear_t, **{**apart, **kw})), None, 0, None)  # noqa: E731
+    w = 2 * (2 * LINEAR["expert_stride"] + (LINEAR["N"] - 1) * LINEAR["w_stride"] + LINEAR["K"])  # bytes of three matrices
+    for kw in (dict(y=at(0)), dict(z=at(0)), dict(y=at(0) + 2), dict(y=at(1)), dict(y=at(1) + w - 2), dict(z=at(2)), dict(y=at(2) + 2 * 3 * LINEAR["N"] - 2)):
+        assert run(**kw) == P.OOB_EINVAL, kw
+    back = lambda dx, **kw: lib().oob_expert_linear_backward(  # noqa: E731
+        C.byref(make(X.oob_expert_linear_t, **{**apart, **kw})), C.byref(X.oob_expert_linear_grad(at(5), dx, at(6), None, LINEAR["N"], LINEAR["K"])), FAKE, 1 << 40, None)
+    for kw in (dict(dx=at(5)), dict(dx=at(1)), dict(dx=at(0) + 2), dict(dx=at(4), act=4)):
+        assert back(**kw) == P.OOB_EINVAL, kw
