@@ -6,7 +6,7 @@ namespace layer {
 namespace {
 
 /* A token takes `width` threads of a workgroup (a power of two), eight columns each at a time, eight choices' rows on their way together.  Memory bounds it: 4096
- * tokens, 8 choices, 4096 columns, bfloat16: 78 us (335 MB, 4.3 TB/s), the gradients 122 us (570 MB, 4.7 TB/s). */
+ * tokens, 8 choices, 4096 columns, bfloat16: 83 us (335 MB, 4.0 TB/s, behind the writes of what ran before), the gradients 107 us (570 MB, 5.3 TB/s). */
 struct Sum {
   oob_expert_sum_t p;
   int width;
@@ -17,17 +17,28 @@ struct Sum {
 };
 constexpr int TOGETHER = 8; /* rows of y that are on their way at once */
 
-/* Place and weight of a choice; -1: it has no part. */
-__device__ inline int64_t place_of(const oob_expert_sum_t &p, int64_t t, int j, float &w) {
-  int64_t r = j < p.k ? p.place[t * p.k + j] : -1;
-  if (r < 0 || r >= p.R) r = -1;
-  w = r < 0 ? 0.f : p.weights ? p.weights[t * p.k + j] : 1.f;
-  return r;
+/* WAVE: a wave has one token (rows of more than 256 values), and what goes by the token and its choices lies in scalar registers: the gradients take 69 vector
+ * registers, seven waves a SIMD, and 107 us; 147, three and 122 otherwise. */
+template <bool WAVE> __device__ inline int64_t token_of(const Sum &g) {
+  int in = threadIdx.x / g.width;
+  return (int64_t)blockIdx.x * (256 / g.width) + (WAVE ? uniform(in) : in);
+}
+/* Places and weights of choices from number j0 on; a place below 0 has no part.  All are asked for before the first is waited for. */
+template <bool WAVE> __device__ __forceinline__ void places_of(const oob_expert_sum_t &p, int64_t t, int j0, int (&r)[TOGETHER], float (&w)[TOGETHER]) {
+#pragma unroll
+  for (int j = 0; j < TOGETHER; j++) r[j] = j0 + j < p.k ? p.place[t * p.k + j0 + j] : -1;
+#pragma unroll
+  for (int j = 0; j < TOGETHER; j++) w[j] = j0 + j >= p.k ? 0.f : p.weights ? p.weights[t * p.k + j0 + j] : 1.f;
+#pragma unroll
+  for (int j = 0; j < TOGETHER; j++) {
+    if (WAVE) r[j] = uniform(r[j]), w[j] = __uint_as_float(uniform(__float_as_uint(w[j])));
+    if (r[j] >= p.R) r[j] = -1;
+  }
 }
 
-template <class E> __global__ __launch_bounds__(256) void k_sum(Sum g) {
+template <class E, bool WAVE> __global__ __launch_bounds__(256) void k_sum(Sum g) {
   const oob_expert_sum_t &p = g.p;
-  int64_t t = (int64_t)blockIdx.x * (256 / g.width) + threadIdx.x / g.width;
+  int64_t t = token_of<WAVE>(g);
   int64_t c = ((int64_t)blockIdx.y * g.width + threadIdx.x % g.width) * 8, left = p.C - c;
   if (t >= p.T || left <= 0) return;
   float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -36,12 +47,11 @@ template <class E> __global__ __launch_bounds__(256) void k_sum(Sum g) {
   for (int j0 = 0; j0 < p.k; j0 += TOGETHER) {
     typename Vec<E>::v8 y[TOGETHER];
     float w[TOGETHER];
-    int64_t r[TOGETHER];
+    int r[TOGETHER];
+    places_of<WAVE>(p, t, j0, r, w);
 #pragma unroll
-    for (int j = 0; j < TOGETHER; j++) {
-      r[j] = place_of(p, t, j0 + j, w[j]);
+    for (int j = 0; j < TOGETHER; j++)
       if (r[j] >= 0) y[j] = load8<E>((const E *)p.y + r[j] * p.y_stride + c, left);
-    }
 #pragma unroll
     for (int j = 0; j < TOGETHER; j++)
       if (r[j] >= 0)
@@ -53,39 +63,43 @@ template <class E> __global__ __launch_bounds__(256) void k_sum(Sum g) {
 }
 
 /* dy[place] = w dout, dweights = dout . y[place]: a token's row of dout is read once for every TOGETHER choices. */
-template <class E> __global__ __launch_bounds__(256) void k_sum_grad(Sum g) {
+template <class E, bool WAVE> __global__ __launch_bounds__(256) void k_sum_grad(Sum g) {
   __shared__ float part[4][TOGETHER];
   const oob_expert_sum_t &p = g.p;
-  int64_t t = (int64_t)blockIdx.x * (256 / g.width) + threadIdx.x / g.width;
+  int64_t t = token_of<WAVE>(g);
   bool live = t < p.T;
   int at = threadIdx.x % g.width;
   for (int j0 = 0; j0 < p.k; j0 += TOGETHER) {
     float w[TOGETHER], dot[TOGETHER];
-    int64_t r[TOGETHER];
+    int r[TOGETHER];
 #pragma unroll
-    for (int j = 0; j < TOGETHER; j++) {
-      dot[j] = 0, r[j] = -1;
-      if (live) r[j] = place_of(p, t, j0 + j, w[j]);
-    }
-    for (int64_t c = (int64_t)at * 8; live && c < p.C; c += g.width * 8) {
-      int64_t left = p.C - c;
+    for (int j = 0; j < TOGETHER; j++) dot[j] = 0, r[j] = -1;
+    if (live) places_of<WAVE>(p, t, j0, r, w);
+    auto columns = [&](int64_t c, int64_t left) __attribute__((always_inline)) {
       typename Vec<E>::v8 y[TOGETHER], d = load8<E>((const E *)g.dout + t * g.ld_dout + c, left);
       if (g.dweights)
 #pragma unroll
         for (int j = 0; j < TOGETHER; j++)
           if (r[j] >= 0) y[j] = load8<E>((const E *)p.y + r[j] * p.y_stride + c, left);
+      if (g.dy)
 #pragma unroll
-      for (int j = 0; j < TOGETHER; j++) {
-        if (r[j] < 0) continue;
-        if (g.dweights)
-          for (int e = 0; e < 8; e++) dot[j] += e < left ? (float)d[e] * (float)y[j][e] : 0.f;
-        if (g.dy) {
+        for (int j = 0; j < TOGETHER; j++) {
+          if (r[j] < 0) continue;
           typename Vec<E>::v8 out;
           for (int e = 0; e < 8; e++) out[e] = (E)(w[j] * (float)d[e]);
           store8<E>((E *)g.dy + r[j] * g.ld_dy + c, out, left);
         }
+      if (g.dweights)
+#pragma unroll
+        for (int j = 0; j < TOGETHER; j++)
+          if (r[j] >= 0)
+            for (int e = 0; e < 8; e++) dot[j] += (float)d[e] * (float)y[j][e]; /* past the row: zeros */
+    };
+    if (live)
+      for (int64_t c = (int64_t)at * 8; c < p.C; c += g.width * 8) {
+        if (p.C - c >= 8) columns(c, 8);
+        else columns(c, p.C - c);
       }
-    }
     if (!g.dweights) continue;
     int run = g.width < 64 ? g.width : 64;
 #pragma unroll
@@ -94,12 +108,14 @@ template <class E> __global__ __launch_bounds__(256) void k_sum_grad(Sum g) {
     if (g.width > 64) { /* the sums of a token's waves, in their order */
       __syncthreads();
       if (lane() == 0)
+#pragma unroll
         for (int j = 0; j < TOGETHER; j++) part[threadIdx.x / 64][j] = dot[j];
       __syncthreads();
       if (at == 0)
-        for (int j = 0; j < TOGETHER; j++) {
-          dot[j] = part[threadIdx.x / 64][j];
-          for (int wave = 1; wave < g.width / 64; wave++) dot[j] += part[threadIdx.x / 64 + wave][j];
+#pragma unroll
+        for (int j = 0; j < TOGETHER; j++) { /* width is 128 or 256 */
+          dot[j] = part[threadIdx.x / 64][j] + part[threadIdx.x / 64 + 1][j];
+          if (g.width > 128) dot[j] += part[2][j], dot[j] += part[3][j];
         }
     }
     if (live && at == 0)
@@ -146,14 +162,17 @@ template <class E> void sum(const Sum &all, hipStream_t st) {
   for (int64_t t = 0; t < all.p.T; t += n) {
     Sum g = part_of<E>(all, t, n);
     dim3 grid((unsigned)((g.p.T + per - 1) / per), (unsigned)((g.p.C + g.width * 8 - 1) / (g.width * 8)));
-    k_sum<E><<<grid, 256, 0, st>>>(g);
+    if (g.width >= 64) k_sum<E, true><<<grid, 256, 0, st>>>(g);
+    else k_sum<E, false><<<grid, 256, 0, st>>>(g);
   }
 }
 template <class E> void sum_grad(const Sum &all, hipStream_t st) {
   int64_t per = 256 / all.width, n = per << 23;
   for (int64_t t = 0; t < all.p.T; t += n) {
     Sum g = part_of<E>(all, t, n);
-    k_sum_grad<E><<<(unsigned)((g.p.T + per - 1) / per), 256, 0, st>>>(g);
+    unsigned groups = (unsigned)((g.p.T + per - 1) / per);
+    if (g.width >= 64) k_sum_grad<E, true><<<groups, 256, 0, st>>>(g);
+    else k_sum_grad<E, false><<<groups, 256, 0, st>>>(g);
   }
 }
 
