@@ -465,10 +465,10 @@ struct Packed {
 /* Two matrices in one launch, w and x: the first takes workgroups below `first`. */
 struct Packs { Packed p[2]; int64_t first; };
 
-__global__ __launch_bounds__(256) void k_pack_rows(Packs packs) {
-  const bool second = (int64_t)blockIdx.x >= packs.first;
+template <int THREADS> __device__ __forceinline__ void pack_rows(const Packs &packs, int64_t group) {
+  const bool second = group >= packs.first;
   const Packed &p = packs.p[second];
-  int64_t per = p.ld_to / 8, id = ((int64_t)blockIdx.x - (second ? packs.first : 0)) * 256 + threadIdx.x, r = id / per, c = id % per * 8;
+  int64_t per = p.ld_to / 8, id = (group - (second ? packs.first : 0)) * THREADS + threadIdx.x, r = id / per, c = id % per * 8;
   if (p.offsets) {
     int end = 0;
     for (int e = lane(); e <= p.E; e += 64) end = max(end, p.offsets[e]);
@@ -487,6 +487,7 @@ __global__ __launch_bounds__(256) void k_pack_rows(Packs packs) {
   if (at >= 0) v = __builtin_bit_cast(i16x8, load8<fp16>((const fp16 *)p.from + at + c, p.cols - c));
   *(i16x8 *)(p.to + r * p.ld_to + c) = v;
 }
+__global__ __launch_bounds__(256) void k_pack_rows(Packs packs) { pack_rows<256>(packs, blockIdx.x); }
 
 /* ---- dz = dy act'(z) and the sums of its columns, runs of an expert's rows -------------------------------------------------- */
 struct ActGrad {
@@ -535,6 +536,58 @@ template <class E, int ACT> __global__ __launch_bounds__(256) void k_experts_act
   }
 }
 
+/* Few rows in all: an expert's 64 columns to a workgroup of 16 waves, 128 rows of them at a time, twice over on their way; its sums are db, and nothing is
+ * joined in a launch of its own; copies of w and x go along.  1206 rows, 7 experts, 1021 columns, float16, with copies of 15 MB: 12.9 us; 23.1 in three launches.
+ * 2048 rows, 8 experts, 1024 columns, without copies: 4.9 us evenly divided, 17.2 where one has all; 8.7 and 16.9 in two launches (8192 rows: 11.2 and 61 against 16.0 and 50). */
+constexpr int64_t FEW_ROWS = 2048;
+constexpr int FEW_THREADS = 1024;
+template <class E, int ACT> __global__ __launch_bounds__(FEW_THREADS) void k_experts_act_few(ActGrad g, E *db, Packs packs) {
+  constexpr int DEEP = 2, AT_ONCE = FEW_THREADS / 8, WAVES = FEW_THREADS / 64;
+  __shared__ float part[WAVES][64];
+  const int across = (int)((g.N + 63) / 64), e = blockIdx.x / across, at = threadIdx.x % 8 * 8;
+  if (e >= g.d.E) {
+    pack_rows<FEW_THREADS>(packs, blockIdx.x - across * g.d.E);
+    return;
+  }
+  const int64_t n0 = (int64_t)(blockIdx.x % across) * 64;
+  int64_t first, rows = rows_of(g.d, e, first), n = n0 + at, left = g.N - n;
+  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  const int64_t stop = left > 0 ? first + rows : 0;
+  for (int64_t t0 = first + threadIdx.x / 8; t0 < stop; t0 += AT_ONCE * DEEP) {
+    typename Vec<E>::v8 d[DEEP], z[DEEP], out;
+#pragma unroll
+    for (int u = 0; u < DEEP; u++)
+      if (t0 + AT_ONCE * u < stop) {
+        d[u] = load8<E>((const E *)g.dy + (t0 + AT_ONCE * u) * g.ld_dy + n, left);
+        if (ACT != OOB_ACT_NONE) z[u] = load8<E>((const E *)g.z + (t0 + AT_ONCE * u) * g.ld_z + n, left);
+      }
+#pragma unroll
+    for (int u = 0; u < DEEP; u++) {
+      if (t0 + AT_ONCE * u >= stop) continue;
+      for (int i = 0; i < 8; i++) {
+        float v = (float)d[u][i] * (ACT == OOB_ACT_NONE ? 1.f : slope((float)z[u][i], ACT));
+        out[i] = (E)v; /* as above */
+        sum[i] += v;
+      }
+      if (g.dz) store8<E>((E *)g.dz + (t0 + AT_ONCE * u) * g.ld_dz + n, out, 8);
+    }
+  }
+  if (!db) return;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    for (int o = 8; o < 64; o *= 2) sum[i] += __shfl_xor(sum[i], o);
+    if (lane() < 8) part[threadIdx.x / 64][at + i] = sum[i];
+  }
+  __syncthreads();
+  n = n0 + threadIdx.x;
+  if (threadIdx.x < 64 && n < g.N) {
+    float all = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; w++) all += part[w][threadIdx.x];
+    db[e * g.N + n] = (E)all;
+  }
+}
+
 /* db[e]: the sums of the expert's runs, in their order. */
 template <class E> __global__ __launch_bounds__(256) void k_experts_db(ActGrad g, E *out) {
   __shared__ float part[4][64];
@@ -561,10 +614,11 @@ bool x_loadable(const oob_expert_linear_t *p) {
   return loadable(p->x, p->x_stride, p->K) && (!p->rows || p->T * p->x_stride < (int64_t)1 << 30);
 }
 
-int64_t groups_of(const Packed &k) { return (k.n * (k.ld_to / 8) + 255) / 256; }
+int64_t groups_of(const Packed &k, int threads) { return (k.n * (k.ld_to / 8) + threads - 1) / threads; }
+Packs both(const Packed &a, const Packed &b, int threads) { return {{a, b}, groups_of(a, threads)}; }
 void pack(const Packed &a, const Packed &b, hipStream_t st) {
-  int64_t first = groups_of(a), n = first + groups_of(b);
-  if (n) k_pack_rows<<<(unsigned)n, 256, 0, st>>>(Packs{{a, b}, first});
+  int64_t n = groups_of(a, 256) + groups_of(b, 256);
+  if (n) k_pack_rows<<<(unsigned)n, 256, 0, st>>>(both(a, b, 256));
 }
 /* As the products take them, in the workspace where they have to be copied: `how` says so then (n is 0 otherwise). */
 Operand plan_w(const oob_expert_linear_t *p, Arena &w, Packed &how) {
@@ -680,11 +734,13 @@ int run_rows(const oob_expert_linear_t *p) { /* about 1024 workgroups, 16 rows a
 }
 size_t sums_bytes(const oob_expert_linear_t *p) { return (size_t)row_tiles(p->R, p->E, run_rows(p)) * p->N * 4; }
 
+bool few_rows(const oob_expert_linear_t *p) { return p->R <= FEW_ROWS && tiles(p->N, 64) * p->E + ((int64_t)p->E * p->N + p->R) * (up(p->K, 8) / 8) / FEW_THREADS < 1 << 21; }
+
 struct Backward { Operand dz, w, x; Packed how_w, how_x; float *sums, *rest; };
 Backward plan(const oob_expert_linear_t *p, const oob_expert_linear_grad *g, Arena &w) {
   Backward b{{g->dy, g->dy_stride, 0}, {}, {}, {}, {}, nullptr, nullptr};
   if (makes_dz(p, g)) b.dz = {w.take((size_t)p->R * up(p->N, 8) * 2), up(p->N, 8), 0};
-  if (g->db) b.sums = (float *)w.take(sums_bytes(p));
+  if (g->db && !few_rows(p)) b.sums = (float *)w.take(sums_bytes(p));
   if (g->dx) {
     b.w = plan_w(p, w, b.how_w);
     size_t rest = rest_bytes(p->R, p->E, p->K, p->N);
@@ -698,7 +754,13 @@ template <class E> int backward(const oob_expert_linear_t *p, const oob_expert_l
   bool makes = makes_dz(p, g);
   Backward b = plan(p, g, w);
   if (!w.ok()) return OOB_ECAPACITY;
-  if (p->R) pack(b.how_w, b.how_x, st);
+  const bool few = few_rows(p);
+  if (!p->R) b.how_w = b.how_x = Packed{};
+  if (!few || !(makes || g->db)) { /* otherwise with dz, in one launch */
+    pack(b.how_w, b.how_x, st);
+    b.how_w = b.how_x = Packed{};
+  }
+  const Packs packs = both(b.how_w, b.how_x, FEW_THREADS);
   Operand dz = b.dz;
   float *sums = b.sums;
   Division d{p->offsets, p->E, p->R};
@@ -707,14 +769,20 @@ template <class E> int backward(const oob_expert_linear_t *p, const oob_expert_l
     a.d = d, a.dy = g->dy, a.ld_dy = g->dy_stride, a.z = p->z, a.ld_z = p->z_stride, a.N = p->N, a.sums = sums, a.rows = run_rows(p), a.runs = row_tiles(p->R, p->E, a.rows);
     a.dz = makes ? const_cast<void *>(dz.p) : nullptr, a.ld_dz = dz.ld;
     dim3 grid((unsigned)tiles(p->N, 512), (unsigned)a.runs);
-    if (p->R) switch (p->act) {
-      case OOB_ACT_RELU: k_experts_act<E, OOB_ACT_RELU><<<grid, 256, 0, st>>>(a); break;
-      case OOB_ACT_GELU: k_experts_act<E, OOB_ACT_GELU><<<grid, 256, 0, st>>>(a); break;
-      case OOB_ACT_GELU_TANH: k_experts_act<E, OOB_ACT_GELU_TANH><<<grid, 256, 0, st>>>(a); break;
-      case OOB_ACT_SILU: k_experts_act<E, OOB_ACT_SILU><<<grid, 256, 0, st>>>(a); break;
-      default: k_experts_act<E, OOB_ACT_NONE><<<grid, 256, 0, st>>>(a);
+    if (few) grid = dim3((unsigned)(tiles(p->N, 64) * p->E + packs.first + groups_of(b.how_x, FEW_THREADS)));
+#define OOB_ACT_GRAD(ACT)                                                          \
+  if (few) k_experts_act_few<E, ACT><<<grid, FEW_THREADS, 0, st>>>(a, (E *)g->db, packs);  \
+  else k_experts_act<E, ACT><<<grid, 256, 0, st>>>(a);                             \
+  break
+    if (few || p->R) switch (p->act) {
+      case OOB_ACT_RELU: OOB_ACT_GRAD(OOB_ACT_RELU);
+      case OOB_ACT_GELU: OOB_ACT_GRAD(OOB_ACT_GELU);
+      case OOB_ACT_GELU_TANH: OOB_ACT_GRAD(OOB_ACT_GELU_TANH);
+      case OOB_ACT_SILU: OOB_ACT_GRAD(OOB_ACT_SILU);
+      default: OOB_ACT_GRAD(OOB_ACT_NONE);
     }
-    if (g->db) k_experts_db<E><<<dim3((unsigned)tiles(p->N, 64), p->E), 256, 0, st>>>(a, (E *)g->db);
+#undef OOB_ACT_GRAD
+    if (g->db && !few) k_experts_db<E><<<dim3((unsigned)tiles(p->N, 64), p->E), 256, 0, st>>>(a, (E *)g->db);
   }
   int rc = hipGetLastError() == hipSuccess ? OOB_OK : OOB_EHIP;
   Experts x{};

@@ -335,6 +335,13 @@ def test_linear_shares_and_skewed_divisions(P):
     linear_case(P, 2, 1, 1000, 16, 24, "gelu", torch.bfloat16)
 
 
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("T,k,E,N,skew", [(2047, 1, 3, 65, 0.0), (2048, 1, 2, 64, 1.0), (2049, 1, 3, 63, 0.0), (1500, 3, 7, 520, 20.0)])
+def test_linear_gradients_on_both_sides_of_few_rows(P, T, k, E, N, skew, act):
+    linear_case(P, T, k, E, N, 24, act, torch.bfloat16, skew=skew)
+    linear_case(P, T, k, E, N, 24, act, torch.float16, gather=False, skew=skew, need=("b",))
+
+
 def test_linear_strides_and_parts(P):
     for at in (0, 1):
         linear_case(P, 90, 2, 3, 48, 40, "gelu", torch.float16, view=lambda a: strided(a, 8, at))
