@@ -157,6 +157,8 @@ static inline bool share(const Lies &a, const Lies &b) {
   if (gap < 0) gap += a.ld;
   return gap < a.cols || gap + b.cols > a.ld;
 }
+/* An array without rows. */
+static inline Lies lies_flat(const void *p, int64_t bytes) { return {p, p && bytes ? 1 : 0, bytes, 0}; }
 
 }  // namespace layer
 #endif

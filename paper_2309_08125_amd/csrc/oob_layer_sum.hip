@@ -138,6 +138,14 @@ bool sum_ok(const oob_expert_sum_t *p, bool forward) {
   return p->out && p->out_stride >= p->C && multiple(p->out, of);
 }
 
+/* The result on memory that other workgroups still read. */
+bool out_shared(const oob_expert_sum_t *p) {
+  const int64_t of = p->dtype == OOB_FP32 ? 4 : 2, cols = p->C * of, n = p->T * p->k * 4;
+  Lies out{p->out, p->T, cols, p->out_stride * of}, res{p->residual, p->residual ? p->T : 0, cols, p->residual_stride * of};
+  bool in_place = p->out == p->residual && (p->out_stride == p->residual_stride || p->T == 1);
+  return share(out, {p->y, p->R, cols, p->y_stride * of}) || share(out, lies_flat(p->place, n)) || share(out, lies_flat(p->weights, n)) || (!in_place && share(out, res));
+}
+
 /* Threads of a token: those that its columns need, up to a workgroup. */
 int width_of(int64_t C) {
   int w = 1;
@@ -184,6 +192,7 @@ using namespace layer;
 extern "C" int oob_expert_sum(const oob_expert_sum_t *p, void *stream) {
   if (!sum_ok(p, true)) return OOB_EINVAL;
   if (p->T == 0) return OOB_OK;
+  if (out_shared(p)) return OOB_EINVAL;
   Sum g{};
   g.p = *p, g.width = width_of(p->C);
   if ((p->C + g.width * 8 - 1) / (g.width * 8) > 65535) return OOB_EINVAL; /* rows of 2^27 values */

@@ -98,7 +98,8 @@ size_t oob_expert_linear_backward_workspace_size(const oob_expert_linear_t *p, c
 int oob_expert_linear_backward(const oob_expert_linear_t *p, const oob_expert_linear_grad *g, void *workspace, size_t bytes, void *stream);
 
 /* ---- a token's results summed ----------------------------------------------------------------------
- * out[t] = residual[t] + sum over j < k of weights[t][j] y[place[t][j]], in the order of j; a place out of 0 .. R-1 has no part. */
+ * out[t] = residual[t] + sum over j < k of weights[t][j] y[place[t][j]], in the order of j; a place out of 0 .. R-1 has no part.  out shares no
+ * memory with what is read (OOB_EINVAL), but may be the residual in its place. */
 typedef struct oob_expert_sum_t {
   int dtype, k;            /* OOB_BF16, OOB_FP16, OOB_FP32; 1 <= k <= OOB_EXPERT_MAX_CHOICES */
   int64_t T, R, C;         /* each below 2^31, C >= 1 */
