@@ -701,6 +701,10 @@ bool launches_fit(const oob_expert_linear_t *p, bool forward) {
 Lies lies(const void *p, int64_t rows, int64_t cols, int64_t ld) { return {p, rows, cols * 2, ld * 2}; }
 Lies lies_w(const oob_expert_linear_t *p) { return lies(p->w, p->w ? 1 : 0, (p->E - 1) * p->expert_stride + (p->N - 1) * p->w_stride + p->K, 0); }
 Lies lies_x(const oob_expert_linear_t *p) { return lies(p->x, p->x ? p->T : 0, p->K, p->x_stride); }
+/* Offsets and rows are read by every workgroup, whenever it runs. */
+bool on_numbers(const Lies &to, const oob_expert_linear_t *p) {
+  return share(to, lies_flat(p->offsets, (p->E + 1) * 4)) || share(to, lies_flat(p->rows, p->R * 4));
+}
 
 struct Forward { Operand a, b; Packed x, w; float *rest; };
 Forward plan(const oob_expert_linear_t *p, Arena &w) {
@@ -829,8 +833,10 @@ extern "C" int oob_expert_linear(const oob_expert_linear_t *p, void *workspace, 
   if (!multiple(workspace, 256)) return OOB_EINVAL;
   size_t need = forward_bytes(p);
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
-  for (Lies y : {lies(p->y, p->R, p->N, p->y_stride), lies(p->z, p->z ? p->R : 0, p->N, p->z_stride)})
-    if (share(y, lies_x(p)) || share(y, lies_w(p)) || share(y, lies(p->bias, p->bias ? 1 : 0, p->E * p->N, 0))) return OOB_EINVAL;
+  Lies y = lies(p->y, p->R, p->N, p->y_stride), z = lies(p->z, p->z ? p->R : 0, p->N, p->z_stride);
+  for (Lies to : {y, z})
+    if (share(to, lies_x(p)) || share(to, lies_w(p)) || share(to, lies_flat(p->bias, (int64_t)p->E * p->N * 2)) || on_numbers(to, p)) return OOB_EINVAL;
+  if (share(y, z)) return OOB_EINVAL;
   Arena w{(char *)workspace, bytes, 0};
   return p->dtype == OOB_BF16 ? forward<bf16>(p, w, (hipStream_t)stream) : forward<fp16>(p, w, (hipStream_t)stream);
 }

@@ -235,7 +235,7 @@ def expert_linear(x, w, offsets, bias=None, rows=None, act="none", keep=False, o
     """Row r of expert e, offsets[e] <= r < offsets[e + 1]: y[r] = act(x[token] w[e]^T + bias[e]).
 
     x [T, K] with rows [R] of expert_rows: row r is that of token rows[r] // (R // T); or x [R, K], in order already (rows None).  w [E, N,
-    K], bias [E, N]; bfloat16 or float16, rows of any stride.  y [R, N], or `out`, which shares no memory with x, w and bias; rows that are no expert's stay as they are (in a
+    K], bias [E, N]; bfloat16 or float16, rows of any stride.  y [R, N], or `out`, which shares no memory with what is read; rows that are no expert's stay as they are (in a
     new y: whatever memory held).  keep=True: (y, z) with z = x w^T + bias, which the backward pass wants where there is an
     activation (z is None without one).  No autograd graph is built: gradients are expert_linear_backward's."""
     _load()
@@ -248,7 +248,7 @@ def expert_linear(x, w, offsets, bias=None, rows=None, act="none", keep=False, o
         args.bias = bias.data_ptr()
     args.y, args.y_stride, args.z, args.z_stride = y.data_ptr(), _stride(y), _ptr(z), args.N
     ref = C.byref(args)
-    _enqueue("oob_expert_linear", x.get_device(), ref, size=("oob_expert_linear_workspace_size", ref), out=out, read=(x, w, bias))
+    _enqueue("oob_expert_linear", x.get_device(), ref, size=("oob_expert_linear_workspace_size", ref), out=out, read=(x, w, bias, offsets, rows))
     return (y, z) if keep else y
 
 

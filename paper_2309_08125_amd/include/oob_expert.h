@@ -71,7 +71,7 @@ int oob_expert_rows(const int32_t *experts, int64_t n, int first, int E, int32_t
  * Row r of expert e, offsets[e] <= r < offsets[e + 1]:  z[r] = x[token(r)] w[e]^T + bias[e];  y[r] = act(z[r]).
  * token(r) = rows[r] / per where rows is given (x [T][K], R = T per), r itself otherwise (x [R][K]).  Rows of y and z that
  * are no expert's stay as they are.  Offsets out of 0 .. R are taken as the nearest of these, a run that ends before it begins as empty; a row
- * whose token is out of 0 .. T-1 is one of zeros.  y and z share no memory with what is read (OOB_EINVAL).  Rows that offsets give to two experts are undefined (nothing outside the arrays is touched). */
+ * whose token is out of 0 .. T-1 is one of zeros.  y and z share no memory with what is read (offsets and rows too) or with one another (OOB_EINVAL).  Rows that offsets give to two experts are undefined (nothing outside the arrays is touched). */
 typedef struct oob_expert_linear_t {
   int dtype, act;          /* OOB_BF16 or OOB_FP16; OOB_ACT_* */
   int E, per;              /* experts, at most OOB_EXPERT_MAX; pairs of a token (rows NULL: 1) */

@@ -29,3 +29,17 @@ def test_sum_on_what_it_reads():
                dict(out=at(1)), dict(out=at(1) + 28), dict(out=at(2) - 100), dict(out=at(2) + 28),  # places, weights
                dict(out=at(3), out_stride=17), dict(out=at(3), residual_stride=17), dict(out=at(3) + 2), dict(out=at(3) - 32)):  # the residual, not in its place
         assert call(**kw) == P.OOB_EINVAL, kw
+
+
+LINEAR = dict(dtype=0, act=0, E=3, per=2, R=8, T=4, N=16, K=8, offsets=at(0), rows=at(1), x=at(2), w=at(3), bias=at(4), y=at(5), z=at(6), x_stride=8, w_stride=8,
+              expert_stride=128, y_stride=16, z_stride=16)
+
+
+def test_products_on_what_they_read():
+    call = lambda **kw: X._load().oob_expert_linear(C.byref(make(X.oob_expert_linear_t, **{**LINEAR, **kw})), None, 0, None)  # noqa: E731
+    for name in ("y", "z"):
+        for first, size in ((at(0), 16), (at(1), 32)):  # offsets, rows: later tiles read them too
+            for where in (first, first + size - 2, first - 8 * 32 + 2):
+                assert call(**{name: where}) == P.OOB_EINVAL, (name, where - BASE)
+    for kw in (dict(y=at(6)), dict(y=at(6) + 30), dict(y=at(6) + 32, y_stride=24), dict(z=at(5) + 8 * 32 - 2)):  # one another
+        assert call(**kw) == P.OOB_EINVAL, kw
