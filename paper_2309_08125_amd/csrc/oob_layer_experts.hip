@@ -686,7 +686,7 @@ bool sizes_ok(const oob_expert_linear_t *p) {
   const int64_t most = (int64_t)1 << 31;
   return p && (p->dtype == OOB_BF16 || p->dtype == OOB_FP16) && p->act >= 0 && p->act < OOB_ACTS && p->E >= 1 && p->E <= OOB_EXPERT_MAX &&
          p->per >= 1 && p->R >= 0 && p->T >= 0 && p->N >= 1 && p->K >= 1 && p->R < most && p->T < most && p->N < (1 << 21) && p->K < (1 << 21) &&
-         (p->rows ? p->T * p->per == p->R : p->per == 1);
+         p->T * p->per == p->R && (p->rows || p->per == 1);
 }
 bool fits(int64_t tiles) { return tiles < (int64_t)1 << 31; }
 /* Numbers of the smallest tiles, which are 32-bit; threads of the copies, 2^32 at most. */

@@ -43,3 +43,14 @@ def test_products_on_what_they_read():
                 assert call(**{name: where}) == P.OOB_EINVAL, (name, where - BASE)
     for kw in (dict(y=at(6)), dict(y=at(6) + 30), dict(y=at(6) + 32, y_stride=24), dict(z=at(5) + 8 * 32 - 2)):  # one another
         assert call(**kw) == P.OOB_EINVAL, kw
+
+
+def test_products_in_order_have_as_many_tokens_as_rows():
+    """Without rows x is [R][K]: a smaller T would leave the end of x out of what results are held against."""
+    in_order = dict(LINEAR, rows=0, per=1)
+    for T in (0, 4, 7, 9):
+        p = make(X.oob_expert_linear_t, **{**in_order, "T": T, "y": at(2) + 7 * 16})  # on the last row of x
+        assert X._load().oob_expert_linear(C.byref(p), None, 0, None) == P.OOB_EINVAL, T
+        g = X.oob_expert_linear_grad(at(7), at(2) + 7 * 16, at(8), 0, 16, 8)
+        assert X._load().oob_expert_linear_backward(C.byref(p), C.byref(g), at(9), 1 << 40, None) == P.OOB_EINVAL, T
+        assert X._load().oob_expert_linear_workspace_size(C.byref(p)) == 0
