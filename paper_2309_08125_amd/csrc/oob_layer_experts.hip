@@ -854,10 +854,11 @@ extern "C" int oob_expert_linear_backward(const oob_expert_linear_t *p, const oo
   if (!multiple(p->offsets, 4) || !multiple(p->rows, 4) || !multiple(workspace, 256)) return OOB_EINVAL;
   size_t need = backward_bytes(p, g);
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
-  Lies dx = lies(g->dx, g->dx ? p->R : 0, p->K, g->dx_stride);
-  if (share(dx, lies(g->dy, p->R, p->N, g->dy_stride)) || share(dx, lies(p->z, p->z && p->act != OOB_ACT_NONE ? p->R : 0, p->N, p->z_stride)) || share(dx, lies_w(p)) ||
-      (g->dw && share(dx, lies_x(p))))
-    return OOB_EINVAL;
+  Lies dx = lies(g->dx, g->dx ? p->R : 0, p->K, g->dx_stride), dw = lies_flat(g->dw, p->E * p->N * p->K * 2), db = lies_flat(g->db, p->E * p->N * 2);
+  Lies dy = lies(g->dy, p->R, p->N, g->dy_stride), z = lies(p->z, p->z && p->act != OOB_ACT_NONE ? p->R : 0, p->N, p->z_stride);
+  for (Lies to : {dx, dw, db})
+    if (share(to, dy) || share(to, z) || (g->dx && share(to, lies_w(p))) || (g->dw && share(to, lies_x(p))) || on_numbers(to, p)) return OOB_EINVAL;
+  if (share(dx, dw) || share(dx, db) || share(dw, db)) return OOB_EINVAL;
   Arena w{(char *)workspace, bytes, 0};
   return p->dtype == OOB_BF16 ? backward<bf16>(p, g, w, (hipStream_t)stream) : backward<fp16>(p, g, w, (hipStream_t)stream);
 }

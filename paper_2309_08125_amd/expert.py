@@ -290,7 +290,7 @@ def expert_linear_backward(dy, x, w, offsets, z=None, rows=None, act="none", nee
     grad = oob_expert_linear_grad(dy2.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db), _stride(dy2), args.K if dx is None else _stride(dx))
     refs = C.byref(args), C.byref(grad)
     _enqueue("oob_expert_linear_backward", x.get_device(), *refs, size=("oob_expert_linear_backward_workspace_size", *refs), out=out,
-             read=(dy2, x, w, z))
+             read=(dy2, x, w, z, offsets, rows))
     return dx, dw, db
 
 

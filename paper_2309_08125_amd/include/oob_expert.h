@@ -87,7 +87,7 @@ int oob_expert_linear(const oob_expert_linear_t *p, void *workspace, size_t byte
 
 /* dz = dy act'(z);  dx[r] = dz[r] w[e] (a row of x's gradient each: oob_expert_sum without weights adds those of a token);
  * dw[e] = sum of dz[r]^T x[token(r)], db[e] = sum of dz[r] over the rows of e, 0 where it has none.  dx, dw, db: each may be NULL.
- * Reads p's sizes, offsets, rows, x, w and z; dx shares no memory with what is read (OOB_EINVAL). */
+ * Reads p's sizes, offsets, rows, x (for dw), w (for dx) and z; dx, dw and db share no memory with what is read or with one another (OOB_EINVAL). */
 typedef struct oob_expert_linear_grad {
   const void *dy;          /* [R][N] */
   void *dx, *dw, *db;      /* [R][K], [E][N][K] contiguous, [E][N] */

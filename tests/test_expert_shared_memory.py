@@ -54,3 +54,21 @@ def test_products_in_order_have_as_many_tokens_as_rows():
         g = X.oob_expert_linear_grad(at(7), at(2) + 7 * 16, at(8), 0, 16, 8)
         assert X._load().oob_expert_linear_backward(C.byref(p), C.byref(g), at(9), 1 << 40, None) == P.OOB_EINVAL, T
         assert X._load().oob_expert_linear_workspace_size(C.byref(p)) == 0
+
+
+def test_gradients_of_products_on_what_is_read_and_on_one_another():
+    grad = dict(dy=at(7), dx=at(8), dw=at(9), db=at(10), dy_stride=16, dx_stride=8)
+
+    def call(p=(), **kw):
+        q = make(X.oob_expert_linear_t, **{**LINEAR, "act": 4, **dict(p)})
+        return X._load().oob_expert_linear_backward(C.byref(q), C.byref(make(X.oob_expert_linear_grad, **{**grad, **kw})), at(11), 1 << 40, None)
+
+    sizes = {at(7): 8 * 32, at(6): 8 * 32, at(3): 3 * 256, at(2): 4 * 16, at(0): 16, at(1): 32}  # dy, z, w, x, offsets, rows
+    results = dict(dx=8 * 16, dw=3 * 256, db=3 * 32)
+    for name, mine in results.items():
+        for first, size in sizes.items():
+            for where in (first, first + size - 2, first - mine + 2):
+                assert call(**{name: where}) == P.OOB_EINVAL, (name, where - BASE)
+        for other in results.keys() - {name}:
+            for where in (grad[other], grad[other] + results[other] - 2):
+                assert call(**{name: where}) == P.OOB_EINVAL, (name, other)
