@@ -210,8 +210,13 @@ extern "C" int oob_expert_sum_backward(const oob_expert_sum_t *p, const void *do
   size_t of = p->dtype == OOB_FP32 ? 4 : 2;
   if (!dout || dout_stride < p->C || !multiple(dout, of) || (!dy && !dweights)) return OOB_EINVAL;
   if ((dy && (dy_stride < p->C || !multiple(dy, of))) || !multiple(dweights, 4)) return OOB_EINVAL;
-  Lies to{dy, dy ? p->R : 0, p->C * (int64_t)of, dy_stride * (int64_t)of};
-  if (share(to, {dout, p->T, to.cols, dout_stride * (int64_t)of}) || share(to, {p->y, p->R, to.cols, p->y_stride * (int64_t)of})) return OOB_EINVAL;
+  const int64_t cols = p->C * (int64_t)of, n = p->T * p->k * 4;
+  Lies rows{dy, dy ? p->R : 0, cols, dy_stride * (int64_t)of}, dots = lies_flat(dweights, n);
+  for (Lies to : {rows, dots})
+    if (share(to, {dout, p->T, cols, dout_stride * (int64_t)of}) || share(to, {p->y, p->R, cols, p->y_stride * (int64_t)of}) || share(to, lies_flat(p->place, n)) ||
+        share(to, lies_flat(p->weights, n)))
+      return OOB_EINVAL;
+  if (share(rows, dots)) return OOB_EINVAL;
   Sum g{*p, width_of(p->C), dout, dy, dout_stride, dy_stride, dweights};
   hipStream_t st = (hipStream_t)stream;
   if (p->dtype == OOB_BF16) sum_grad<bf16>(g, st);

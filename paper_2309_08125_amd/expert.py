@@ -327,7 +327,7 @@ def expert_sum(y, place, weights=None, residual=None):
 
 def expert_sum_backward(dout, y, place, weights=None, need=("y", "weights"), out=None):
     """(dy, dweights) of expert_sum: dy[place[t, j]] = weights[t, j] dout[t], dweights[t, j] = dout[t] . y[place[t, j]] (0 where the
-    place is out of range); None for what `need` does not name.  out: where dy goes, apart from y and dout; rows that are nobody's stay as they are.  No two
+    place is out of range); None for what `need` does not name.  out: where dy goes, no memory that the call reads; rows that are nobody's stay as they are.  No two
     places may be the same (expert_rows makes such).  The residual's gradient is dout."""
     _load()
     args = _sum_args(y, place, weights)
@@ -343,7 +343,7 @@ def expert_sum_backward(dout, y, place, weights=None, need=("y", "weights"), out
         dy = y.new_empty((args.R, args.C)) if out is None else _out(out, args.R, args.C, y, "out")
     dweights = y.new_empty(place.shape, dtype=torch.float32) if "weights" in need else None
     _enqueue("oob_expert_sum_backward", y.get_device(), C.byref(args), d.data_ptr(), _stride(d), _ptr(dy), args.C if dy is None else _stride(dy),
-             _ptr(dweights), out=out, read=(y, d))
+             _ptr(dweights), out=out, read=(y, d, place, weights))
     return dy, dweights
 
 

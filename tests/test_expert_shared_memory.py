@@ -72,3 +72,12 @@ def test_gradients_of_products_on_what_is_read_and_on_one_another():
         for other in results.keys() - {name}:
             for where in (grad[other], grad[other] + results[other] - 2):
                 assert call(**{name: where}) == P.OOB_EINVAL, (name, other)
+
+
+def test_gradients_of_sums_on_what_is_read_and_on_one_another():
+    p = make(X.oob_expert_sum_t, **SUM)
+    call = lambda dy=at(6), dw=at(7): X._load().oob_expert_sum_backward(C.byref(p), at(5), 16, dy, 16, dw, None)  # noqa: E731
+    for first, size in ((at(0), 8 * 32), (at(1), 32), (at(2), 32), (at(5), 4 * 32)):  # y, places, weights, dout
+        for where in (first, first + size - 4, first - 28):
+            assert call(dy=where) == call(dw=where) == P.OOB_EINVAL, where - BASE
+    assert call(dw=at(6)) == call(dw=at(6) + 8 * 32 - 4) == call(dy=at(7) - 8 * 32 + 2) == P.OOB_EINVAL
