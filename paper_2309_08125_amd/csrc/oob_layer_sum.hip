@@ -213,7 +213,7 @@ extern "C" int oob_expert_sum_backward(const oob_expert_sum_t *p, const void *do
   const int64_t cols = p->C * (int64_t)of, n = p->T * p->k * 4;
   Lies rows{dy, dy ? p->R : 0, cols, dy_stride * (int64_t)of}, dots = lies_flat(dweights, n);
   for (Lies to : {rows, dots})
-    if (share(to, {dout, p->T, cols, dout_stride * (int64_t)of}) || share(to, {p->y, p->R, cols, p->y_stride * (int64_t)of}) || share(to, lies_flat(p->place, n)) ||
+    if (share(to, {dout, p->T, cols, dout_stride * (int64_t)of}) || (dweights && share(to, {p->y, p->R, cols, p->y_stride * (int64_t)of})) || share(to, lies_flat(p->place, n)) ||
         share(to, lies_flat(p->weights, n)))
       return OOB_EINVAL;
   if (share(rows, dots)) return OOB_EINVAL;

@@ -115,7 +115,7 @@ int oob_expert_sum(const oob_expert_sum_t *p, void *stream);
 
 /* dy[place[t][j]] = weights[t][j] dout[t];  dweights[t][j] = dout[t] . y[place[t][j]], 0 where the place is out of 0 .. R-1.  Rows of
  * dy that are nobody's stay as they are; no two places may be the same.  dy, dweights: one may be NULL; neither shares
- * memory with what is read or with the other (OOB_EINVAL).  The residual's gradient is dout. */
+ * memory with what is read (y for dweights alone) or with the other (OOB_EINVAL).  The residual's gradient is dout. */
 int oob_expert_sum_backward(const oob_expert_sum_t *p, const void *dout, int64_t dout_stride, void *dy, int64_t dy_stride, float *dweights,
                             void *stream);
 
