@@ -154,6 +154,13 @@ bool overlap(int n, const void *const *from, const void *const *to, const int64_
   return true;
 }
 
+/* The norm is written while other workgroups still read and write the tensors. */
+bool norm_shared(int n, const void *const *from, const int64_t *sizes, const int *types, const float *norm) {
+  for (int i = 0; i < n; i++)
+    if (share({norm, 1, 4, 0}, lies_flat(from[i], sizes[i] * (types[i] == OOB_FP32 ? 4 : 2)))) return true;
+  return false;
+}
+
 /* The next launch's tensors from number `at` on: those with values, as many as fit. */
 template <int N> bool next(int &at, int n, const void *const *from, void *const *to, const int64_t *sizes, const int *types, Tensors<N> &t) {
   int64_t chunks = 0;
@@ -237,6 +244,7 @@ extern "C" int oob_clip_scale(int n, const void *const *from, void *const *to, c
   if (!multiple(given, 4) || !multiple(norm, 4) || (!given && !norm) || overlap(n, from, to, sizes, types, given)) return OOB_EINVAL;
   size_t need = n && !given ? oob_clip_workspace_size(n, sizes) : 0;
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
+  if (!given && (norm_shared(n, from, sizes, types, norm) || norm_shared(n, to, sizes, types, norm))) return OOB_EINVAL;
   hipStream_t st = (hipStream_t)stream;
   double *sums = (double *)workspace;
   int count = given ? 0 : first_pass(n, from, sizes, types, sums, st);

@@ -130,7 +130,8 @@ int oob_clip_norm(int n, const void *const *from, const int64_t *sizes, const in
 int oob_clip_overlap(int n, const void *const *from, const void *const *to, const int64_t *sizes, const int *types, const float *given);
 /* to[i] = from[i] factor, factor = max_norm / norm where norm > max_norm and finite, 1 otherwise.  to[i] may be from[i]: with a factor of
  * 1 nothing is written then.  given (float [1], on the device) is the norm if it is not NULL, one that several GPUs have added up, say; otherwise it is
- * that of oob_clip_norm, which is written to `norm`.  Where oob_clip_overlap is 1: OOB_EINVAL. */
+ * that of oob_clip_norm, which is written to `norm`.  Where oob_clip_overlap is 1, or `norm` lies on a
+ * tensor: OOB_EINVAL. */
 int oob_clip_scale(int n, const void *const *from, void *const *to, const int64_t *sizes, const int *types, float max_norm,
                    const float *given, float *norm, void *workspace, size_t bytes, void *stream);
 

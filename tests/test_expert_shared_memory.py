@@ -81,3 +81,14 @@ def test_gradients_of_sums_on_what_is_read_and_on_one_another():
         for where in (first, first + size - 4, first - 28):
             assert call(dy=where) == call(dw=where) == P.OOB_EINVAL, where - BASE
     assert call(dw=at(6)) == call(dw=at(6) + 8 * 32 - 4) == call(dy=at(7) - 8 * 32 + 2) == P.OOB_EINVAL
+
+
+def test_norm_on_tensors_that_are_scaled():
+    """The norm is written while other workgroups still read and write the tensors."""
+    n, sizes, types = 2, (C.c_int64 * 2)(100, 50), (C.c_int * 2)(0, 2)
+    arrays = lambda *a: (C.c_void_p * 2)(*a)  # noqa: E731
+    need = X._load().oob_clip_workspace_size(n, sizes)
+    for to in (arrays(at(0), at(1)), arrays(at(2), at(3))):
+        for first in (at(0), at(1), to[0], to[1]):
+            for where in (first, first + 196):
+                assert X._load().oob_clip_scale(n, arrays(at(0), at(1)), to, sizes, types, 1.0, None, where, at(4), need, None) == P.OOB_EINVAL, where - BASE
