@@ -697,9 +697,16 @@ bool launches_fit(const oob_expert_linear_t *p, bool forward) {
          ((w_loadable(p) ? 0 : p->E * p->N) + (x_lies ? 0 : p->R)) * (up(p->K, 8) / 8) < ((int64_t)1 << 32) - 512;
 }
 
-/* Where matrices lie; an expert's after the other: one long row. */
+/* Where matrices lie. */
 Lies lies(const void *p, int64_t rows, int64_t cols, int64_t ld) { return {p, rows, cols * 2, ld * 2}; }
-Lies lies_w(const oob_expert_linear_t *p) { return lies(p->w, p->w ? 1 : 0, (p->E - 1) * p->expert_stride + (p->N - 1) * p->w_stride + p->K, 0); }
+/* On an expert's matrix: between those of far-apart experts there is room for others. */
+bool on_w(const Lies &to, const oob_expert_linear_t *p) {
+  if (!share(to, lies_flat(p->w, 2 * ((p->E - 1) * p->expert_stride + (p->N - 1) * p->w_stride + p->K)))) return false;
+  if (p->expert_stride == p->N * p->w_stride) return share(to, lies(p->w, p->E * p->N, p->K, p->w_stride));
+  for (int e = 0; e < p->E; e++)
+    if (share(to, lies((const uint16_t *)p->w + e * p->expert_stride, p->N, p->K, p->w_stride))) return true;
+  return false;
+}
 Lies lies_x(const oob_expert_linear_t *p) { return lies(p->x, p->x ? p->T : 0, p->K, p->x_stride); }
 /* Offsets and rows are read by every workgroup, whenever it runs. */
 bool on_numbers(const Lies &to, const oob_expert_linear_t *p) {
@@ -835,7 +842,7 @@ extern "C" int oob_expert_linear(const oob_expert_linear_t *p, void *workspace, 
   if (need > bytes || (need && !workspace)) return OOB_ECAPACITY;
   Lies y = lies(p->y, p->R, p->N, p->y_stride), z = lies(p->z, p->z ? p->R : 0, p->N, p->z_stride);
   for (Lies to : {y, z})
-    if (share(to, lies_x(p)) || share(to, lies_w(p)) || share(to, lies_flat(p->bias, (int64_t)p->E * p->N * 2)) || on_numbers(to, p)) return OOB_EINVAL;
+    if (share(to, lies_x(p)) || on_w(to, p) || share(to, lies_flat(p->bias, (int64_t)p->E * p->N * 2)) || on_numbers(to, p)) return OOB_EINVAL;
   if (share(y, z)) return OOB_EINVAL;
   Arena w{(char *)workspace, bytes, 0};
   return p->dtype == OOB_BF16 ? forward<bf16>(p, w, (hipStream_t)stream) : forward<fp16>(p, w, (hipStream_t)stream);
@@ -857,7 +864,7 @@ extern "C" int oob_expert_linear_backward(const oob_expert_linear_t *p, const oo
   Lies dx = lies(g->dx, g->dx ? p->R : 0, p->K, g->dx_stride), dw = lies_flat(g->dw, p->E * p->N * p->K * 2), db = lies_flat(g->db, p->E * p->N * 2);
   Lies dy = lies(g->dy, p->R, p->N, g->dy_stride), z = lies(p->z, p->z && p->act != OOB_ACT_NONE ? p->R : 0, p->N, p->z_stride);
   for (Lies to : {dx, dw, db})
-    if (share(to, dy) || share(to, z) || (g->dx && share(to, lies_w(p))) || (g->dw && share(to, lies_x(p))) || on_numbers(to, p)) return OOB_EINVAL;
+    if (share(to, dy) || share(to, z) || (g->dx && on_w(to, p)) || (g->dw && share(to, lies_x(p))) || on_numbers(to, p)) return OOB_EINVAL;
   if (share(dx, dw) || share(dx, db) || share(dw, db)) return OOB_EINVAL;
   Arena w{(char *)workspace, bytes, 0};
   return p->dtype == OOB_BF16 ? backward<bf16>(p, g, w, (hipStream_t)stream) : backward<fp16>(p, g, w, (hipStream_t)stream);

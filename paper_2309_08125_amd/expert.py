@@ -85,7 +85,7 @@ def _enqueue(name, at, *args, size=None, out=None, read=()):
         ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
         rc = _calls[name](*args, ws.data_ptr() if nbytes else None, nbytes, stream)
     if rc:
-        if out is not None and not all([t is None or _apart(out, t) for t in read]):
+        if out is not None and not all([_apart(out, m) for t in read if t is not None for m in (t if t.dim() == 3 else (t,))]):
             raise ValueError("out: it shares memory with what the call reads")
         binding.check(rc, name)
 

@@ -48,3 +48,22 @@ def test_gradient_of_y_in_its_place(P):
     assert P.expert_sum_backward(d, y, place, w, need=("y",), out=y)[0] is y and torch.equal(y, want)
     with pytest.raises(ValueError, match="shares memory"):
         P.expert_sum_backward(d, y, place, w, out=y)
+
+
+# ---- results between the experts' matrices --------------------------------------------------------------------
+@pytest.mark.parametrize("T", [4, 3])
+def test_results_between_matrices_far_apart(P, T):
+    """Matrices with room between them: what lies in the room shares nothing with them."""
+    wide = rand(3, 40, 16)
+    w, room = wide[:, :24], wide[1, 24:].reshape(-1)
+    x, offsets = rand(T, 16), ints(0, 1, 1, T)
+    before = w.clone()
+    out = room[8: 8 + T * 24].view(T, 24)
+    y = P.expert_linear(x, w, offsets)
+    assert P.expert_linear(x, w, offsets, out=out) is out and torch.equal(out, y) and torch.equal(w, before)
+    out = room[8: 8 + T * 16].view(T, 16)
+    dx = P.expert_linear_backward(y, x, w, offsets, need=("x",))[0]
+    assert torch.equal(P.expert_linear_backward(y, x, w, offsets, need=("x",), out=out)[0], dx) and torch.equal(w, before)
+    for bad in (wide.view(-1)[16 * 23: 16 * 23 + T * 24].view(T, 24), wide.view(-1)[16 * 40 - T * 24 + 1: 16 * 40 + 1].view(T, 24)):
+        with pytest.raises(ValueError, match="shares memory"):
+            P.expert_linear(x, w, offsets, out=bad)
