@@ -145,6 +145,9 @@ struct Arena {
 
 static inline bool multiple(const void *p, size_t of) { return (uintptr_t)p % of == 0; }
 
+/* Rows that are read: `cols` apart at least, or all of them one (stride 0). */
+static inline bool readable(int64_t stride, int64_t cols) { return stride >= cols || stride == 0; }
+
 /* Rows in memory, columns and pitch in bytes. */
 struct Lies { const void *p; int64_t rows, cols, ld; };
 /* Whether two share bytes; columns of one matrix do not. */

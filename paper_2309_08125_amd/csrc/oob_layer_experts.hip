@@ -834,7 +834,7 @@ extern "C" size_t oob_expert_linear_workspace_size(const oob_expert_linear_t *p)
 extern "C" int oob_expert_linear(const oob_expert_linear_t *p, void *workspace, size_t bytes, void *stream) {
   if (!sizes_ok(p) || !launches_fit(p, true)) return OOB_EINVAL;
   if (p->R == 0) return OOB_OK;
-  if (!p->offsets || !p->x || !p->w || !p->y || p->x_stride < p->K || p->w_stride < p->K || p->y_stride < p->N || p->expert_stride < 0) return OOB_EINVAL;
+  if (!p->offsets || !p->x || !p->w || !p->y || !readable(p->x_stride, p->K) || p->w_stride < p->K || p->y_stride < p->N || p->expert_stride < 0) return OOB_EINVAL;
   if (p->z && p->z_stride < p->N) return OOB_EINVAL;
   if (!even(p->x) || !even(p->w) || !even(p->y) || !even(p->bias) || !even(p->z) || !multiple(p->offsets, 4) || !multiple(p->rows, 4)) return OOB_EINVAL;
   if (!multiple(workspace, 256)) return OOB_EINVAL;
@@ -854,9 +854,9 @@ extern "C" size_t oob_expert_linear_backward_workspace_size(const oob_expert_lin
 
 extern "C" int oob_expert_linear_backward(const oob_expert_linear_t *p, const oob_expert_linear_grad *g, void *workspace, size_t bytes, void *stream) {
   if (!sizes_ok(p) || !g || !launches_fit(p, false) || !p->offsets) return OOB_EINVAL;
-  if (p->R && (!g->dy || g->dy_stride < p->N || (p->act != OOB_ACT_NONE && (!p->z || p->z_stride < p->N)))) return OOB_EINVAL;
+  if (p->R && (!g->dy || !readable(g->dy_stride, p->N) || (p->act != OOB_ACT_NONE && (!p->z || p->z_stride < p->N)))) return OOB_EINVAL;
   if (p->R && g->dx && (!p->w || p->w_stride < p->K || p->expert_stride < 0 || g->dx_stride < p->K)) return OOB_EINVAL;
-  if (p->R && g->dw && (!p->x || p->x_stride < p->K)) return OOB_EINVAL;
+  if (p->R && g->dw && (!p->x || !readable(p->x_stride, p->K))) return OOB_EINVAL;
   if (!even(g->dy) || !even(p->x) || !even(p->w) || !even(p->z) || !even(g->dx) || !even(g->dw) || !even(g->db)) return OOB_EINVAL;
   if (!multiple(p->offsets, 4) || !multiple(p->rows, 4) || !multiple(workspace, 256)) return OOB_EINVAL;
   size_t need = backward_bytes(p, g);

@@ -388,7 +388,7 @@ bool route_ok(const oob_route *p, bool forward) {
   }
   if (p->T == 0) return true;
   size_t of = p->dtype == OOB_FP32 ? 4 : 2;
-  if (!p->logits || p->logits_stride < p->E || !p->experts || !multiple(p->logits, of) || !multiple(p->experts, 4)) return false;
+  if (!p->logits || !readable(p->logits_stride, p->E) || !p->experts || !multiple(p->logits, of) || !multiple(p->experts, 4)) return false;
   return !forward || (p->weights && multiple(p->weights, 4) && multiple(p->bias, 4));
 }
 

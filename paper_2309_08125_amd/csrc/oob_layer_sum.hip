@@ -132,9 +132,9 @@ bool sum_ok(const oob_expert_sum_t *p, bool forward) {
   if (p->T == 0) return true;
   size_t of = p->dtype == OOB_FP32 ? 4 : 2;
   if (!p->place || !multiple(p->place, 4) || !multiple(p->weights, 4)) return false;
-  if (p->R && (!p->y || p->y_stride < p->C || !multiple(p->y, of))) return false;
+  if (p->R && (!p->y || !readable(p->y_stride, p->C) || !multiple(p->y, of))) return false;
   if (!forward) return true;
-  if (p->residual && (p->residual_stride < p->C || !multiple(p->residual, of))) return false;
+  if (p->residual && (!readable(p->residual_stride, p->C) || !multiple(p->residual, of))) return false;
   return p->out && p->out_stride >= p->C && multiple(p->out, of);
 }
 
@@ -208,7 +208,7 @@ extern "C" int oob_expert_sum_backward(const oob_expert_sum_t *p, const void *do
   if (!sum_ok(p, false)) return OOB_EINVAL;
   if (p->T == 0) return OOB_OK;
   size_t of = p->dtype == OOB_FP32 ? 4 : 2;
-  if (!dout || dout_stride < p->C || !multiple(dout, of) || (!dy && !dweights)) return OOB_EINVAL;
+  if (!dout || !readable(dout_stride, p->C) || !multiple(dout, of) || (!dy && !dweights)) return OOB_EINVAL;
   if ((dy && (dy_stride < p->C || !multiple(dy, of))) || !multiple(dweights, 4)) return OOB_EINVAL;
   const int64_t cols = p->C * (int64_t)of, n = p->T * p->k * 4;
   Lies rows{dy, dy ? p->R : 0, cols, dy_stride * (int64_t)of}, dots = lies_flat(dweights, n);

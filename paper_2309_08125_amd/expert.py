@@ -139,7 +139,7 @@ def route(logits, k, score="softmax", bias=None, groups=1, keep_groups=None, gro
     """(experts, weights) of every token: the k experts with the largest score + bias, of equals the first, and scale times their
     scores (renormalize: their share of the k scores' sum).
 
-    logits [..., E] in bfloat16, float16 or float32, rows of any stride, E up to 1024; score: "softmax" or "sigmoid"; bias: float32 [E]
+    logits [..., E] in bfloat16, float16 or float32, rows of any stride that do not overlap or one for all (stride 0), E up to 1024; score: "softmax" or "sigmoid"; bias: float32 [E]
     or None, counts for the choice alone.  groups > 1: the experts are so many runs of neighbours, and only the keep_groups (all where None)
     take part whose group_best (1 or 2) largest add up to most.  An expert whose logit is -inf comes after all others and has score 0; a
     token that has no other gets weights 0.  experts int32 [..., k] in falling order, weights float32 [..., k].  No autograd graph
@@ -235,7 +235,7 @@ def expert_linear(x, w, offsets, bias=None, rows=None, act="none", keep=False, o
     """Row r of expert e, offsets[e] <= r < offsets[e + 1]: y[r] = act(x[token] w[e]^T + bias[e]).
 
     x [T, K] with rows [R] of expert_rows: row r is that of token rows[r] // (R // T); or x [R, K], in order already (rows None).  w [E, N,
-    K], bias [E, N]; bfloat16 or float16, rows of any stride.  y [R, N], or `out`, which shares no memory with what is read; rows that are no expert's stay as they are (in a
+    K], bias [E, N]; bfloat16 or float16, rows of any stride that do not overlap, of x also one for all (stride 0).  y [R, N], or `out`, which shares no memory with what is read; rows that are no expert's stay as they are (in a
     new y: whatever memory held).  keep=True: (y, z) with z = x w^T + bias, which the backward pass wants where there is an
     activation (z is None without one).  No autograd graph is built: gradients are expert_linear_backward's."""
     _load()
@@ -309,7 +309,7 @@ def _sum_args(y, place, weights):
 def expert_sum(y, place, weights=None, residual=None):
     """out[t] = residual[t] + sum over j of weights[t, j] y[place[t, j]], in the order of j.
 
-    y [R, C] in bfloat16, float16 or float32, rows of any stride; place int32 [..., k] of expert_rows (what is out of 0 .. R-1 has no part);
+    y [R, C] in bfloat16, float16 or float32, rows of any stride that do not overlap or one for all (stride 0), those of the residual too; place int32 [..., k] of expert_rows (what is out of 0 .. R-1 has no part);
     weights float32 like place, or None: 1; residual [..., C] or None.  The result is [..., C].  No autograd graph is built: gradients are
     expert_sum_backward's."""
     _load()

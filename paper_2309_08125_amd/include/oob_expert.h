@@ -8,7 +8,8 @@
  * operators with some of the experts, or some of their columns.  Run and timed, they give the profile of
  * a model with experts.  oob_clip_* take the norm over all gradients of a step, and scale them.
  *
- * Conventions, types and errors: as in oob_layer.h.  Arrays of numbers of experts, rows and places are
+ * Conventions, types and errors: as in oob_layer.h.  Strides of rows are at least a row's length; those of logits, x, dy, y (of a sum), residual and dout, which
+ * are only read, may be 0: one row for all.  Arrays of numbers of experts, rows and places are
  * int32.  What such an array holds out of range is never used as an address: each call says what it does
  * instead.
  */

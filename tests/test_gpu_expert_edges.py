@@ -39,6 +39,40 @@ def ints(*v):
     return torch.tensor(v, dtype=torch.int32, device="cuda")
 
 
+# ---- rows of stride 0: one row for all ------------------------------------------------------------------------
+@pytest.mark.parametrize("K,N", [(64, 48), (33, 47)])
+def test_linear_of_one_row_for_all(P, K, N):
+    T, k, E = 70, 2, 3
+    offsets, rows, _ = P.expert_rows(torch.randint(0, E, (T, k), dtype=torch.int32, device="cuda"), E)
+    w = rand(E, N, K)
+    for gather in (True, False):
+        x, dy = rand(1, K).expand(T if gather else T * k, K), rand(1, N).expand(T * k, N)
+        for act in ("none", "silu"):
+            kind = dict(rows=rows if gather else None, act=act)
+            (y, z), (want, _) = (P.expert_linear(a, w, offsets, keep=True, **kind) for a in (x, x.contiguous()))
+            assert torch.equal(y, want)
+            got, ref = (P.expert_linear_backward(d, a, w, offsets, z, **kind) for d, a in ((dy, x), (dy.contiguous(), x.contiguous())))
+            assert all(torch.equal(a, b) for a, b in zip(got, ref))
+
+
+def test_route_of_one_row_for_all(P):
+    l, dw = rand(1, 20).expand(9, 20), rand(9, 3, t=torch.float32)  # noqa: E741
+    experts, w = P.route(l, 3)
+    want = P.route(l.contiguous(), 3)
+    assert torch.equal(experts, want[0]) and torch.equal(w, want[1])
+    assert torch.equal(P.route_backward(dw, l, experts), P.route_backward(dw, l.contiguous(), experts))
+
+
+@pytest.mark.parametrize("C", [40, 37, 520])
+def test_sum_of_one_row_for_all(P, C):
+    place, w = torch.randperm(18, device="cuda").int().view(9, 2), rand(9, 2, t=torch.float32)
+    for t in ALL:
+        y, res, d = rand(1, C, t=t).expand(18, C), rand(1, C, t=t).expand(9, C), rand(1, C, t=t).expand(9, C)
+        assert torch.equal(P.expert_sum(y, place, w, residual=res), P.expert_sum(y.contiguous(), place, w, residual=res.contiguous()))
+        got, want = P.expert_sum_backward(d, y, place, w), P.expert_sum_backward(d.contiguous(), y.contiguous(), place, w)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 # ---- results in the place of what the call does not read --------------------------------------------------------
 def test_gradient_of_y_in_its_place(P):
     """Without the weights' gradient y is not read: its gradient may take its place."""
