@@ -108,9 +108,9 @@ template <class E> __device__ inline void scale(const E *from, E *to, int64_t si
 
 /* Each workgroup adds up the first pass's sums itself, in the same order, in place of a launch between the two. */
 template <int N> __global__ __launch_bounds__(256) void k_scale(Tensors<N> t, const double *sums, int n, float max_norm, const float *given, float *norm) {
-  double s = given ? (double)*given : sqrt(add_up(sums, n));
-  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)s;
-  float factor = s > max_norm && s < INFINITY ? (float)(max_norm / s) : 1.f;
+  float s = given ? *given : (float)sqrt(add_up(sums, n)); /* as it is returned: one that is given back does the same */
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = s;
+  float factor = s > max_norm && s < INFINITY ? (float)((double)max_norm / s) : 1.f;
   int chunks = t.until[t.n - 1];
   for (int c = chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) { /* from the end: what was read last is still in the last-level cache */
     int64_t first;

@@ -363,7 +363,7 @@ def _tensors(tensors, name):
 
 def gradient_norm(tensors):
     """The root of the sum of all squares of contiguous tensors (bfloat16, float16, float32, mixed) as a float32 scalar on their
-    device; squares are summed in 64 bits."""
+    device; squares are summed in 64 bits, and a norm that passes 32 bits is an infinity."""
     _load()
     tensors = list(tensors)
     n, at, ptrs, sizes, types = _tensors(tensors, "tensors")

@@ -122,7 +122,8 @@ int oob_expert_sum_backward(const oob_expert_sum_t *p, const void *dout, int64_t
 
 /* ---- the norm over many tensors, and clipping ------------------------------------------------------
  * The arrays below lie on the HOST and are read before the call returns: n tensors of sizes[i] values of types[i] (OOB_*), at from[i].
- * norm [1] (float, out): the root of the sum of all squares, squares summed in 64 bits. */
+ * norm [1] (float, out): the root of the sum of all squares, squares summed in 64 bits (an infinity where it
+ * passes 32 bits). */
 size_t oob_clip_workspace_size(int n, const int64_t *sizes);
 int oob_clip_norm(int n, const void *const *from, const int64_t *sizes, const int *types, float *norm, void *workspace, size_t bytes,
                   void *stream);

@@ -101,3 +101,30 @@ def test_results_between_matrices_far_apart(P, T):
     for bad in (wide.view(-1)[16 * 23: 16 * 23 + T * 24].view(T, 24), wide.view(-1)[16 * 40 - T * 24 + 1: 16 * 40 + 1].view(T, 24)):
         with pytest.raises(ValueError, match="shares memory"):
             P.expert_linear(x, w, offsets, out=bad)
+
+
+# ---- norm and clipping ----------------------------------------------------------------------------------------
+def test_clip_leaves_what_has_no_norm_in_32_bits(P):
+    """Finite values whose norm passes 32 bits: it is an infinity, and they are left as they are, with the norm given or not."""
+    for t in (torch.bfloat16, torch.float32):
+        g = torch.full((4,), 3e38, device="cuda", dtype=t)
+        before = g.clone()
+        assert P.gradient_norm([g]).item() == math.inf
+        assert P.clip_gradients([g], 1.0).item() == math.inf and torch.equal(g, before)
+        out = torch.zeros_like(g)
+        assert P.clip_gradients([g], 1.0, out=[out]).item() == math.inf and torch.equal(out, before)
+        P.clip_gradients([g], 1.0, norm=P.gradient_norm([g]))
+        assert torch.equal(g, before)
+
+
+def test_clip_goes_by_the_norm_that_it_returns(P):
+    """By its own norm or by the same one given: the same bits, at the bound too."""
+    for n in range(1, 200):
+        g = [rand(3 * n, t=torch.float32), rand(n, t=torch.bfloat16)]
+        norm = P.gradient_norm(g)
+        for bound in (0.37 * norm.item(), norm.item()):
+            a, b = [torch.zeros_like(v) for v in g], [torch.zeros_like(v) for v in g]
+            assert torch.equal(P.clip_gradients(g, bound, out=a), norm)
+            P.clip_gradients(g, bound, norm=norm, out=b)
+            assert all(torch.equal(u, v) for u, v in zip(a, b)), (n, bound)
+        assert all(torch.equal(u, v) for u, v in zip(a, g)), n
