@@ -89,7 +89,7 @@ __global__ __launch_bounds__(256) void k_norm(const double *sums, int n, float *
   if (threadIdx.x == 0) *norm = (float)s;
 }
 
-template <class E> __device__ inline void scale(const E *from, E *to, int64_t size, int64_t first, float factor) {
+template <class E, class F> __device__ inline void scale(const E *from, E *to, int64_t size, int64_t first, F factor) {
   int64_t last = first + CHUNK < size ? first + CHUNK : size;
   for (int64_t i = first + threadIdx.x * 8; i < last; i += 256 * 8 * 4) {
     typename Vec<E>::v8 v[4];
@@ -99,26 +99,32 @@ template <class E> __device__ inline void scale(const E *from, E *to, int64_t si
 #pragma unroll
     for (int u = 0; u < 4; u++)
       if (i + u * 2048 < last) {
-        if (factor != 1.f)
-          for (int e = 0; e < 8; e++) v[u][e] = (E)((float)v[u][e] * factor);
+        if (factor != 1)
+          for (int e = 0; e < 8; e++) v[u][e] = (E)(float)((F)(float)v[u][e] * factor);
         store8<E>(to + i + u * 2048, v[u], last - (i + u * 2048));
       }
   }
+}
+
+template <int N, class F> __device__ inline void scale_one(const Tensors<N> &t, int i, int64_t first, F factor) {
+  if (t.types[i] == OOB_FP32) scale((const float *)t.from[i], (float *)t.to[i], t.sizes[i], first, factor);
+  else if (t.types[i] == OOB_BF16) scale((const bf16 *)t.from[i], (bf16 *)t.to[i], t.sizes[i], first, factor);
+  else scale((const fp16 *)t.from[i], (fp16 *)t.to[i], t.sizes[i], first, factor);
 }
 
 /* Each workgroup adds up the first pass's sums itself, in the same order, in place of a launch between the two. */
 template <int N> __global__ __launch_bounds__(256) void k_scale(Tensors<N> t, const double *sums, int n, float max_norm, const float *given, float *norm) {
   float s = given ? *given : (float)sqrt(add_up(sums, n)); /* as it is returned: one that is given back does the same */
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = s;
-  float factor = s > max_norm && s < INFINITY ? (float)((double)max_norm / s) : 1.f;
+  double factor = s > max_norm && s < INFINITY ? (double)max_norm / s : 1;
+  bool small = factor < 0x1p-126; /* below, 32 bits lose its digits: the products are formed in 64 */
   int chunks = t.until[t.n - 1];
   for (int c = chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) { /* from the end: what was read last is still in the last-level cache */
     int64_t first;
     int i = find(t, c, first);
-    if (factor == 1.f && t.to[i] == t.from[i]) continue;
-    if (t.types[i] == OOB_FP32) scale((const float *)t.from[i], (float *)t.to[i], t.sizes[i], first, factor);
-    else if (t.types[i] == OOB_BF16) scale((const bf16 *)t.from[i], (bf16 *)t.to[i], t.sizes[i], first, factor);
-    else scale((const fp16 *)t.from[i], (fp16 *)t.to[i], t.sizes[i], first, factor);
+    if ((float)factor == 1.f && t.to[i] == t.from[i]) continue;
+    if (small) scale_one(t, i, first, factor);
+    else scale_one(t, i, first, (float)factor);
   }
 }
 

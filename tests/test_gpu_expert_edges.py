@@ -128,3 +128,15 @@ def test_clip_goes_by_the_norm_that_it_returns(P):
             P.clip_gradients(g, bound, norm=norm, out=b)
             assert all(torch.equal(u, v) for u, v in zip(a, b)), (n, bound)
         assert all(torch.equal(u, v) for u, v in zip(a, g)), n
+
+
+def test_clip_by_factors_that_32_bits_hardly_hold(P):
+    """max_norm / norm below the smallest normal float: the results are ordinary numbers and keep their digits."""
+    for t in ALL[::2]:
+        for bound in (1e-3, 1e-10):
+            g = rand(5000, t=t, std=3e36)
+            before = g.clone()
+            norm = P.clip_gradients([g], bound).double().item()
+            want = before.double() * (bound / norm)
+            # the bound and the norm are rounded to 32 bits, the quotient and the product in 64
+            within(g, want, (U[t] + 4 * 2.0 ** -24) * want.abs() + TINY[t], "clipped")
