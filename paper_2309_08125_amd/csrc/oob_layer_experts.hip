@@ -247,7 +247,7 @@ __device__ __forceinline__ void finish(const Product &g, f32x16 (&acc)[TM / WM /
         if (bias)
 #pragma unroll
           for (int e = 0; e < 8; e++) v[e] += (float)add[j][h][e];
-        if (ACT != OOB_ACT_NONE && g.Z) { /* rounded to the type, as y is: half the memory between the passes; act' sees the rounding, act does not */
+        if (g.Z) { /* rounded to the type, as y is: half the memory between the passes; act' sees the rounding, act does not */
 #pragma unroll
           for (int e = 0; e < 8; e++) out[e] = (E)v[e];
           store8<E>((E *)g.Z + at * g.ldz + n, out, FULL ? 8 : g.N - n);
@@ -448,7 +448,6 @@ template <class E> __global__ __launch_bounds__(256) void k_experts_join(Experts
   }
   Product one = g;
   if (g.bias) one.bias = (const E *)g.bias + (int64_t)f.expert * g.N;
-  if (g.act == OOB_ACT_NONE) one.Z = nullptr;
   epilogue<E>(one, f.first + m, n, v);
 }
 

@@ -79,7 +79,7 @@ typedef struct oob_expert_linear_t {
   int64_t R, T, N, K;      /* rows, rows of x (R = T per, so R where rows is NULL); N, K >= 1; each below 2^31 */
   const int32_t *offsets, *rows; /* [E + 1], [R] or NULL */
   const void *x, *w, *bias; /* w [E][N][K], bias [E][N] or NULL, contiguous but for w's strides */
-  void *y, *z;             /* [R][N]; z or NULL: what the backward pass needs where act is not NONE */
+  void *y, *z;             /* [R][N]; z or NULL: what the backward pass needs where act is not NONE (y without act otherwise) */
   int64_t x_stride, w_stride, expert_stride, y_stride, z_stride; /* w: between rows and between experts */
 } oob_expert_linear_t;
 

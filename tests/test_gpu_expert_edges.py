@@ -140,3 +140,22 @@ def test_clip_by_factors_that_32_bits_hardly_hold(P):
             want = before.double() * (bound / norm)
             # the bound and the norm are rounded to 32 bits, the quotient and the product in 64
             within(g, want, (U[t] + 4 * 2.0 ** -24) * want.abs() + TINY[t], "clipped")
+
+
+# ---- z of a product without activation --------------------------------------------------------------------------
+@pytest.mark.parametrize("T,E,N,K", [(40, 3, 48, 64), (40, 3, 47, 33), (800, 4, 2048, 72), (2048, 4, 4096, 64), (2048, 4, 8192, 2048)])
+def test_z_without_an_activation(P, T, E, N, K):
+    """z[r] = x w^T + bias whatever the activation is: tiles of every size, and those whose depth is divided."""
+    from paper_2309_08125_amd import expert
+
+    lib = expert._load()
+    offsets, rows, _ = P.expert_rows(torch.randint(0, E, (T, 1), dtype=torch.int32, device="cuda"), E)
+    x, w, b = rand(T, K), rand(E, N, K, std=K ** -0.5), rand(E, N)
+    y, z = torch.full((T, N), 3.0, dtype=x.dtype, device="cuda"), torch.full((T, N), 5.0, dtype=x.dtype, device="cuda")
+    p = expert.oob_expert_linear_t(0, 0, E, 1, T, T, N, K, offsets.data_ptr(), rows.data_ptr(), x.data_ptr(), w.data_ptr(), b.data_ptr(), y.data_ptr(), z.data_ptr(),
+                                   K, K, N * K, N, N)
+    size = lib.oob_expert_linear_workspace_size(C.byref(p))
+    ws = torch.empty(max(size, 1), dtype=torch.uint8, device="cuda")
+    assert lib.oob_expert_linear(C.byref(p), ws.data_ptr(), size, torch.cuda.current_stream().cuda_stream) == P.OOB_OK
+    torch.cuda.synchronize()
+    assert torch.equal(y, P.expert_linear(x, w, offsets, b, rows=rows)) and torch.equal(z, y)
