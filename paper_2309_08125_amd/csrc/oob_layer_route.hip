@@ -67,6 +67,10 @@ __device__ inline uint64_t key_of(double v) {
   return b >> 63 ? ~b : b | 0x8000000000000000ull;
 }
 
+/* The key of a closed expert among keys of 64 bits: after all others, one that a bias of -inf rules out among them, but before NaN.  (Those of 32 bits are never the
+ * last word where two follow one another whose scores are -inf.) */
+constexpr uint64_t CLOSED = 2;
+
 /* sigmoid(l) e^-m: with m the largest min(l, 0) of several, their ratios keep all digits however small they are. */
 __device__ inline float sigmoid_over(float l, float m) { return expf(fminf(l, 0.f) - m) / (1 + expf(-fabsf(l))); }
 
@@ -117,6 +121,7 @@ template <class F, int V, class K> __device__ __forceinline__ F keys_of(const Ro
       if (r.p.bias) c += a.bias[i];
     }
     key[i] = i < a.there ? key_of(c) : 0;
+    if constexpr (sizeof(F) == 8) key[i] = i < a.there && a.x[i] == -INFINITY ? CLOSED : key[i];
     F low = c > best ? best : c; /* a NaN is neither */
     best = c > best ? c : best;
     next = low > next ? low : next;

@@ -159,3 +159,26 @@ def test_z_without_an_activation(P, T, E, N, K):
     assert lib.oob_expert_linear(C.byref(p), ws.data_ptr(), size, torch.cuda.current_stream().cuda_stream) == P.OOB_OK
     torch.cuda.synchronize()
     assert torch.equal(y, P.expert_linear(x, w, offsets, b, rows=rows)) and torch.equal(z, y)
+
+
+# ---- routing ----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("E", [8, 60, 256])
+@pytest.mark.parametrize("T", [3, 3000])
+def test_closed_experts_come_after_those_that_a_bias_rules_out(P, T, E):
+    l = rand(T, E, t=torch.float32)  # noqa: E741
+    closed = torch.rand(T, E, device="cuda") < 0.4
+    l[closed] = -math.inf
+    bias = rand(E, t=torch.float32, std=0.1)
+    bias[torch.rand(E, device="cuda") < 0.5] = -math.inf
+    k = min(E, 64)
+    for score in ("softmax", "sigmoid"):
+        experts, w = P.route(l, k, score, bias=bias)
+        c = X.scores(l.double().cpu(), score) + bias.double().cpu()
+        order = torch.tensor([sorted(range(E), key=lambda e: (bool(closed[t, e]), -float(c[t, e])))[:k] for t in range(min(T, 40))])  # noqa: B023
+        order = torch.where(torch.gather(closed[: len(order)].cpu(), 1, order), -1, order)  # which of the closed ones does not count here
+        got = experts[: len(order)].cpu().long()
+        assert torch.equal(torch.where(torch.gather(closed[: len(order)].cpu(), 1, got), -1, got), order)
+        at = torch.gather(closed, 1, experts.long())
+        assert bool((at.int().cummax(1).values == at.int()).all()) and not bool(w[at].any())
+        # closed ones follow one another by their numbers
+        assert bool(((experts[:, 1:] > experts[:, :-1]) | ~at[:, :-1]).all())
