@@ -96,7 +96,12 @@ template <int V> struct Token {
   int e0;
 };
 
-/* Keys of scores in type F (double, float). */
+/* Whether b is more than a.  In 64 bits NaN is less than everything; in 32 a token that holds one is not sure (see below), and what is absent counts as -inf. */
+__device__ inline bool more(float b, float a) { return b > a; }
+__device__ inline bool more(double b, double a) { return b > a || a != a; }
+template <class F> constexpr F NONE = sizeof(F) == 8 ? (F)NAN : (F)-INFINITY;
+
+/* Keys of scores in type F (double, float), and the best two scores. */
 template <class F, int V, class K> __device__ __forceinline__ F keys_of(const Route &r, const Token<V> &a, int L, float top, K (&key)[V], F &best, F &next) {
   F s[V], total = 0;
   for (int i = 0; i < V; i++) {
@@ -112,9 +117,9 @@ template <class F, int V, class K> __device__ __forceinline__ F keys_of(const Ro
     total = sum_over(total, L);
     if constexpr (sizeof(F) == 4) part = 1 / total;
   }
-  best = next = -INFINITY;
+  best = next = NONE<F>;
   for (int i = 0; i < V; i++) {
-    F c = -INFINITY;
+    F c = sizeof(F) == 8 && i >= a.there ? NONE<F> : (F)-INFINITY;
     if (a.x[i] != -INFINITY) {
       c = s[i];
       if (r.p.score == OOB_ROUTE_SOFTMAX) c = sizeof(F) == 8 ? s[i] / total : s[i] * part;
@@ -122,9 +127,9 @@ template <class F, int V, class K> __device__ __forceinline__ F keys_of(const Ro
     }
     key[i] = i < a.there ? key_of(c) : 0;
     if constexpr (sizeof(F) == 8) key[i] = i < a.there && a.x[i] == -INFINITY ? CLOSED : key[i];
-    F low = c > best ? best : c; /* a NaN is neither */
-    best = c > best ? c : best;
-    next = low > next ? low : next;
+    F low = more(c, best) ? best : c;
+    best = more(c, best) ? c : best;
+    next = more(low, next) ? low : next;
   }
   return total;
 }
@@ -138,10 +143,10 @@ template <class F, int V, class K> __device__ __forceinline__ bool groups(const 
   const oob_route &p = r.p;
   for (int o = 1; o < r.in_group; o *= 2) {
     F b = __shfl_xor(best, o), n = __shfl_xor(next, o);
-    F low = b > best ? best : b; /* second of the four: the lower first or one of the seconds */
-    best = b > best ? b : best;
-    n = n > next ? n : next;
-    next = low > n ? low : n;
+    F low = more(b, best) ? best : b; /* second of the four: the lower first or one of the seconds */
+    best = more(b, best) ? b : best;
+    n = more(n, next) ? n : next;
+    next = more(low, n) ? low : n;
   }
   K of = a.group < p.groups ? key_of(p.group_best == 2 && r.per > 1 ? best + next : best) : 0;
   bool kept = false, sure = true;
@@ -198,8 +203,9 @@ template <bool CHECK, int V, class K> __device__ __forceinline__ bool choose(con
   return sure;
 }
 
-/* LANES: a token's, where they are known (the reductions then have no branches); 0: r.lanes. */
-template <int V, bool SCORES, int LANES> __global__ __launch_bounds__(256) void k_route(Route r) {
+/* LANES: a token's, where they are known (the reductions then have no branches); 0: r.lanes. 32 experts a lane: three waves a SIMD and 12 registers of the way through 64
+ * bits in memory, 16384 tokens of 33 groups of 31 experts 146 us; two waves without it 185 us. */
+template <int V, bool SCORES, int LANES> __global__ __launch_bounds__(256, V == 32 ? 3 : 1) void k_route(Route r) {
   const oob_route &p = r.p;
   const int L = LANES ? LANES : r.lanes, l = lane() & (L - 1);
   const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
@@ -253,9 +259,11 @@ template <int V, bool SCORES, int LANES> __global__ __launch_bounds__(256) void 
     if (p.bias)
 #pragma unroll
       for (int i = 0; i < V; i++) sure &= fabsf(a.bias[i]) <= LARGE;
-    if (p.groups > 1) sure = groups(r, a, L, key, best, next) && sure;
+    if (p.groups > 1) sure = groups(r, a, L, key, best, next) && sure && all == all; /* NaN: some score is */
     sure = choose<true>(r, a, L, key, expert) && sure;
     if (__ballot(live && !sure)) {
+#pragma unroll
+      for (int i = 0; i < V; i++) asm("" : "+v"(a.x[i])); /* conditions on it are formed anew, not kept from above in scalar registers */
       uint64_t wide[V];
       double b, n;
       keys_of<double>(r, a, L, top, wide, b, n);

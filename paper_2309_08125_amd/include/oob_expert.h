@@ -32,7 +32,7 @@ extern "C" {
  * What is compared: c = s + bias (compared in 64 bits), and l itself where there is neither a bias nor a
  * group (the same order).  NaN comes after everything, closed experts included.
  * groups > 1: experts are `groups` runs of E / groups; a group counts what its `group_best` largest c add
- * up to, and the keep_groups best groups take part, of equals those that come first.
+ * up to (NaN where fewer are numbers), and the keep_groups best groups take part, of equals those that come first.
  * experts[t]: the k largest c in falling order, of equals the first.  weights[t]: scale s of these, and with
  * renormalize scale s / (sum of s of these), formed from their logits alone whatever the size of s, 0 where all are closed. */
 enum { OOB_ROUTE_SOFTMAX = 0, OOB_ROUTE_SIGMOID = 1 };

@@ -182,3 +182,20 @@ def test_closed_experts_come_after_those_that_a_bias_rules_out(P, T, E):
         assert bool((at.int().cummax(1).values == at.int()).all()) and not bool(w[at].any())
         # closed ones follow one another by their numbers
         assert bool(((experts[:, 1:] > experts[:, :-1]) | ~at[:, :-1]).all())
+
+
+@pytest.mark.parametrize("groups,per,keep,k", [(2, 2, 1, 1), (4, 2, 2, 3), (8, 32, 4, 8), (5, 3, 2, 4), (64, 16, 3, 9), (3, 341, 2, 6)])
+def test_groups_that_hold_nan_come_after_all_others(P, groups, per, keep, k):
+    """What a group's best add up to is NaN where a number is missing, and NaN comes after everything, a group of closed experts included."""
+    for t in ALL:
+        l = rand(60, groups, per, t=t)  # noqa: E741
+        l[torch.rand(60, groups, device="cuda") < 0.3] = -math.inf
+        nan = torch.rand(60, groups, device="cuda") < 0.4
+        l[:, :, 1:][nan] = math.nan  # one number is left
+        l[::7][nan[::7]] = math.nan  # or none
+        l = l.view(60, -1)  # noqa: E741
+        for best in (1, 2):
+            for bias in (None, rand(groups * per, t=torch.float32, std=0.1)):
+                experts, _ = P.route(l, k, "sigmoid", bias=bias, groups=groups, keep_groups=keep, group_best=best)
+                want = X.choose(l.double().cpu(), k, "sigmoid", None if bias is None else bias.double().cpu(), groups, keep, best)
+                assert torch.equal(experts.cpu().long(), want), (t, best)
