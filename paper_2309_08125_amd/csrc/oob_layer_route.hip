@@ -405,16 +405,22 @@ bool route_ok(const oob_route *p, bool forward) {
   return !forward || (p->weights && multiple(p->weights, 4) && multiple(p->bias, 4));
 }
 
-template <int V> void route(const Route &r, hipStream_t st) {
+template <int V, int LANES> void route(const Route &r, hipStream_t st) {
   unsigned n = (unsigned)((r.p.T * r.lanes + 255) / 256);
-  bool scores = r.p.bias || r.p.groups > 1;
-  if (V == 8 && r.lanes == 32) {
-    if (scores) k_route<V, true, 32><<<n, 256, 0, st>>>(r);
-    else k_route<V, false, 32><<<n, 256, 0, st>>>(r);
-  } else {
-    if (scores) k_route<V, true, 0><<<n, 256, 0, st>>>(r);
-    else k_route<V, false, 0><<<n, 256, 0, st>>>(r);
+  if (r.p.bias || r.p.groups > 1) k_route<V, true, LANES><<<n, 256, 0, st>>>(r);
+  else k_route<V, false, LANES><<<n, 256, 0, st>>>(r);
+}
+/* Where tokens fill the GPU (V is 8 then, unless groups are small or experts many) and have eight lanes or more, their number is compiled in: 65536 tokens, 8 of 64, 128, 256 and 512
+ * experts in 8 groups 20, 32, 58 and 110 us, with lanes as a number 23, 37, 63 and 118; without groups and bias 9, 16, 33 and 68 against 10, 18, 35 and 71.  Fewer lanes take less than
+ * the host's call. */
+template <int V> void route(const Route &r, hipStream_t st) {
+  if constexpr (V == 8) {
+    if (r.lanes == 8) return route<V, 8>(r, st);
+    if (r.lanes == 16) return route<V, 16>(r, st);
+    if (r.lanes == 32) return route<V, 32>(r, st);
+    if (r.lanes == 64) return route<V, 64>(r, st);
   }
+  route<V, 0>(r, st);
 }
 
 /* ---- the chosen pairs in order of their experts ------------------------------------------------------------------------

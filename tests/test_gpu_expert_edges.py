@@ -199,3 +199,22 @@ def test_groups_that_hold_nan_come_after_all_others(P, groups, per, keep, k):
                 experts, _ = P.route(l, k, "sigmoid", bias=bias, groups=groups, keep_groups=keep, group_best=best)
                 want = X.choose(l.double().cpu(), k, "sigmoid", None if bias is None else bias.double().cpu(), groups, keep, best)
                 assert torch.equal(experts.cpu().long(), want), (t, best)
+
+
+@pytest.mark.parametrize("E", [16, 60, 64, 100, 128, 129, 256, 500, 512, 1024])
+def test_route_of_every_number_of_lanes(P, E):
+    """As many tokens as fill the GPU, where a token's lanes are known when it is compiled, against the definition and against few tokens."""
+    T = 64 * 2048 * 8 // E + 3
+    for groups, keep in ((1, 1), (4, 3)):
+        if E % groups:
+            continue
+        for t in ALL:
+            l, bias = rand(T, E, t=t), rand(E, t=torch.float32, std=0.1)  # noqa: E741
+            l[:: 3, :: 5], l[5, 1] = -math.inf, math.nan
+            for score, b, renormalize in (("sigmoid", bias, True), ("softmax", bias, False), ("softmax", None, True)):
+                kind = dict(score=score, bias=b, groups=groups, keep_groups=keep, renormalize=renormalize)
+                (experts, w), (few, few_w) = P.route(l, 6, **kind), P.route(l[-40:], 6, **kind)
+                assert torch.equal(experts[-40:], few)
+                within(w[-40:], few_w.double(), 4e-6 * few_w.double().abs() + 1e-30, "weights")
+                want = X.choose(l[:40].double().cpu(), 6, score, None if b is None else b.double().cpu(), groups, keep, 2)
+                assert torch.equal(experts[:40].cpu().long(), want), (groups, t, score)
