@@ -134,8 +134,9 @@ template <class F, int V, class K> __device__ __forceinline__ F keys_of(const Ro
   return total;
 }
 
-/* By how much a score and a bias of at most 4 formed in 32 bits may be off: the sum of up to 1024 exponentials 1.3e-6 of itself (16 in a row, then 6
- * halvings), the exponentials' arguments 4e-7, three more roundings 2e-7, the bias's addition 3e-7.  Larger biases are left to 64 bits. */
+/* By how much a score and a bias of at most 4 formed in 32 bits may be off: the sum of up to 1024 exponentials 2.2e-6 of itself (32 in a row in a lane, then 6
+ * halvings: 37 roundings of 2^-24; 16 in a row 1.3e-6), the exponentials' arguments 4e-7, three more roundings 2e-7, the bias's addition 3e-7: 3.1e-6 in all.  Larger
+ * biases are left to 64 bits. */
 constexpr float OFF = 4e-6f, LARGE = 4.f;
 
 /* Closes the experts of the groups that are not kept; false: in 32 bits, two groups' sums lie too close to tell. */

@@ -142,6 +142,15 @@ def test_clip_by_factors_that_32_bits_hardly_hold(P):
             within(g, want, (U[t] + 4 * 2.0 ** -24) * want.abs() + TINY[t], "clipped")
 
 
+def test_clip_in_place_below_the_bound_changes_nothing(P):
+    for t in ALL:
+        for sizes in ([1], [70, 40_000], [65] * 300):
+            g = [rand(n, t=t) for n in sizes]
+            before = [a.clone() for a in g]
+            norm = P.clip_gradients(g, 1.01 * float(P.gradient_norm(g)))
+            assert all(torch.equal(a, b) for a, b in zip(g, before)) and torch.equal(norm, P.gradient_norm(before))
+
+
 # ---- z of a product without activation --------------------------------------------------------------------------
 @pytest.mark.parametrize("T,E,N,K", [(40, 3, 48, 64), (40, 3, 47, 33), (800, 4, 2048, 72), (2048, 4, 4096, 64), (2048, 4, 8192, 2048)])
 def test_z_without_an_activation(P, T, E, N, K):
@@ -201,6 +210,19 @@ def test_groups_that_hold_nan_come_after_all_others(P, groups, per, keep, k):
                 assert torch.equal(experts.cpu().long(), want), (t, best)
 
 
+@pytest.mark.parametrize("groups,per", [(33, 31), (3, 341), (64, 16), (1, 1000)])
+def test_scores_closer_than_32_bits_tell(P, groups, per):
+    """As many experts in one lane as there can be: scores that differ by less than their errors in 32 bits are compared in 64."""
+    E = groups * per
+    bias = torch.zeros(E, device="cuda")
+    for step in (0.0, 1e-7, 3e-6, 1e-5, 1e-4, 1e-3, 1e-2):  # softmax scores around 1 / E, their differences from none to far beyond the errors
+        l = (torch.randn(24, E, device="cuda") * step * E).clamp(-4, 4)  # noqa: E741
+        for b in (bias, bias + 1.0, rand(E, t=torch.float32, std=0.2)):
+            experts, _ = P.route(l, 7, "softmax", bias=b, groups=groups, keep_groups=max(1, groups // 3), group_best=2)
+            want = X.choose(l.double().cpu(), 7, "softmax", b.double().cpu(), groups, max(1, groups // 3), 2)
+            assert torch.equal(experts.cpu().long(), want), step
+
+
 @pytest.mark.parametrize("E", [16, 60, 64, 100, 128, 129, 256, 500, 512, 1024])
 def test_route_of_every_number_of_lanes(P, E):
     """As many tokens as fill the GPU, where a token's lanes are known when it is compiled, against the definition and against few tokens."""
@@ -218,3 +240,23 @@ def test_route_of_every_number_of_lanes(P, E):
                 within(w[-40:], few_w.double(), 4e-6 * few_w.double().abs() + 1e-30, "weights")
                 want = X.choose(l[:40].double().cpu(), 6, score, None if b is None else b.double().cpu(), groups, keep, 2)
                 assert torch.equal(experts[:40].cpu().long(), want), (groups, t, score)
+
+
+# ---- gradients with offsets and rows out of range ------------------------------------------------------------------
+def test_dx_where_offsets_and_rows_are_out_of_range(P):
+    T, k, E, N, K = 40, 2, 4, 24, 64
+    x, w, dy = rand(T, K), rand(E, N, K), rand(T * k, N)
+    rows = torch.randperm(T * k, device="cuda").int()
+    rows[5], rows[6], rows[79] = -7, T * k, 2147483647
+    out = torch.full((T * k, K), 3.0, dtype=x.dtype, device="cuda")
+    dx, dw, db = P.expert_linear_backward(dy, x, w, ints(-5, 20, 20, 1 << 30, -1), rows=rows, out=out)
+    want = torch.cat([dy[:20].double() @ w[0].double(), dy[20:].double() @ w[2].double()])  # dx goes by the rows of dy alone
+    size = torch.cat([dy[:20].double().abs() @ w[0].double().abs(), dy[20:].double().abs() @ w[2].double().abs()])
+    within(dx, want, U[x.dtype] * want.abs() + EPS * size + TINY[x.dtype], "dx")
+    token = rows[:20].long().div(k, rounding_mode="floor")
+    a = torch.where(((token < 0) | (token >= T))[:, None], 0.0, x.double()[token.clamp(0, T - 1)])
+    want = dy[:20].double().t() @ a
+    within(dw[0], want, U[x.dtype] * want.abs() + EPS * dy[:20].double().abs().t() @ a.abs() + TINY[x.dtype], "dw")
+    for e, part in ((0, dy[:20]), (2, dy[20:])):
+        want = part.double().sum(0)
+        within(db[e], want, U[x.dtype] * want.abs() + EPS * part.double().abs().sum(0) + TINY[x.dtype], "db")
