@@ -289,8 +289,8 @@ struct Where { int expert, left, k, part; int64_t row, n0; const char *pa, *pb; 
 
 /* Rows of y (BK: W as it is), of dx (W by its columns) or, DW, the matrices dw[e] = dz^T x over the rows of e.  A workgroup takes one tile after the other, every
  * gridDim-th: the first loads of the next are asked for before the present one's epilogue.
- * 8192 rows, 8 experts, 4096 x 8192, bfloat16 (550 GFLOP each): y 620 us, dx 510, dw 555; a library's eight products of 1024 rows, without bias, activation and z, 497, 622 and 618.  Matrix
- * cores are busy 60 % of the time that a unit has a tile, at 1.8 GHz; without the loads y takes 510 us, without the epilogue 535.  Few rows: 16 tokens, 8 experts of 2048 x 2048: 13.2 us,
+ * 8192 rows, 8 experts, 4096 x 8192, bfloat16 (550 GFLOP each): y 620 us, dx 510, dw 555; a library's eight products of 1024 rows, without bias, activation and z, 497, 622 and 618.  Of
+ * the time that a unit has a tile the matrix cores are busy 59 % (y), 76 % (dx's whole rounds) and 51 % (dw), at 2.0, 1.75 and 2.0 GHz.  Few rows: 16 tokens, 8 experts of 2048 x 2048: 13.2 us,
  * 5.1 TB/s of matrices (two buffers: 19.2).
  * Large tiles that are left over from whole rounds of the GPU, where they would keep few compute units busy for a round, are left to a second launch (REST), in which k
  * is divided among several workgroups that leave their sums, and a third that joins them.  8192 rows, 8 experts, 4096 x 8192, dx: 576 tiles,
@@ -408,7 +408,9 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_experts(Experts x) {
         case OOB_ACT_GELU_TANH: OOB_FINISH(OOB_ACT_GELU_TANH, true); break;
         default: OOB_FINISH(OOB_ACT_NONE, true);
       }
-      wait_but<STORES<TM, TN, WM, WN>>(); /* the next tile's loads, which are older than the stores, have landed; the stores have not */
+      /* The next tile's loads, which are older than the stores, have landed; the stores need not have.  They are counted in order, so that with two buffers the next tile's first
+       * step waits for them (vmcnt(0) in `back`); with four they have two steps' time. */
+      wait_but<STORES<TM, TN, WM, WN>>();
     } else {
       switch (g.act) {
         case OOB_ACT_RELU: OOB_FINISH(OOB_ACT_RELU, false); break;
@@ -643,10 +645,12 @@ int64_t tiles(int64_t n, int tile) { return (n + tile - 1) / tile; }
 /* Tiles of R rows: as many as the worst division into E experts has. */
 int64_t row_tiles(int64_t R, int E, int tile) { return R / tile + (R < E ? R : E); }
 
-/* By the rows that an expert has on average. */
+/* By the rows that an expert has on average, if all experts are here: where some are elsewhere R counts their pairs too, and the host does not know how many are not.  A tile of 256 is
+ * then taken where few have rows: 4096 tokens, 2 choices, 2 of 8 experts here, 2048 x 2048 y 49 us, the middle one 32; 4 choices, 1 of 4 experts, 2048 x 512 41, the small one 18.  Where
+ * there are enough of them it is the better one all the same: 4 choices, 32 of 128 experts, 2048 x 2048 82 us, the middle one 89; 2 of 8 experts, 4096 x 8192 153 and 159. */
 int choose_tile(int64_t R, int E, int64_t N) {
   int64_t mean = R / E;
-  if (mean >= 192 && tiles(R, 256) * tiles(N, 256) >= 112) return 256; /* 4096 x 2048 x 2048, 8 experts: 49 us, the middle one 56; of 64 tiles 77 and 55 */
+  if (mean >= 192 && tiles(R, 256) * tiles(N, 256) >= 112) return 256; /* 4096 rows, 8 experts, 2048 x 2048: 49 us, the middle one 56 (8192 rows in uneven runs: 99 and 85); of 64 tiles 77 and 55 */
   if (mean >= 96 && tiles(R, 128) * tiles(N, 128) >= 192) return 128;
   return 64;
 }

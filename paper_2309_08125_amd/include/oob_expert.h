@@ -76,7 +76,7 @@ int oob_expert_rows(const int32_t *experts, int64_t n, int first, int E, int32_t
 typedef struct oob_expert_linear_t {
   int dtype, act;          /* OOB_BF16 or OOB_FP16; OOB_ACT_* */
   int E, per;              /* experts, at most OOB_EXPERT_MAX; pairs of a token (rows NULL: 1) */
-  int64_t R, T, N, K;      /* rows, rows of x (R = T per, so R where rows is NULL); N, K >= 1; each below 2^31 */
+  int64_t R, T, N, K;      /* rows, rows of x (R = T per, so R where rows is NULL), below 2^31; N and K from 1 to 2^21 - 1 */
   const int32_t *offsets, *rows; /* [E + 1], [R] or NULL */
   const void *x, *w, *bias; /* w [E][N][K], bias [E][N] or NULL, contiguous but for w's strides */
   void *y, *z;             /* [R][N]; z or NULL: what the backward pass needs where act is not NONE (y without act otherwise) */
